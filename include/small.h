@@ -71,6 +71,7 @@ enum {
     SMALL_MATH_TF32 = 1u << 4,   /* TF32 tensor-core products, FP32 accumulate */
     SMALL_MATH_3XTF32 = 2u << 4, /* three TF32 products per term (hi*hi + hi*lo + lo*hi), FP32 accumulate */
     SMALL_RELU_MID = 4u,   /* small_dwpw_conv2d only: max(x, 0) on the depthwise result, before the 1x1 convolution */
+    SMALL_SILU = 8u,       /* small_group_norm only: out = y / (1 + exp(-y)); not together with SMALL_RELU */
     SMALL_MATH_MASK = 3u << 4
 };
 
@@ -361,6 +362,70 @@ int small_set_fc_chain_tile(small_ctx *ctx, int images);
 int small_fc_chain_fused(const int *widths, int L, unsigned math);
 /* 1 if small_fc runs this layer on the tensor cores under the given math mode, else 0. */
 int small_fc_uses_tensor_cores(int N, int J, int K, unsigned math);
+
+/* ---- the layers of an attention block (the paper has no counterpart: its networks have none; float tensors, the same blocked
+ * layout and the same conventions) ---------------------------------------------------------------------------------------- */
+
+/* Group normalisation with an activation: the channels are dealt out in order to `groups` groups of C / groups (which must
+ * be whole: SMALL_ERR_SHAPE), each image's group is brought to mean 0 and variance 1 over its channels and the whole plane, and
+ *     out = act(gamma[c] * (in - mean) / sqrt(variance + eps) + beta[c])            variance = mean of squared deviations
+ * gamma, beta: C floats each, or NULL (1, 0).  eps: finite and >= 0.  flags: SMALL_RELU or SMALL_SILU or neither.  out may equal in.
+ * workspace: device, 16-byte aligned, small_group_norm_workspace_bytes bytes; may be NULL where that is 0 - planes whose group fits
+ * a cluster's shared memory, which are read once.  Calls that may run at the same time need workspaces of their own.  The mean is
+ * taken first and the deviations are summed after it, all sums in FP32.  A value that is not finite makes its image's group NaN.
+ * Errors: INVALID_ARG, SHAPE, ALIGN, OVERLAP, WORKSPACE (needed and NULL). */
+size_t small_group_norm_workspace_bytes(int N, int C, int H, int W, int groups);
+int small_group_norm(small_ctx *ctx, const float *in, const float *gamma, const float *beta, float *out, void *workspace,
+                     int N, int C, int H, int W, int groups, float eps, unsigned flags, void *stream);
+
+/* Attention over the pixels of a plane.  Head h of `heads` has channels h * D .. h * D + D - 1 of q and out; keys and values
+ * have kv_heads heads, each shared by heads / kv_heads (whole: SMALL_ERR_SHAPE) neighbouring query heads.  For query pixel
+ * i = (qy, qx) of the QH x QW plane and key pixel j = (ky, kx) of the KH x KW plane
+ *     x_ij = s_ij + bias[h][qy - ky + KH - 1][qx - kx + KW - 1]     s_ij = scale * sum_d q[i][d] * k[j][d],  or with cap > 0
+ *                                                                   s_ij = cap * tanh(that / cap)
+ *     out[i][d] = sum_j exp(x_ij) * v[j][d] / sum_j exp(x_ij)
+ * (computed with the running maximum taken off).  A query plane of 1 x 1 is attention pooling.
+ * q: blocked, heads * D channels; k, v: blocked, kv_heads * D channels; out: blocked, heads * D channels, pad lanes written as +0.
+ * q_stride, k_stride, v_stride: floats from one image to the next, 0 for a tensor of its own; q, k and v may be runs of whole
+ * channel blocks of one stacked tensor (a stride below the run's own size is SMALL_ERR_SHAPE, one not a multiple of 4 floats
+ * SMALL_ERR_ALIGN).
+ * bias: float[heads][QH + KH - 1][QW + KW - 1], a value for each displacement, or NULL.  -inf keeps a pair apart; any finite value,
+ * the type's lowest too, is a number to be added.
+ * q_extents, k_extents: int32[N][2], the rows and columns of image n's plane that hold its pixels (clamped to the plane), or
+ * NULL for whole planes.  Key pixels outside are not read as keys: whatever they hold, NaN too, has no part in the result.  Query
+ * pixels outside, and queries that no key is left for, get 0.
+ * scale, cap: finite, cap >= 0 (0: no cap).  D at most 128, any number; heads, kv_heads at least 1.
+ * flags: one SMALL_MATH_*.  FP32: FP32 multiply-adds.  TF32, 3XTF32: both products on the tensor cores where the shape has the
+ * queries for it, operands of 11 significant bits, or two such terms each (three products: FP32 accuracy); scores, their
+ * maxima and sums and the accumulation over keys in FP32.
+ * workspace: device, 16-byte aligned, small_attention_workspace_bytes bytes (keys and values as the tensor cores read them; 0 and
+ * NULL where they are read as they lie).  Calls that may run at the same time, and graphs that may be replayed at the same
+ * time, need workspaces of their own.
+ * Errors: INVALID_ARG, SHAPE, ALIGN, OVERLAP (out or workspace with anything read), WORKSPACE (too small). */
+size_t small_attention_workspace_bytes(int N, int heads, int kv_heads, int D, int QH, int QW, int KH, int KW, unsigned math);
+int small_attention(small_ctx *ctx, const float *q, const float *k, const float *v, const float *bias, const int32_t *q_extents,
+                    const int32_t *k_extents, float *out, void *workspace, size_t workspace_bytes, int N, int heads, int kv_heads,
+                    int D, int QH, int QW, int KH, int KW, long long q_stride, long long k_stride, long long v_stride,
+                    float scale, float cap, unsigned flags, void *stream);
+
+/* 1 x 1 convolution (a full reduction where H = W = 1) whose images bring low-rank adapters of their own beside the filters
+ * that all of them share:
+ *     out = act(W in + bias + scale[a] * Up[a] (Down[a] in))        a = adapter[n], the adapter of image n
+ * An index outside 0 .. adapters - 1 (-1, say) means none.  Down: [R][C], Up: [K][R], R at most 128.
+ * small_pack_adapters lays out all adapters once: down: device float[adapters][R][C], up: device float[adapters][K][R],
+ * packed: device, small_adapter_elems floats. */
+size_t small_adapter_elems(int adapters, int C, int K, int R);
+int small_pack_adapters(small_ctx *ctx, const float *down, const float *up, float *packed, int adapters, int C, int K, int R,
+                        void *stream);
+/* in: blocked [N][C][H][W]; w_blk: from small_pack_conv_weights(C, K, 1, 1, math); bias: K floats or NULL; adapter: device
+ * int32[N]; scale: device float[adapters] or NULL (1); out: blocked [N][K][H][W].  flags: SMALL_RELU, SMALL_ACCUMULATE (out_previous is
+ * added in front of the activation) and one SMALL_MATH_* for both parts.  workspace: device, 16-byte aligned,
+ * small_adapted_conv2d_workspace_bytes bytes (the products with Down); calls that may run at the same time need their own.
+ * Errors as small_conv2d, and WORKSPACE (NULL). */
+size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R);
+int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,
+                         const int32_t *adapter, const float *scale, float *out, void *workspace, int N, int C, int K, int H, int W,
+                         int R, int adapters, unsigned flags, void *stream);
 
 /* ---- networks (Section 5.3: layers share intermediate buffers; Section 5.4: end-to-end inference) -- */
 

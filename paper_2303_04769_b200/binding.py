@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libsmall.so")
 
 # mirrors of the header's enums
 OK = 0
-RELU, ACCUMULATE, RELU_MID = 1, 2, 4
+RELU, ACCUMULATE, RELU_MID, SILU = 1, 2, 4, 8
 MATH_FP32, MATH_TF32, MATH_3XTF32 = 0 << 4, 1 << 4, 2 << 4
 POOL_MAX, POOL_AVG = 0, 1
 OP_CONV, OP_DWCONV, OP_POOL, OP_RELU, OP_ADD, OP_FC, OP_DWPW, OP_CONVPOOL = range(8)
@@ -33,6 +33,8 @@ EXPORTS = [
     "small_net_host_staging_bytes", "small_run_net_host", "small_static_workspace_bytes", "small_run_net_static",
     "small_q_packed_bytes", "small_q_pack", "small_q_unpack", "small_q_conv_weight_bytes", "small_q_pack_conv_weights", "small_q_conv2d",
     "small_q_dw_weight_bytes", "small_q_pack_dw_weights", "small_q_dwconv2d", "small_q_maxpool2d", "small_q_relu",
+    "small_group_norm_workspace_bytes", "small_group_norm", "small_attention_workspace_bytes", "small_attention",
+    "small_adapter_elems", "small_pack_adapters", "small_adapted_conv2d_workspace_bytes", "small_adapted_conv2d",
 ]
 
 
@@ -143,6 +145,19 @@ def lib():
     L.small_q_dwconv2d.argtypes = [P, P, P, P, P] + [I] * 16 + [U, P]
     L.small_q_maxpool2d.argtypes = [P, P, P] + [I] * 12 + [P]
     L.small_q_relu.argtypes = [P, P, P, I, I, I, I, I, P]
+    F, Q = ctypes.c_float, ctypes.c_longlong
+    L.small_group_norm_workspace_bytes.argtypes = [I] * 5
+    L.small_group_norm_workspace_bytes.restype = Z
+    L.small_group_norm.argtypes = [P] * 6 + [I] * 5 + [F, U, P]
+    L.small_attention_workspace_bytes.argtypes = [I] * 8 + [U]
+    L.small_attention_workspace_bytes.restype = Z
+    L.small_attention.argtypes = [P] * 9 + [Z] + [I] * 8 + [Q] * 3 + [F, F, U, P]
+    L.small_adapter_elems.argtypes = [I] * 4
+    L.small_adapter_elems.restype = Z
+    L.small_pack_adapters.argtypes = [P] * 4 + [I] * 4 + [P]
+    L.small_adapted_conv2d_workspace_bytes.argtypes = [I] * 6
+    L.small_adapted_conv2d_workspace_bytes.restype = Z
+    L.small_adapted_conv2d.argtypes = [P] * 9 + [I] * 7 + [U, P]
     _lib = L
     return L
 
@@ -447,6 +462,46 @@ def small_measure_tf32_peak(ctx, n=128, iters=4096, stream=None):
     _check(lib().small_measure_tf32_peak(ctx, n, iters, _ptr(cycles), ctypes.byref(tf), ctypes.byref(cpm), _stream(stream)),
            "small_measure_tf32_peak")
     return tf.value, cpm.value
+
+
+# ---- the layers of an attention block ----
+
+def small_group_norm_workspace_bytes(N, C, H, W, groups):
+    return lib().small_group_norm_workspace_bytes(N, C, H, W, groups)
+
+
+def small_group_norm(ctx, inp, gamma, beta, out, workspace, N, C, H, W, groups, eps=1e-5, flags=0, stream=None):
+    _n.small_group_norm(ctx, inp, gamma, beta, out, workspace, N, C, H, W, groups, eps, flags, stream)
+
+
+def small_attention_workspace_bytes(N, heads, kv_heads, D, q_plane, k_plane, math):
+    return lib().small_attention_workspace_bytes(N, heads, kv_heads, D, *q_plane, *k_plane, math)
+
+
+def small_attention(ctx, q, k, v, out, workspace, workspace_bytes, N, heads, kv_heads, D, q_plane, k_plane, scale=None, cap=0.0,
+                    bias=None, q_extents=None, k_extents=None, strides=(0, 0, 0), flags=0, stream=None):
+    """q_plane, k_plane: (rows, columns).  scale: 1 / sqrt(D) where None.  strides: floats between the images of q, k and v (0: a
+    tensor of its own).  extents: int32[N][2] tensors of valid rows and columns."""
+    _n.small_attention(ctx, q, k, v, bias, q_extents, k_extents, out, workspace, workspace_bytes, N, heads, kv_heads, D, q_plane[0], q_plane[1],
+                       k_plane[0], k_plane[1], strides[0], strides[1], strides[2], D ** -0.5 if scale is None else scale, cap, flags, stream)
+
+
+def small_adapter_elems(adapters, C, K, R):
+    return lib().small_adapter_elems(adapters, C, K, R)
+
+
+def small_pack_adapters(ctx, down, up, packed, adapters, C, K, R, stream=None):
+    """down: float[adapters][R][C], up: float[adapters][K][R]."""
+    _n.small_pack_adapters(ctx, down, up, packed, adapters, C, K, R, stream)
+
+
+def small_adapted_conv2d_workspace_bytes(N, C, K, H, W, R):
+    return lib().small_adapted_conv2d_workspace_bytes(N, C, K, H, W, R)
+
+
+def small_adapted_conv2d(ctx, inp, w_blk, bias, packed, adapter, scale, out, workspace, N, C, K, H, W, R, adapters, flags=0, stream=None):
+    """adapter: int32[N], the adapter of each image (-1: none); scale: float[adapters] or None."""
+    _n.small_adapted_conv2d(ctx, inp, w_blk, bias, packed, adapter, scale, out, workspace, N, C, K, H, W, R, adapters, flags, stream)
 
 
 # ---- quantised layers (uint8 tensors; qp = (z_in, z_w, z_out, mult, shift)) ----

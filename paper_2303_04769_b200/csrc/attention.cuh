@@ -1,0 +1,48 @@
+// What the attention kernels share: the call's arguments, where a head's channels and an image's valid pixels lie.
+#pragma once
+
+#include "entry.cuh"
+
+namespace small {
+
+struct AttnArgs {
+    const float *q, *k, *v, *bias;
+    const int32_t *q_ext, *k_ext;
+    float *out;
+    void *ws;
+    int N, heads, kv_heads, D, QH, QW, KH, KW;
+    int QP, KP, CB;                                      // pixels of the planes, channel blocks of q and out
+    long long q_stride, k_stride, v_stride;              // floats between images
+    float scale, cap;
+};
+
+#ifdef __CUDACC__
+// An image's valid rows and columns.
+__device__ __forceinline__ int2 extent(const int32_t *e, int n, int h, int w) {
+    if (!e) return make_int2(h, w);
+    return make_int2(min(max(e[2 * n], 0), h), min(max(e[2 * n + 1], 0), w));
+}
+// Float of channel c, pixel p in an image of `pixels`.
+__device__ __forceinline__ size_t at(int c, int p, int pixels) { return ((size_t)(c >> 5) * pixels + p) * 32 + (c & 31); }
+
+// Places in the bias table: of_query(i) - of_key(j) is that of the pair's displacement.
+__device__ __forceinline__ int of_query(const AttnArgs &a, int i) { return (i / a.QW + a.KH - 1) * (a.QW + a.KW - 1) + i % a.QW + a.KW - 1; }
+__device__ __forceinline__ int of_key(const AttnArgs &a, int y, int x) { return y * (a.QW + a.KW - 1) + x; }
+
+// cap * tanh(x / cap).  Below 1/2 by Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + x^2 / (7 + x^2 / 9)))), whose
+// relative error there is some x^10 / 1e7, 1e-10; above by 1 - 2 / (1 + exp(2 x)), which is not small there.
+__device__ __forceinline__ float capped(float x, float cap, float over_cap) {
+    const float t = x * over_cap, u = fabsf(t);
+    const float big = 1.0f - __fdividef(2.0f, 1.0f + __expf(2.0f * fminf(u, 16.0f)));
+    const float s = t * t;
+    const float num = fmaf(s, fmaf(s, 1.0f, 105.0f), 945.0f), den = fmaf(s, fmaf(s, 15.0f, 420.0f), 945.0f);
+    const float small = u * __fdividef(num, den);
+    const float r = u < 0.5f ? small : big;
+    return u == u ? copysignf(cap * r, t) : x;
+}
+#endif
+
+// attention.cu
+int launch_attention_fp32(small_ctx *, const AttnArgs &, cudaStream_t);
+
+}  // namespace small

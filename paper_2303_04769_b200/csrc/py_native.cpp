@@ -1,7 +1,7 @@
 // Python module `_native`: the functions of include/small.h called with Python arguments.  A layer call has some twenty
 // arguments; converting them one by one in ctypes and asking torch for a Stream object took 7 of the 10 microseconds of a
 // small layer's call, more than its kernel.  Here a wrapper per function is generated from the function's own C type:
-// integers are read directly, device pointers come from an int, None or an object with data_ptr(), and a stream argument of
+// integers and floats are read directly, device pointers come from an int, None or an object with data_ptr(), and a stream argument of
 // None (always the last one) is the current stream's handle.  Argument marshalling only, like binding.py, which names the
 // parameters and adds the defaults.
 #define PY_SSIZE_T_CLEAN
@@ -87,6 +87,11 @@ bool convert(PyObject *o, T &out, bool is_stream) {
         else ok = is_stream ? to_stream(o, p) : to_memory(o, p);
         out = static_cast<T>(p);
         return ok;
+    } else if constexpr (std::is_floating_point_v<T>) {
+        const double v = PyFloat_AsDouble(o);
+        if (v == -1.0 && PyErr_Occurred()) return false;
+        out = static_cast<T>(v);
+        return true;
     } else {
         long long v;
         if (!to_int(o, v)) return false;
@@ -135,7 +140,8 @@ struct Call<Fn, kStatus> {
     S(small_conv2d) S(small_group_conv2d) S(small_dwpw_conv2d) S(small_conv_maxpool2d) S(small_dwconv2d) S(small_pool2d) S(small_relu) \
     S(small_scale_shift) S(small_upsample_nearest) S(small_add) S(small_fc) S(small_gap_fc) S(small_set_net_fusion) S(small_run_net) \
     S(small_run_net_host) S(small_run_net_static) S(small_q_pack) S(small_q_unpack) S(small_q_pack_conv_weights) S(small_q_conv2d) \
-    S(small_q_pack_dw_weights) S(small_q_dwconv2d) S(small_q_maxpool2d) S(small_q_relu) V(small_out_size) V(small_packed_elems) V(small_q_packed_bytes)
+    S(small_q_pack_dw_weights) S(small_q_dwconv2d) S(small_q_maxpool2d) S(small_q_relu) \
+    S(small_group_norm) S(small_attention) S(small_pack_adapters) S(small_adapted_conv2d) V(small_out_size) V(small_packed_elems) V(small_q_packed_bytes)
 
 EACH(STATUS, VALUE)
 
