@@ -138,6 +138,9 @@ bool attention_shape_ok(int N, int heads, int kv_heads, int D, int QH, int QW, i
     return N <= 65535 && heads <= 65535 && ((long long)QH + KH) * ((long long)QW + KW) <= (1ll << 30);
 }
 
+// Tiles of 128 queries: worth it where at least some of a tile is real.
+bool on_tensor_cores(int QP, unsigned math) { return math != SMALL_MATH_FP32 && QP >= 32; }
+
 }  // namespace
 
 int launch_attention_fp32(small_ctx *ctx, const AttnArgs &a, cudaStream_t st) {
@@ -150,7 +153,7 @@ using namespace small;
 
 SMALL_API size_t small_attention_workspace_bytes(int N, int heads, int kv_heads, int D, int QH, int QW, int KH, int KW, unsigned math) {
     if (!attention_shape_ok(N, heads, kv_heads, D, QH, QW, KH, KW) || (math & ~SMALL_MATH_MASK) || !one_math_mode(math)) return 0;
-    return 0;
+    return on_tensor_cores(QH * QW, math) ? attention_tc_workspace(N, kv_heads, D, KH * KW) : 0;
 }
 
 SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, const float *v, const float *bias, const int32_t *q_extents,
@@ -186,5 +189,7 @@ SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, co
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
     const AttnArgs a{q, k, v, bias, q_extents, k_extents, out, workspace, N, heads, kv_heads, D, QH, QW, KH, KW, QP, KP, blocks_of(heads * D),
                      q_stride, k_stride, v_stride, scale, cap};
-    return launch_attention_fp32(ctx, a, static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (on_tensor_cores(QP, flags)) return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
+    return launch_attention_fp32(ctx, a, st);
 }

@@ -44,5 +44,8 @@ __device__ __forceinline__ float capped(float x, float cap, float over_cap) {
 
 // attention.cu
 int launch_attention_fp32(small_ctx *, const AttnArgs &, cudaStream_t);
+// attention_tc.cu: the tensor-core form, and the workspace it takes
+size_t attention_tc_workspace(int N, int kv_heads, int D, int KP);
+int launch_attention_tc(small_ctx *, const AttnArgs &, bool x3, cudaStream_t);
 
 }  // namespace small

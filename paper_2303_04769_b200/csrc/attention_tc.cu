@@ -1,0 +1,531 @@
+// Attention over the pixels of a plane on the tensor cores (tcgen05, kind::f16), at TF32's or FP32's accuracy.
+//
+// Operands.  A float x is x_hi + x_lo, two halves of 11 significant bits each after a power of two has brought the largest value of its
+// row (queries) or tile (keys, values) to 2^14 .. 2^15, so nothing the sums can see is lost to half precision's range.  3xTF32 forms
+// hi*hi + hi*lo + lo*hi, TF32 hi*hi alone: a half has TF32's 11 bits, and kind::f16 runs at twice kind::tf32's rate and reads half
+// the bytes.  Weights exp(x - m) are scaled by 2^14 for the same reason; the sum of weights too, so that it cancels.
+//
+// attention_tiles_kernel lays the valid keys and values of each image out once, 128 keys a tile, as the MMAs read them: keys
+// [key][hi | lo channels], values transposed [channel][hi keys | lo keys], rows of 128 bytes swizzled, so that a tile is two plain
+// bulk copies.  Every block of queries (QP / 256 a head, times the heads that share them) reads them so; converting in each
+// block instead would repeat it that many times beside the softmax, which is what bounds the main kernel.
+//
+// attention_tc_kernel: a block takes one or two tiles of 128 queries of a head.  Warp 8 loads tiles, warp 9 issues MMAs, warps 0-3
+// and 4-7 do the softmax of a tile each, a thread a row.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128
+// columns); a thread reads its row, and writes the weights as halves over it, where they are the second product's A operand.  While
+// one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
+// added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
+// thousands of keys would add up (5e-8 a step), and no rescaling of tensor memory is needed when the maximum grows.
+#include <cuda_fp16.h>
+#include <cmath>
+
+#include "attention.cuh"
+#include "sm100.cuh"
+
+namespace small {
+namespace {
+using namespace sm100;
+
+constexpr int kTile = 128;               // queries and keys of a tile
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLift = 14.0f;           // weights are scaled by 2^14
+
+// The exponent that brings |x| <= most to below 2^15: x * lift(e) and back by drop(e).
+__device__ __forceinline__ int top_exponent(float most) { return min(max((int)(__float_as_uint(most) >> 23), 15), 254); }     // most >= 0
+__device__ __forceinline__ float lift(int e) { return __uint_as_float((uint32_t)(268 - e) << 23); }
+__device__ __forceinline__ float drop(int e) { return __uint_as_float((uint32_t)(e - 14) << 23); }
+
+// |x|; what is not finite does not count: it stays what it is at any scale, and must not take its tile's other values with it.
+__device__ __forceinline__ float magnitude(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
+
+__device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Two floats -> their leading halves and what these leave.
+__device__ __forceinline__ void split(float a, float b, uint32_t &hi, uint32_t &lo) {
+    const float ah = __uint_as_float(__float_as_uint(a) & 0xffffe000u), bh = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
+    hi = pack_halves(ah, bh);
+    lo = pack_halves(a - ah, b - bh);
+}
+// The same for operands: what is left of a value that is not finite is 0, or it would turn infinities into NaN in every product.
+__device__ __forceinline__ void split_finite(float a, float b, uint32_t &hi, uint32_t &lo) {
+    split(a, b, hi, lo);
+    if (!(fabsf(a) <= 65504.0f) || !(fabsf(b) <= 65504.0f)) {
+        const float ah = __uint_as_float(__float_as_uint(a) & 0xffffe000u), bh = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
+        hi = pack_halves(fabsf(a) <= 65504.0f ? ah : a, fabsf(b) <= 65504.0f ? bh : b);
+        lo = pack_halves(fabsf(a) <= 65504.0f ? a - ah : 0.0f, fabsf(b) <= 65504.0f ? b - bh : 0.0f);
+    }
+}
+
+// Byte of the 16-byte chunk that holds columns c .. c + 7 of row r: atoms of 64 columns, `rows` rows of 128 bytes each, swizzled.
+__device__ __forceinline__ uint32_t chunk_at(int r, int c, int rows) {
+    return (uint32_t)(c >> 6) * rows * 128 + r * 128 + ((((uint32_t)c >> 3 & 7) ^ (r & 7)) << 4);
+}
+
+// Eight consecutive channels from c on of a head's `D` at pixel p, 0 behind the last.
+__device__ __forceinline__ void load8(const float *x, int first, int c, int D, int p, int pixels, float (&v)[8]) {
+    if (((first | D) & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 u = c + i < D ? *reinterpret_cast<const float4 *>(x + at(first + c + i, p, pixels)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[i] = u.x; v[i + 1] = u.y; v[i + 2] = u.z; v[i + 3] = u.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < D ? x[at(first + c + i, p, pixels)] : 0.0f;
+    }
+}
+
+// Workspace: [N][kv_heads][tiles]{keys: DP * 512 bytes, values: DP * 512 bytes}; int[N][tiles][128], the keys' places in the bias table
+// (of_key); float[N][kv_heads][tiles][2], how to undo the scaling.
+__device__ __forceinline__ int *key_places(const AttnArgs &a, int tiles, int tile_bytes) {
+    return reinterpret_cast<int *>(static_cast<char *>(a.ws) + (size_t)a.N * a.kv_heads * tiles * 2 * tile_bytes);
+}
+__device__ __forceinline__ float *undo_scaling(const AttnArgs &a, int tiles, int tile_bytes) {
+    return reinterpret_cast<float *>(key_places(a, tiles, tile_bytes) + (size_t)a.N * tiles * kTile);
+}
+template <int DP>
+__global__ void __launch_bounds__(256) attention_tiles_kernel(const AttnArgs a, int tiles) {
+    constexpr int kBytes = DP * 512, kChunks = DP / 8;
+    __shared__ float most_s[8];
+    extern __shared__ float values[];                    // [128][DP + 1]
+    grid_dep_sync();
+    grid_dep_trigger();
+    const int t = blockIdx.x >> 1, hk = blockIdx.y, n = blockIdx.z;
+    const bool is_v = blockIdx.x & 1;
+    const int2 e = extent(a.k_ext, n, a.KH, a.KW);
+    const int keys = e.x * e.y;
+    if (t * kTile >= keys) return;
+    const size_t tile = ((size_t)n * a.kv_heads + hk) * tiles + t;
+    char *out = static_cast<char *>(a.ws) + tile * 2 * kBytes + (is_v ? kBytes : 0);
+    const float *x = is_v ? a.v + n * a.v_stride : a.k + n * a.k_stride;
+    // a thread takes half of a key's channels, in chunks of eight
+    const int r = threadIdx.x >> 1, j = t * kTile + r, half = threadIdx.x & 1;
+    const int p = j < keys ? j / e.y * a.KW + j % e.y : -1;
+    constexpr int kMine = (kChunks + 1) / 2;
+    float v[kMine][8], most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        if (p >= 0) load8(x, hk * a.D, (half * kMine + i) * 8, a.D, p, a.KP, v[i]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (p < 0) v[i][u] = 0.0f;
+            most = fmaxf(most, magnitude(v[i][u]));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    if ((threadIdx.x & 31) == 0) most_s[threadIdx.x >> 5] = most;
+    if (is_v)
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) values[r * (DP + 1) + (half * kMine + i) * 8 + u] = v[i][u];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, most_s[i]);
+    const int ex = top_exponent(most);
+    const float up = lift(ex);
+    if (threadIdx.x == 0) undo_scaling(a, tiles, kBytes)[tile * 2 + is_v] = drop(ex);
+    if (!is_v && hk == 0 && half == 0) key_places(a, tiles, kBytes)[((size_t)n * tiles + t) * kTile + r] = p >= 0 ? of_key(a, j / e.y, j % e.y) : 0;
+    auto store = [&](const float (&w)[8], int row, int c_hi, int c_lo, int rows) {
+        uint4 hi, lo;
+        split_finite(w[0] * up, w[1] * up, hi.x, lo.x); split_finite(w[2] * up, w[3] * up, hi.y, lo.y);
+        split_finite(w[4] * up, w[5] * up, hi.z, lo.z); split_finite(w[6] * up, w[7] * up, hi.w, lo.w);
+        *reinterpret_cast<uint4 *>(out + chunk_at(row, c_hi, rows)) = hi;
+        *reinterpret_cast<uint4 *>(out + chunk_at(row, c_lo, rows)) = lo;
+    };
+    if (!is_v) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int c = (half * kMine + i) * 8;
+            store(v[i], r, c, DP + c, kTile);
+        }
+        return;
+    }
+    for (int i = threadIdx.x; i < DP * 16; i += 256) {
+        const int d = i % DP, k0 = i / DP * 8;
+        float w[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) w[u] = values[(k0 + u) * (DP + 1) + d];
+        store(w, d, k0, kTile + k0, DP);
+    }
+}
+
+// D[tmem] (+)= A * B^T in halves, FP32 accumulate, M = 128, K = 16; A from shared memory, or from tensor memory (two halves a column).
+__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ uint32_t f16_desc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+constexpr int kThreads = 320;
+constexpr int kMaxRing = 4;
+
+struct TcArgs {
+    AttnArgs a;
+    int tiles;                           // key tiles of a whole plane, as the workspace counts them
+    int q_tiles;                         // tiles of queries that a block takes: 1 or 2
+    int ring;                            // shared-memory slots for key and value tiles
+    int table_floats;                    // of the bias table's part in shared memory; 0: read where it lies
+    int *status;
+    uint32_t limit;
+};
+
+struct Barriers {
+    uint64_t full[kMaxRing], empty[kMaxRing];            // a slot has its tile; its last product is done
+    uint64_t scores[3], weights[3];                      // a buffer has a tile's scores; 128 threads have written their weights
+    uint64_t part[2], taken[2];                          // a query tile's product with the values is there; 128 threads have added it
+    uint64_t drained;                                    // after a wait that ran out: all MMAs are done
+};
+
+// kGeneral: scores pass through the cap and the bias table and are kept in tensor memory between the two passes over them.
+template <int DP, bool kX3, bool kGeneral>
+__global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const TcArgs c) {
+    constexpr int kBytes = DP * 512;                     // of a tile of queries, keys or values
+    extern __shared__ char raw[];
+    __shared__ Barriers bars;
+    __shared__ uint32_t tmem_s;
+    __shared__ int gave_up;
+    const AttnArgs &a = c.a;
+    const int n = blockIdx.z, h = blockIdx.y, hk = h / (a.heads / a.kv_heads);
+    const int i0 = blockIdx.x * c.q_tiles * kTile, nq = min(c.q_tiles, (a.QP - i0 + kTile - 1) / kTile);
+    const int warp = warp_index();
+    char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    char *queries = base, *slots = base + c.q_tiles * kBytes;
+    float *table = reinterpret_cast<float *>(slots + c.ring * kBytes);
+    if (warp == 9) tmem_alloc(smem_u32(&tmem_s), 512);
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < kMaxRing; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.empty[i]), 1); }
+        for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&bars.scores[i]), 1); mbar_init(smem_u32(&bars.weights[i]), kTile); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.part[i]), 1); mbar_init(smem_u32(&bars.taken[i]), kTile); }
+        mbar_init(smem_u32(&bars.drained), 1);
+        mbar_fence_init();
+    }
+    // What this kernel reads besides the tiles is older than the kernel in front of it, which has waited for all before itself.
+    const int2 qe = extent(a.q_ext, n, a.QH, a.QW), ke = extent(a.k_ext, n, a.KH, a.KW);
+    const int keys = ke.x * ke.y, tiles = (keys + kTile - 1) / kTile, steps = tiles * nq;
+    const int wg = warp >> 2, row = threadIdx.x & (kTile - 1);          // of the softmax warps
+    const int TW = a.QW + a.KW - 1;
+    const float *bias = a.bias ? a.bias + (size_t)h * (a.QH + a.KH - 1) * TW : nullptr;
+    int qoff = 0;
+    float q_drop = 0.0f;
+    const int i = i0 + wg * kTile + row;
+    if (warp < 8 && wg < nq) {
+        const float *q = a.q + n * a.q_stride;
+        char *mine = queries + wg * kBytes;
+        const float sign = a.scale < 0.0f ? -1.0f : 1.0f;               // the scale's sign goes with the queries: what is left is >= 0
+        float most = 0.0f;
+        float v[8];
+        for (int ch = 0; ch < DP; ch += 8) {
+            if (i < a.QP) load8(q, h * a.D, ch, a.D, i, a.QP, v);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) most = fmaxf(most, i < a.QP ? magnitude(v[u]) : 0.0f);
+        }
+        const int ex = top_exponent(most);
+        const float up = lift(ex) * sign;
+        q_drop = fabsf(a.scale) * drop(ex);
+        for (int ch = 0; ch < DP; ch += 8) {
+            if (i < a.QP) load8(q, h * a.D, ch, a.D, i, a.QP, v);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = i < a.QP ? v[u] * up : 0.0f;
+            uint4 hi, lo;
+            split_finite(v[0], v[1], hi.x, lo.x); split_finite(v[2], v[3], hi.y, lo.y);
+            split_finite(v[4], v[5], hi.z, lo.z); split_finite(v[6], v[7], hi.w, lo.w);
+            *reinterpret_cast<uint4 *>(mine + chunk_at(row, ch, kTile)) = hi;
+            *reinterpret_cast<uint4 *>(mine + chunk_at(row, DP + ch, kTile)) = lo;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (kGeneral && bias && warp < 8) {
+        qoff = of_query(a, min(i, a.QP - 1));
+        if (c.table_floats) {                            // the table's rows that these queries meet
+            const int y0 = i0 / a.QW, y1 = min(i0 + nq * kTile, a.QP) - 1;
+            const int count = (y1 / a.QW - y0 + a.KH) * TW;
+            const float *from = bias + (size_t)y0 * TW;
+            for (int e = threadIdx.x; e < count; e += 256) table[e] = from[e];
+            qoff -= y0 * TW;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_s;
+    volatile int *stop = &gave_up;
+    const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), scores = smem_u32(bars.scores), weights = smem_u32(bars.weights),
+                   part = smem_u32(bars.part), taken = smem_u32(bars.taken);
+    int issued = 0;                                      // tiles, by warp 8
+    auto s_at = [&](int buffer) { return tmem + buffer * kTile; };
+    auto o_at = [&](int wgi) { return tmem + 3 * kTile + wgi * DP; };
+
+    if (warp == 8) {
+        grid_dep_sync();                                 // the tiles
+        grid_dep_trigger();
+        const char *from = static_cast<const char *>(a.ws) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2 * kBytes;
+        // without the low parts: values' lie in the second half of their tile, keys' too but for 32 channels, whose rows hold both
+        const uint32_t k_bytes = kX3 || DP == 32 ? kBytes : kBytes / 2, v_bytes = kX3 ? kBytes : kBytes / 2;
+        for (int x = 0; x < 2 * tiles; ++x) {
+            const int slot = x % c.ring, use = x / c.ring;
+            if (use && !mbar_wait_uniform(empty + slot * 8, (use - 1) & 1, stop, c.status, c.limit)) break;
+            const uint32_t bytes = x & 1 ? v_bytes : k_bytes;
+            if (elect_one()) {
+                mbar_expect_tx(full + slot * 8, bytes);
+                bulk_load(smem_u32(slots + slot * kBytes), from + (size_t)x * kBytes, bytes, full + slot * 8);
+            }
+            __syncwarp();
+            ++issued;
+        }
+    } else if (warp == 9) {
+        const uint32_t q_lo = smem_desc_lo(smem_u32(queries)), slot_lo = smem_desc_lo(smem_u32(slots));
+        auto column = [&](int col, int rows) { return (uint32_t)(((col >> 6) * rows * 128 + (col & 63) * 2) >> 4); };
+        auto score = [&](int s) -> bool {                // queries x keys of step s
+            const int j = s % nq, t = s / nq, slot = 2 * t % c.ring, use = 2 * t / c.ring;
+            if (j == 0 && !mbar_wait_uniform(full + slot * 8, use & 1, stop, c.status, c.limit)) return false;
+            // the buffer's last weights, those of step s - 3, are used up (with one query tile `taken` has said so in front of step s - 2's product)
+            if (nq == 2 && s >= 3 && !mbar_wait_uniform(part + ((s - 3) & 1) * 8, ((s - 3) >> 1) & 1, stop, c.status, c.limit)) return false;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t d = s_at(s % 3), qa = q_lo + j * (kBytes >> 4), kb = slot_lo + slot * (kBytes >> 4), desc = f16_desc(kTile);
+#pragma unroll
+                for (int term = kX3 ? 0 : 2; term < 3; ++term)           // small terms first
+#pragma unroll
+                    for (int k = 0; k < DP; k += 16)
+                        mma_f16(d, qa + column(k + (term == 0 ? DP : 0), kTile), kb + column(k + (term == 1 ? DP : 0), kTile), desc, k > 0 || term > (kX3 ? 0 : 2));
+                mma_commit(scores + s % 3 * 8);
+                if (j == nq - 1) mma_commit(empty + slot * 8);
+            }
+            __syncwarp();
+            return true;
+        };
+        bool ok = true;
+        for (int s = 0; s < min(2, steps) && ok; ++s) ok = score(s);
+        for (int s = 0; s < steps && ok; ++s) {
+            const int j = s % nq, t = s / nq, x = 2 * t + 1, slot = x % c.ring, use = x / c.ring;
+            ok = mbar_wait_uniform(weights + s % 3 * 8, (s / 3) & 1, stop, c.status, c.limit);
+            if (ok && t > 0) ok = mbar_wait_uniform(taken + j * 8, (t - 1) & 1, stop, c.status, c.limit);
+            if (ok && j == 0) ok = mbar_wait_uniform(full + slot * 8, use & 1, stop, c.status, c.limit);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t d = o_at(j), pa = s_at(s % 3), vb = slot_lo + slot * (kBytes >> 4), desc = f16_desc(DP);
+#pragma unroll
+                for (int term = kX3 ? 0 : 2; term < 3; ++term)
+#pragma unroll
+                    for (int k = 0; k < kTile; k += 16)
+                        mma_f16_tmem(d, pa + (k >> 5) * 32 + (k & 16) / 2 + (term == 0 ? 16 : 0), vb + column(k + (term == 1 ? kTile : 0), DP), desc,
+                                     k > 0 || term > (kX3 ? 0 : 2));
+                mma_commit(part + j * 8);
+                if (j == nq - 1) mma_commit(empty + slot * 8);
+            }
+            __syncwarp();
+            if (s + 2 < steps) ok = score(s + 2);
+        }
+        if (!ok) {
+            if (elect_one()) mma_commit(smem_u32(&bars.drained));
+            __syncwarp();
+            mbar_wait(smem_u32(&bars.drained), 0, c.limit);
+        }
+    } else if (wg < nq) {
+        grid_dep_sync();
+        const float *undo = undo_scaling(a, c.tiles, kBytes) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2;
+        const int *places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kTile;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;               // this warp's 32 lanes of tensor memory
+        const float over_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+        const float *at_table = c.table_floats ? table : bias;
+        float o[DP], l = 0.0f, m = kGeneral ? -INFINITY : INFINITY;      // m: the running maximum, or 14 - that in powers of two
+#pragma unroll
+        for (int d = 0; d < DP; ++d) o[d] = 0.0f;
+        bool ok = true;
+        for (int t = 0; t < tiles; ++t) {
+            const int s = t * nq + wg, buffer = s % 3, left = min(keys - t * kTile, kTile);
+            const float k_drop = undo[2 * t], v_drop = undo[2 * t + 1] * (1.0f / (1 << (int)kLift));
+            ok = mbar_wait_uniform(scores + buffer * 8, (s / 3) & 1, stop, c.status, c.limit);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t st = s_at(buffer) + lanes;
+            const float f = q_drop * k_drop;
+            float top = -INFINITY, shrink;
+#pragma unroll 1
+            for (int g = 0; g < kTile; g += 32) {
+                float v[32];
+                tmem_ld32(st + g, v);
+                if (kGeneral) {
+                    if (a.cap > 0.0f)
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) v[u] = capped(v[u] * f, a.cap, over_cap);
+                    else
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) v[u] *= f;
+                    if (bias)
+#pragma unroll
+                        for (int u = 0; u < 32; u += 4) {
+                            const int4 k4 = *reinterpret_cast<const int4 *>(places + t * kTile + g + u);
+                            v[u] += at_table[qoff - k4.x]; v[u + 1] += at_table[qoff - k4.y]; v[u + 2] += at_table[qoff - k4.z]; v[u + 3] += at_table[qoff - k4.w];
+                        }
+                }
+                if (left < kTile)
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) v[u] = g + u < left ? v[u] : -INFINITY;
+#pragma unroll
+                for (int u = 0; u < 32; ++u) top = fmaxf(top, v[u]);
+                if (kGeneral) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) w[u] = __float_as_uint(v[u]);
+                    tmem_st32(st + g, w);
+                }
+            }
+            if (kGeneral) tmem_st_wait();
+            // weights are exp2(v * scale2 + m) or exp2((v - from) * log2(e) + 14)
+            const float scale2 = f * kLog2e;
+            float from = 0.0f;
+            if (kGeneral) {
+                const float now = fmaxf(m, top);
+                from = now == -INFINITY ? 0.0f : now;    // nothing to weigh yet
+                shrink = exp2_fast((m - from) * kLog2e);
+                m = now;
+            } else {
+                const float now = fminf(m, fmaf(-top, scale2, kLift));
+                shrink = exp2_fast(now - m);
+                m = now;
+            }
+            float sum[4] = {};
+#pragma unroll 1
+            for (int g = 0; g < kTile; g += 32) {
+                float v[32];
+                tmem_ld32(st + g, v);
+#pragma unroll
+                for (int u = 0; u < 32; ++u) v[u] = exp2_fast(kGeneral ? fmaf(v[u] - from, kLog2e, kLift) : fmaf(v[u], scale2, m));
+                if (!kGeneral && left < kTile)
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) v[u] = g + u < left ? v[u] : 0.0f;
+                uint32_t w[32];
+#pragma unroll
+                for (int u = 0; u < 32; u += 2) {
+                    sum[u & 2] += v[u];
+                    sum[(u & 2) + 1] += v[u + 1];
+                    if (kX3) split(v[u], v[u + 1], w[u / 2], w[16 + u / 2]);
+                    else { w[u / 2] = pack_halves(v[u], v[u + 1]); w[16 + u / 2] = 0; }
+                }
+                tmem_st32(st + g, w);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(weights + buffer * 8);
+            l = fmaf(l, shrink, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+            if (__any_sync(~0u, shrink != 1.0f))
+#pragma unroll
+                for (int d = 0; d < DP; ++d) o[d] *= shrink;
+            ok = mbar_wait_uniform(part + wg * 8, t & 1, stop, c.status, c.limit);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int d = 0; d < DP; d += 32) {
+                float v[32];
+                tmem_ld32(o_at(wg) + lanes + d, v);
+#pragma unroll
+                for (int u = 0; u < 32; ++u) o[d + u] = fmaf(v[u], v_drop, o[d + u]);
+            }
+            tc_fence_before();
+            mbar_arrive(taken + wg * 8);
+        }
+        if (i < a.QP) {
+            const bool live = i / a.QW < qe.x && i % a.QW < qe.y && l != 0.0f;
+            const float inv = live ? (1 << (int)kLift) / l : 0.0f;
+            float *out = a.out + (size_t)n * a.CB * a.QP * 32;
+            const int first = h * a.D;
+            if ((a.D & 3) == 0) {
+#pragma unroll
+                for (int d = 0; d < DP; d += 4)
+                    if (d < a.D)
+                        *reinterpret_cast<float4 *>(out + at(first + d, i, a.QP)) =
+                            live ? make_float4(o[d] * inv, o[d + 1] * inv, o[d + 2] * inv, o[d + 3] * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+            } else {
+#pragma unroll
+                for (int d = 0; d < DP; ++d)
+                    if (d < a.D) out[at(first + d, i, a.QP)] = live ? o[d] * inv : 0.0f;
+            }
+            if (h == a.heads - 1)
+                for (int ch = a.heads * a.D; ch < a.CB * 32; ++ch) out[at(ch, i, a.QP)] = 0.0f;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (gave_up && warp == 8)                            // what is still on its way must land before the block ends
+        for (int x = max(0, issued - c.ring); x < issued; ++x) mbar_wait(full + x % c.ring * 8, (x / c.ring) & 1, c.limit);
+    if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+int padded(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
+
+template <int DP>
+int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
+    static std::atomic<unsigned long long> tiled{0}, done[4] = {};
+    const int tiles = ceil_div(a.KP, kTile);
+    const size_t values = sizeof(float) * kTile * (DP + 1);
+    if (int s = allow_shared_memory(ctx, attention_tiles_kernel<DP>, tiled, values)) return s;
+    launch_kernel(ctx, attention_tiles_kernel<DP>, dim3((unsigned)(2 * tiles), (unsigned)a.kv_heads, (unsigned)a.N), dim3(256), values, st, a, tiles);
+    if (int s = check_launch(ctx)) return s;
+    TcArgs c{a, tiles, 1, kMaxRing, 0, ctx->dev_status, ctx->wait_iters};
+    const size_t most = ctx->max_smem_optin - 4096, tile = (size_t)DP * 512;
+    if (DP < 128 && a.QP > kTile) c.q_tiles = 2;
+    while (c.ring > 2 && 1024 + (c.q_tiles + c.ring) * tile > most) --c.ring;
+    if (a.bias) {
+        const int rows = c.q_tiles * kTile, y = (rows + a.QW - 2) / a.QW + 1;        // rows of the plane that such a run of pixels can touch
+        const size_t table = sizeof(float) * ((size_t)(y < a.QH ? y : a.QH) + a.KH - 1) * (a.QW + a.KW - 1);
+        const int fewest = 3 < c.ring ? 3 : c.ring;
+        if (1024 + (c.q_tiles + fewest) * tile + table <= most) {
+            while (1024 + (c.q_tiles + c.ring) * tile + table > most) --c.ring;
+            c.table_floats = (int)(table / 4);
+        }
+    }
+    const size_t smem = 1024 + (c.q_tiles + c.ring) * tile + sizeof(float) * c.table_floats;
+    const bool general = a.bias || a.cap > 0.0f;
+    auto run = [&](auto *kern, std::atomic<unsigned long long> &d) {
+        if (int s = allow_shared_memory(ctx, kern, d, most)) return s;
+        launch_kernel(ctx, kern, dim3((unsigned)ceil_div(a.QP, c.q_tiles * kTile), (unsigned)a.heads, (unsigned)a.N), dim3(kThreads), smem, st, c);
+        return check_launch(ctx);
+    };
+    return x3 ? general ? run(attention_tc_kernel<DP, true, true>, done[0]) : run(attention_tc_kernel<DP, true, false>, done[1])
+              : general ? run(attention_tc_kernel<DP, false, true>, done[2]) : run(attention_tc_kernel<DP, false, false>, done[3]);
+}
+
+}  // namespace
+
+size_t attention_tc_workspace(int N, int kv_heads, int D, int KP) {
+    return (size_t)N * kv_heads * ceil_div(KP, kTile) * ((size_t)padded(D) * 1024 + 2 * sizeof(float)) + (size_t)N * ceil_div(KP, kTile) * kTile * sizeof(int);
+}
+
+int launch_attention_tc(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
+    return padded(a.D) == 32 ? launch<32>(ctx, a, x3, st) : padded(a.D) == 64 ? launch<64>(ctx, a, x3, st) : launch<128>(ctx, a, x3, st);
+}
+
+}  // namespace small
