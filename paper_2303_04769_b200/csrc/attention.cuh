@@ -30,15 +30,12 @@ __device__ __forceinline__ int of_query(const AttnArgs &a, int i) { return (i / 
 __device__ __forceinline__ int of_key(const AttnArgs &a, int y, int x) { return y * (a.QW + a.KW - 1) + x; }
 
 // cap * tanh(x / cap).  Below 1/2 by Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + x^2 / (7 + x^2 / 9)))), whose
-// relative error there is some x^10 / 1e7, 1e-10; above by 1 - 2 / (1 + exp(2 x)), which is not small there.
+// relative error there is some x^10 / 1e7, 1e-10; above as (e - 1) / (e + 1), e = exp(2 x), where neither is a small difference.
 __device__ __forceinline__ float capped(float x, float cap, float over_cap) {
-    const float t = x * over_cap, u = fabsf(t);
-    const float big = 1.0f - __fdividef(2.0f, 1.0f + __expf(2.0f * fminf(u, 16.0f)));
-    const float s = t * t;
-    const float num = fmaf(s, fmaf(s, 1.0f, 105.0f), 945.0f), den = fmaf(s, fmaf(s, 15.0f, 420.0f), 945.0f);
-    const float small = u * __fdividef(num, den);
-    const float r = u < 0.5f ? small : big;
-    return u == u ? copysignf(cap * r, t) : x;
+    const float t = x * over_cap, u = fminf(fabsf(t), 16.0f), s = u * u, e = __expf(2.0f * u);
+    const float num = u < 0.5f ? u * fmaf(s, s + 105.0f, 945.0f) : e - 1.0f;
+    const float den = u < 0.5f ? fmaf(s, fmaf(s, 15.0f, 420.0f), 945.0f) : e + 1.0f;
+    return t == t ? copysignf(cap * __fdividef(num, den), t) : x;
 }
 #endif
 

@@ -10,10 +10,10 @@
 // bulk copies.  Every block of queries (QP / 256 a head, times the heads that share them) reads them so; converting in each
 // block instead would repeat it that many times beside the softmax, which is what bounds the main kernel.
 //
-// attention_tc_kernel: a block takes one or two tiles of 128 queries of a head.  Warp 8 loads tiles, warp 9 issues MMAs, warps 0-3
-// and 4-7 do the softmax of a tile each, a thread a row.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128
-// columns); a thread reads its row, and writes the weights as halves over it, where they are the second product's A operand.  While
-// one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
+// attention_tc_kernel: a block takes one or two tiles of 128 queries of a head.  One warp loads tiles, one issues MMAs, eight do the
+// softmax of each query tile.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128
+// columns); two threads share a row, half of its keys each, and write the weights as halves over the scores, where they are the second
+// product's A operand.  While one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
 // added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
 // thousands of keys would add up (5e-8 a step), and no rescaling of tensor memory is needed when the maximum grows.
 #include <cuda_fp16.h>
@@ -178,6 +178,10 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;
@@ -185,7 +189,29 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return r;
 }
 
-constexpr int kThreads = 320;
+// Two floats as one operand of the packed FP32 instructions.
+__device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
+__device__ __forceinline__ void unpair(uint64_t p, float &a, float &b) { a = __uint_as_float((uint32_t)p); b = __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(taddr) : "memory");
+}
+
 constexpr int kMaxRing = 4;
 
 struct TcArgs {
@@ -198,94 +224,98 @@ struct TcArgs {
     uint32_t limit;
 };
 
-struct Barriers {
+struct Shared {
     uint64_t full[kMaxRing], empty[kMaxRing];            // a slot has its tile; its last product is done
-    uint64_t scores[3], weights[3];                      // a buffer has a tile's scores; 128 threads have written their weights
-    uint64_t part[2], taken[2];                          // a query tile's product with the values is there; 128 threads have added it
+    uint64_t scores[3], weights[3];                      // a buffer has a tile's scores; 256 threads have written their weights
+    uint64_t part[2], taken[2];                          // a query tile's product with the values is there; 256 threads have added it
     uint64_t drained;                                    // after a wait that ran out: all MMAs are done
+    uint32_t tmem;
+    int gave_up;
+    float exchange[2][2][2][kTile];                      // [parity of the key tile][query tile][half of the keys][row]: maxima; at last sums
+    float q_drop[2][kTile];
 };
 
-// kGeneral: scores pass through the cap and the bias table and are kept in tensor memory between the two passes over them.
+// kGeneral: scores pass through the cap and the bias table.
 template <int DP, bool kX3, bool kGeneral>
-__global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const TcArgs c) {
+__global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(const TcArgs c) {
     constexpr int kBytes = DP * 512;                     // of a tile of queries, keys or values
+    constexpr int kHalf = kTile / 2, kOut = DP / 2;      // a thread's keys of a tile, and its channels of the result
     extern __shared__ char raw[];
-    __shared__ Barriers bars;
-    __shared__ uint32_t tmem_s;
-    __shared__ int gave_up;
+    __shared__ Shared sh;
     const AttnArgs &a = c.a;
     const int n = blockIdx.z, h = blockIdx.y, hk = h / (a.heads / a.kv_heads);
     const int i0 = blockIdx.x * c.q_tiles * kTile, nq = min(c.q_tiles, (a.QP - i0 + kTile - 1) / kTile);
-    const int warp = warp_index();
+    const int warp = warp_index(), loader = c.q_tiles * 8, issuer = loader + 1;
     char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     char *queries = base, *slots = base + c.q_tiles * kBytes;
     float *table = reinterpret_cast<float *>(slots + c.ring * kBytes);
-    if (warp == 9) tmem_alloc(smem_u32(&tmem_s), 512);
+    if (warp == issuer) tmem_alloc(smem_u32(&sh.tmem), 512);
     if (threadIdx.x == 0) {
-        gave_up = 0;
-        for (int i = 0; i < kMaxRing; ++i) { mbar_init(smem_u32(&bars.full[i]), 1); mbar_init(smem_u32(&bars.empty[i]), 1); }
-        for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&bars.scores[i]), 1); mbar_init(smem_u32(&bars.weights[i]), kTile); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars.part[i]), 1); mbar_init(smem_u32(&bars.taken[i]), kTile); }
-        mbar_init(smem_u32(&bars.drained), 1);
+        sh.gave_up = 0;
+        for (int i = 0; i < kMaxRing; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
+        for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&sh.scores[i]), 1); mbar_init(smem_u32(&sh.weights[i]), 2 * kTile); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh.part[i]), 1); mbar_init(smem_u32(&sh.taken[i]), 2 * kTile); }
+        mbar_init(smem_u32(&sh.drained), 1);
         mbar_fence_init();
     }
     // What this kernel reads besides the tiles is older than the kernel in front of it, which has waited for all before itself.
     const int2 qe = extent(a.q_ext, n, a.QH, a.QW), ke = extent(a.k_ext, n, a.KH, a.KW);
     const int keys = ke.x * ke.y, tiles = (keys + kTile - 1) / kTile, steps = tiles * nq;
-    const int wg = warp >> 2, row = threadIdx.x & (kTile - 1);          // of the softmax warps
+    const int wg = warp >> 3, half = warp >> 2 & 1, row = threadIdx.x & (kTile - 1);         // of the softmax warps: query tile, half of the keys, row
     const int TW = a.QW + a.KW - 1;
     const float *bias = a.bias ? a.bias + (size_t)h * (a.QH + a.KH - 1) * TW : nullptr;
     int qoff = 0;
-    float q_drop = 0.0f;
     const int i = i0 + wg * kTile + row;
-    if (warp < 8 && wg < nq) {
-        const float *q = a.q + n * a.q_stride;
+    if (wg < nq) {                                       // two neighbouring threads convert a row of the queries
+        const int r = threadIdx.x >> 1 & (kTile - 1), first = (threadIdx.x & 1) * kOut, p = i0 + wg * kTile + r;
         char *mine = queries + wg * kBytes;
-        const float sign = a.scale < 0.0f ? -1.0f : 1.0f;               // the scale's sign goes with the queries: what is left is >= 0
-        float most = 0.0f;
-        float v[8];
-        for (int ch = 0; ch < DP; ch += 8) {
-            if (i < a.QP) load8(q, h * a.D, ch, a.D, i, a.QP, v);
+        float v[kOut / 8][8], most = 0.0f;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) most = fmaxf(most, i < a.QP ? magnitude(v[u]) : 0.0f);
+        for (int k = 0; k < kOut / 8; ++k) {
+            if (p < a.QP) load8(a.q + n * a.q_stride, h * a.D, first + k * 8, a.D, p, a.QP, v[k]);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (p >= a.QP) v[k][u] = 0.0f;
+                most = fmaxf(most, magnitude(v[k][u]));
+            }
         }
+        most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
         const int ex = top_exponent(most);
-        const float up = lift(ex) * sign;
-        q_drop = fabsf(a.scale) * drop(ex);
-        for (int ch = 0; ch < DP; ch += 8) {
-            if (i < a.QP) load8(q, h * a.D, ch, a.D, i, a.QP, v);
+        const float up = a.scale < 0.0f ? -lift(ex) : lift(ex);          // the scale's sign goes with the queries: what is left is >= 0
+        if (first == 0) sh.q_drop[wg][r] = fabsf(a.scale) * drop(ex);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = i < a.QP ? v[u] * up : 0.0f;
+        for (int k = 0; k < kOut / 8; ++k) {
             uint4 hi, lo;
-            split_finite(v[0], v[1], hi.x, lo.x); split_finite(v[2], v[3], hi.y, lo.y);
-            split_finite(v[4], v[5], hi.z, lo.z); split_finite(v[6], v[7], hi.w, lo.w);
-            *reinterpret_cast<uint4 *>(mine + chunk_at(row, ch, kTile)) = hi;
-            *reinterpret_cast<uint4 *>(mine + chunk_at(row, DP + ch, kTile)) = lo;
+            split_finite(v[k][0] * up, v[k][1] * up, hi.x, lo.x); split_finite(v[k][2] * up, v[k][3] * up, hi.y, lo.y);
+            split_finite(v[k][4] * up, v[k][5] * up, hi.z, lo.z); split_finite(v[k][6] * up, v[k][7] * up, hi.w, lo.w);
+            *reinterpret_cast<uint4 *>(mine + chunk_at(r, first + k * 8, kTile)) = hi;
+            *reinterpret_cast<uint4 *>(mine + chunk_at(r, DP + first + k * 8, kTile)) = lo;
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (kGeneral && bias && warp < 8) {
+    if (kGeneral && bias && warp < loader) {
         qoff = of_query(a, min(i, a.QP - 1));
         if (c.table_floats) {                            // the table's rows that these queries meet
             const int y0 = i0 / a.QW, y1 = min(i0 + nq * kTile, a.QP) - 1;
             const int count = (y1 / a.QW - y0 + a.KH) * TW;
             const float *from = bias + (size_t)y0 * TW;
-            for (int e = threadIdx.x; e < count; e += 256) table[e] = from[e];
+#pragma unroll 8
+            for (int e = threadIdx.x; e < count; e += loader * 32) table[e] = from[e];
             qoff -= y0 * TW;
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_s;
-    volatile int *stop = &gave_up;
-    const uint32_t full = smem_u32(bars.full), empty = smem_u32(bars.empty), scores = smem_u32(bars.scores), weights = smem_u32(bars.weights),
-                   part = smem_u32(bars.part), taken = smem_u32(bars.taken);
-    int issued = 0;                                      // tiles, by warp 8
+    const uint32_t tmem = sh.tmem;
+    volatile int *stop = &sh.gave_up;
+    const uint32_t full = smem_u32(sh.full), empty = smem_u32(sh.empty), scores = smem_u32(sh.scores), weights = smem_u32(sh.weights),
+                   part = smem_u32(sh.part), taken = smem_u32(sh.taken);
+    int issued = 0;                                      // tiles, by the loading warp
     auto s_at = [&](int buffer) { return tmem + buffer * kTile; };
-    auto o_at = [&](int wgi) { return tmem + 3 * kTile + wgi * DP; };
+    auto o_at = [&](int tile) { return tmem + 3 * kTile + tile * DP; };
 
-    if (warp == 8) {
+    if (warp == loader) {
         grid_dep_sync();                                 // the tiles
         grid_dep_trigger();
         const char *from = static_cast<const char *>(a.ws) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2 * kBytes;
@@ -302,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const TcArgs 
             __syncwarp();
             ++issued;
         }
-    } else if (warp == 9) {
+    } else if (warp == issuer) {
         const uint32_t q_lo = smem_desc_lo(smem_u32(queries)), slot_lo = smem_desc_lo(smem_u32(slots));
         auto column = [&](int col, int rows) { return (uint32_t)(((col >> 6) * rows * 128 + (col & 63) * 2) >> 4); };
         auto score = [&](int s) -> bool {                // queries x keys of step s
@@ -348,140 +378,183 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tc_kernel(const TcArgs 
             if (s + 2 < steps) ok = score(s + 2);
         }
         if (!ok) {
-            if (elect_one()) mma_commit(smem_u32(&bars.drained));
+            if (elect_one()) mma_commit(smem_u32(&sh.drained));
             __syncwarp();
-            mbar_wait(smem_u32(&bars.drained), 0, c.limit);
+            mbar_wait(smem_u32(&sh.drained), 0, c.limit);
         }
     } else if (wg < nq) {
         grid_dep_sync();
         const float *undo = undo_scaling(a, c.tiles, kBytes) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2;
-        const int *places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kTile;
+        const int *places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kTile + half * kHalf;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;               // this warp's 32 lanes of tensor memory
-        const float over_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
-        const float *at_table = c.table_floats ? table : bias;
-        float o[DP], l = 0.0f, m = kGeneral ? -INFINITY : INFINITY;      // m: the running maximum, or 14 - that in powers of two
+        const float q_drop = sh.q_drop[wg][row], over_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+        const float *at_table = (c.table_floats ? table : bias) + qoff;
+        uint64_t o[kOut / 2];
+        float l = 0.0f, m = kGeneral ? -INFINITY : INFINITY;             // m: the running maximum, or 14 - that in powers of two
 #pragma unroll
-        for (int d = 0; d < DP; ++d) o[d] = 0.0f;
-        bool ok = true;
+        for (int d = 0; d < kOut / 2; ++d) o[d] = 0;
+        // A wait that runs out ends the waits behind it at once; the loop goes on, so that the barrier of these 256 threads is met.
         for (int t = 0; t < tiles; ++t) {
-            const int s = t * nq + wg, buffer = s % 3, left = min(keys - t * kTile, kTile);
+            const int s = t * nq + wg, buffer = s % 3, left = keys - t * kTile - half * kHalf;
             const float k_drop = undo[2 * t], v_drop = undo[2 * t + 1] * (1.0f / (1 << (int)kLift));
-            ok = mbar_wait_uniform(scores + buffer * 8, (s / 3) & 1, stop, c.status, c.limit);
-            if (!ok) break;
+            mbar_wait_uniform(scores + buffer * 8, (s / 3) & 1, stop, c.status, c.limit);
             tc_fence_after();
-            const uint32_t st = s_at(buffer) + lanes;
+            const uint32_t st = s_at(buffer) + lanes + half * kHalf;
             const float f = q_drop * k_drop;
-            float top = -INFINITY, shrink;
-#pragma unroll 1
-            for (int g = 0; g < kTile; g += 32) {
-                float v[32];
+            // scores of 32 keys as the softmax takes them; the largest of each in `top`
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, v[32];
+            auto take = [&](int g) {
                 tmem_ld32(st + g, v);
                 if (kGeneral) {
                     if (a.cap > 0.0f)
 #pragma unroll
                         for (int u = 0; u < 32; ++u) v[u] = capped(v[u] * f, a.cap, over_cap);
-                    else
+                    else if (!bias)
 #pragma unroll
                         for (int u = 0; u < 32; ++u) v[u] *= f;
-                    if (bias)
+                    if (bias) {
+                        const float f1 = a.cap > 0.0f ? 1.0f : f;
+                        const int *place = places + t * kTile + g;
 #pragma unroll
-                        for (int u = 0; u < 32; u += 4) {
-                            const int4 k4 = *reinterpret_cast<const int4 *>(places + t * kTile + g + u);
-                            v[u] += at_table[qoff - k4.x]; v[u + 1] += at_table[qoff - k4.y]; v[u + 2] += at_table[qoff - k4.z]; v[u + 3] += at_table[qoff - k4.w];
+                        for (int u = 0; u < 32; u += 8) {
+                            const int4 k0 = *reinterpret_cast<const int4 *>(place + u), k1 = *reinterpret_cast<const int4 *>(place + u + 4);
+                            if (k1.w - k0.x == 7) {      // one row of the plane: neighbours in the table
+                                const float *b = at_table - k1.w;
+#pragma unroll
+                                for (int w = 0; w < 8; ++w) v[u + w] = fmaf(v[u + w], f1, b[7 - w]);
+                            } else {
+                                v[u] = fmaf(v[u], f1, at_table[-k0.x]); v[u + 1] = fmaf(v[u + 1], f1, at_table[-k0.y]);
+                                v[u + 2] = fmaf(v[u + 2], f1, at_table[-k0.z]); v[u + 3] = fmaf(v[u + 3], f1, at_table[-k0.w]);
+                                v[u + 4] = fmaf(v[u + 4], f1, at_table[-k1.x]); v[u + 5] = fmaf(v[u + 5], f1, at_table[-k1.y]);
+                                v[u + 6] = fmaf(v[u + 6], f1, at_table[-k1.z]); v[u + 7] = fmaf(v[u + 7], f1, at_table[-k1.w]);
+                            }
                         }
+                    }
                 }
-                if (left < kTile)
+                if (left < kHalf)
 #pragma unroll
                     for (int u = 0; u < 32; ++u) v[u] = g + u < left ? v[u] : -INFINITY;
 #pragma unroll
-                for (int u = 0; u < 32; ++u) top = fmaxf(top, v[u]);
-                if (kGeneral) {
-                    uint32_t w[32];
+                for (int u = 0; u < 32; ++u) top[u & 3] = fmaxf(top[u & 3], v[u]);
+            };
+            take(0);
+            if (kGeneral) {                              // kept where the scores were until their turn comes
+                uint32_t w[32];
 #pragma unroll
-                    for (int u = 0; u < 32; ++u) w[u] = __float_as_uint(v[u]);
-                    tmem_st32(st + g, w);
-                }
+                for (int u = 0; u < 32; ++u) w[u] = __float_as_uint(v[u]);
+                tmem_st32(st, w);
             }
-            if (kGeneral) tmem_st_wait();
+            take(32);
+            const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            sh.exchange[t & 1][wg][half][row] = mine;
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + wg) : "memory");
+            const float most = fmaxf(mine, sh.exchange[t & 1][wg][half ^ 1][row]);
             // weights are exp2(v * scale2 + m) or exp2((v - from) * log2(e) + 14)
             const float scale2 = f * kLog2e;
-            float from = 0.0f;
+            float from = 0.0f, shrink;
             if (kGeneral) {
-                const float now = fmaxf(m, top);
+                const float now = fmaxf(m, most);
                 from = now == -INFINITY ? 0.0f : now;    // nothing to weigh yet
                 shrink = exp2_fast((m - from) * kLog2e);
                 m = now;
             } else {
-                const float now = fminf(m, fmaf(-top, scale2, kLift));
+                const float now = fminf(m, fmaf(-most, scale2, kLift));
                 shrink = exp2_fast(now - m);
                 m = now;
             }
-            float sum[4] = {};
-#pragma unroll 1
-            for (int g = 0; g < kTile; g += 32) {
-                float v[32];
-                tmem_ld32(st + g, v);
+            uint64_t sum[2] = {0, 0};
 #pragma unroll
-                for (int u = 0; u < 32; ++u) v[u] = exp2_fast(kGeneral ? fmaf(v[u] - from, kLog2e, kLift) : fmaf(v[u], scale2, m));
-                if (!kGeneral && left < kTile)
-#pragma unroll
-                    for (int u = 0; u < 32; ++u) v[u] = g + u < left ? v[u] : 0.0f;
-                uint32_t w[32];
+            for (int g = 32; g >= 0; g -= 32) {          // the second half's scores are at hand
+                uint32_t hi[8], lo[8];
+                if (g == 0) {
+                    if (kGeneral) tmem_st_wait();
+                    tmem_ld32(st, v);
+                }
 #pragma unroll
                 for (int u = 0; u < 32; u += 2) {
-                    sum[u & 2] += v[u];
-                    sum[(u & 2) + 1] += v[u + 1];
-                    if (kX3) split(v[u], v[u + 1], w[u / 2], w[16 + u / 2]);
-                    else { w[u / 2] = pack_halves(v[u], v[u + 1]); w[16 + u / 2] = 0; }
+                    uint64_t x = pair(v[u], v[u + 1]);
+                    if (kGeneral) x = fma2(add2(x, pair(-from, -from)), pair(kLog2e, kLog2e), pair(kLift, kLift));
+                    else x = fma2(x, pair(scale2, scale2), pair(m, m));
+                    float x0, x1;
+                    unpair(x, x0, x1);
+                    x0 = exp2_fast(x0);
+                    x1 = exp2_fast(x1);
+                    if (!kGeneral && left < kHalf) {     // -inf * 0, where the scores have no scale
+                        x0 = g + u < left ? x0 : 0.0f;
+                        x1 = g + u + 1 < left ? x1 : 0.0f;
+                    }
+                    const uint64_t e = pair(x0, x1);
+                    sum[u >> 1 & 1] = add2(sum[u >> 1 & 1], e);
+                    if (kX3) {
+                        const uint64_t lead = e & 0xffffe000ffffe000ull;
+                        float r0, r1;
+                        unpair(add2(e, lead ^ 0x8000000080000000ull), r0, r1);
+                        hi[u / 2 & 7] = pack_halves(__uint_as_float((uint32_t)lead), __uint_as_float((uint32_t)(lead >> 32)));
+                        lo[u / 2 & 7] = pack_halves(r0, r1);
+                    } else {
+                        hi[u / 2 & 7] = pack_halves(x0, x1);
+                    }
+                    if ((u & 15) == 14) {                // 16 keys are 8 columns of high parts and 8 of low ones, 16 columns on
+                        tmem_st8(st + g + (u & 16) / 2, hi);
+                        if (kX3) tmem_st8(st + g + 16 + (u & 16) / 2, lo);
+                    }
                 }
-                tmem_st32(st + g, w);
             }
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(weights + buffer * 8);
-            l = fmaf(l, shrink, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+            float s0, s1;
+            unpair(add2(sum[0], sum[1]), s0, s1);
+            l = fmaf(l, shrink, s0 + s1);
             if (__any_sync(~0u, shrink != 1.0f))
 #pragma unroll
-                for (int d = 0; d < DP; ++d) o[d] *= shrink;
-            ok = mbar_wait_uniform(part + wg * 8, t & 1, stop, c.status, c.limit);
-            if (!ok) break;
+                for (int d = 0; d < kOut / 2; ++d) o[d] = fma2(o[d], pair(shrink, shrink), 0);
+            mbar_wait_uniform(part + wg * 8, t & 1, stop, c.status, c.limit);
             tc_fence_after();
 #pragma unroll
-            for (int d = 0; d < DP; d += 32) {
-                float v[32];
-                tmem_ld32(o_at(wg) + lanes + d, v);
+            for (int d = 0; d < kOut; d += 16) {
+                float x[16];
+                tmem_ld16(o_at(wg) + lanes + half * kOut + d, x);
 #pragma unroll
-                for (int u = 0; u < 32; ++u) o[d + u] = fmaf(v[u], v_drop, o[d + u]);
+                for (int u = 0; u < 16; u += 2) o[(d + u) / 2] = fma2(pair(x[u], x[u + 1]), pair(v_drop, v_drop), o[(d + u) / 2]);
             }
             tc_fence_before();
             mbar_arrive(taken + wg * 8);
         }
+        sh.exchange[tiles & 1][wg][half][row] = l;
+        asm volatile("bar.sync %0, 256;" ::"r"(1 + wg) : "memory");
+        l += sh.exchange[tiles & 1][wg][half ^ 1][row];
         if (i < a.QP) {
             const bool live = i / a.QW < qe.x && i % a.QW < qe.y && l != 0.0f;
             const float inv = live ? (1 << (int)kLift) / l : 0.0f;
             float *out = a.out + (size_t)n * a.CB * a.QP * 32;
             const int first = h * a.D;
-            if ((a.D & 3) == 0) {
 #pragma unroll
-                for (int d = 0; d < DP; d += 4)
-                    if (d < a.D)
-                        *reinterpret_cast<float4 *>(out + at(first + d, i, a.QP)) =
-                            live ? make_float4(o[d] * inv, o[d + 1] * inv, o[d + 2] * inv, o[d + 3] * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
-            } else {
+            for (int d = 0; d < kOut; d += 4) {
+                const int ch = half * kOut + d;
+                float x[4];
+                unpair(o[d / 2], x[0], x[1]);
+                unpair(o[d / 2 + 1], x[2], x[3]);
 #pragma unroll
-                for (int d = 0; d < DP; ++d)
-                    if (d < a.D) out[at(first + d, i, a.QP)] = live ? o[d] * inv : 0.0f;
+                for (int u = 0; u < 4; ++u) x[u] = live ? x[u] * inv : 0.0f;
+                if ((a.D & 3) == 0) {
+                    if (ch < a.D) *reinterpret_cast<float4 *>(out + at(first + ch, i, a.QP)) = make_float4(x[0], x[1], x[2], x[3]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (ch + u < a.D) out[at(first + ch + u, i, a.QP)] = x[u];
+                }
             }
-            if (h == a.heads - 1)
+            if (h == a.heads - 1 && half == 0)
                 for (int ch = a.heads * a.D; ch < a.CB * 32; ++ch) out[at(ch, i, a.QP)] = 0.0f;
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (gave_up && warp == 8)                            // what is still on its way must land before the block ends
+    if (sh.gave_up && warp == loader)                    // what is still on its way must land before the block ends
         for (int x = max(0, issued - c.ring); x < issued; ++x) mbar_wait(full + x % c.ring * 8, (x / c.ring) & 1, c.limit);
-    if (warp == 9) tmem_dealloc(tmem, 512);
+    if (warp == issuer) tmem_dealloc(tmem, 512);
 }
 
 int padded(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : 128; }
@@ -495,7 +568,7 @@ int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
     launch_kernel(ctx, attention_tiles_kernel<DP>, dim3((unsigned)(2 * tiles), (unsigned)a.kv_heads, (unsigned)a.N), dim3(256), values, st, a, tiles);
     if (int s = check_launch(ctx)) return s;
     TcArgs c{a, tiles, 1, kMaxRing, 0, ctx->dev_status, ctx->wait_iters};
-    const size_t most = ctx->max_smem_optin - 4096, tile = (size_t)DP * 512;
+    const size_t most = ctx->max_smem_optin - 8192, tile = (size_t)DP * 512;
     if (DP < 128 && a.QP > kTile) c.q_tiles = 2;
     while (c.ring > 2 && 1024 + (c.q_tiles + c.ring) * tile > most) --c.ring;
     if (a.bias) {
@@ -511,7 +584,7 @@ int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
     const bool general = a.bias || a.cap > 0.0f;
     auto run = [&](auto *kern, std::atomic<unsigned long long> &d) {
         if (int s = allow_shared_memory(ctx, kern, d, most)) return s;
-        launch_kernel(ctx, kern, dim3((unsigned)ceil_div(a.QP, c.q_tiles * kTile), (unsigned)a.heads, (unsigned)a.N), dim3(kThreads), smem, st, c);
+        launch_kernel(ctx, kern, dim3((unsigned)ceil_div(a.QP, c.q_tiles * kTile), (unsigned)a.heads, (unsigned)a.N), dim3(c.q_tiles * 256 + 64), smem, st, c);
         return check_launch(ctx);
     };
     return x3 ? general ? run(attention_tc_kernel<DP, true, true>, done[0]) : run(attention_tc_kernel<DP, true, false>, done[1])
