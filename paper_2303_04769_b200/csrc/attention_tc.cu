@@ -10,14 +10,16 @@
 // bulk copies.  Every block of queries (QP / 256 a head, times the heads that share them) reads them so; converting in each
 // block instead would repeat it that many times beside the softmax, which is what bounds the main kernel.
 //
-// attention_tc_kernel: a block takes one or two tiles of 128 queries of a head.  One warp loads tiles, one issues MMAs, eight do the
-// softmax of each query tile.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128
-// columns); two threads share a row, half of its keys each, and write the weights as halves over the scores, where they are the second
-// product's A operand.  While one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
+// attention_tc_kernel: a block takes one or two tiles of 128 queries of a head.  One warp loads tiles, one issues MMAs, four (eight)
+// do the softmax of each query tile.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128
+// columns); a thread takes a row (two share it where the result has 128 channels) and writes the weights as halves over the scores, where
+// they are the second product's A operand.  While one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
 // added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
 // thousands of keys would add up (5e-8 a step), and no rescaling of tensor memory is needed when the maximum grows.
 #include <cuda_fp16.h>
+#include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "attention.cuh"
 #include "sm100.cuh"
@@ -64,18 +66,23 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c, int rows) {
     return (uint32_t)(c >> 6) * rows * 128 + r * 128 + ((((uint32_t)c >> 3 & 7) ^ (r & 7)) << 4);
 }
 
-// Eight consecutive channels from c on of a head's `D` at pixel p, 0 behind the last.
-__device__ __forceinline__ void load8(const float *x, int first, int c, int D, int p, int pixels, float (&v)[8]) {
-    if (((first | D) & 3) == 0) {
-#pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-            const float4 u = c + i < D ? *reinterpret_cast<const float4 *>(x + at(first + c + i, p, pixels)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            v[i] = u.x; v[i + 1] = u.y; v[i + 2] = u.z; v[i + 3] = u.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < D ? x[at(first + c + i, p, pixels)] : 0.0f;
-    }
+// Four consecutive channels from c on of a head's `D` at pixel p, 0 behind the last.  Eight lanes take a row's 128 bytes together.
+__device__ __forceinline__ float4 load4(const float *x, int first, int c, int D, int p, int pixels) {
+    if (((first | D) & 3) == 0) return c < D ? *reinterpret_cast<const float4 *>(x + at(first + c, p, pixels)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 v;
+    v.x = c + 0 < D ? x[at(first + c + 0, p, pixels)] : 0.0f; v.y = c + 1 < D ? x[at(first + c + 1, p, pixels)] : 0.0f;
+    v.z = c + 2 < D ? x[at(first + c + 2, p, pixels)] : 0.0f; v.w = c + 3 < D ? x[at(first + c + 3, p, pixels)] : 0.0f;
+    return v;
+}
+__device__ __forceinline__ float magnitude(float4 v) { return fmaxf(fmaxf(magnitude(v.x), magnitude(v.y)), fmaxf(magnitude(v.z), magnitude(v.w))); }
+// Their high and low parts to a tile of `DP` channels of high parts and as many of low ones.
+template <int DP>
+__device__ __forceinline__ void store4(char *tile, int r, int c, float4 v, float up) {
+    uint2 hi, lo;
+    split_finite(v.x * up, v.y * up, hi.x, lo.x);
+    split_finite(v.z * up, v.w * up, hi.y, lo.y);
+    *reinterpret_cast<uint2 *>(tile + chunk_at(r, c, kTile) + (c & 4) * 2) = hi;
+    *reinterpret_cast<uint2 *>(tile + chunk_at(r, DP + c, kTile) + (c & 4) * 2) = lo;
 }
 
 // Workspace: [N][kv_heads][tiles]{keys: DP * 512 bytes, values: DP * 512 bytes}; int[N][tiles][128], the keys' places in the bias table
@@ -88,7 +95,7 @@ __device__ __forceinline__ float *undo_scaling(const AttnArgs &a, int tiles, int
 }
 template <int DP>
 __global__ void __launch_bounds__(256) attention_tiles_kernel(const AttnArgs a, int tiles) {
-    constexpr int kBytes = DP * 512, kChunks = DP / 8;
+    constexpr int kBytes = DP * 512;
     __shared__ float most_s[8];
     extern __shared__ float values[];                    // [128][DP + 1]
     grid_dep_sync();
@@ -101,56 +108,58 @@ __global__ void __launch_bounds__(256) attention_tiles_kernel(const AttnArgs a, 
     const size_t tile = ((size_t)n * a.kv_heads + hk) * tiles + t;
     char *out = static_cast<char *>(a.ws) + tile * 2 * kBytes + (is_v ? kBytes : 0);
     const float *x = is_v ? a.v + n * a.v_stride : a.k + n * a.k_stride;
-    // a thread takes half of a key's channels, in chunks of eight
-    const int r = threadIdx.x >> 1, j = t * kTile + r, half = threadIdx.x & 1;
-    const int p = j < keys ? j / e.y * a.KW + j % e.y : -1;
-    constexpr int kMine = (kChunks + 1) / 2;
-    float v[kMine][8], most = 0.0f;
+    // eight lanes a key, four channels of every 32 each; a warp takes keys 16 w .. 16 w + 15
+    const int lane = threadIdx.x & 31, first = (threadIdx.x >> 5) * 16 + (lane >> 3), c0 = (lane & 7) * 4;
+    float4 v[4][DP / 32];
+    float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        if (p >= 0) load8(x, hk * a.D, (half * kMine + i) * 8, a.D, p, a.KP, v[i]);
+    for (int i = 0; i < 4; ++i) {
+        const int j = t * kTile + first + 4 * i, p = j < keys ? j / e.y * a.KW + j % e.y : -1;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (p < 0) v[i][u] = 0.0f;
-            most = fmaxf(most, magnitude(v[i][u]));
-        }
+        for (int k = 0; k < DP / 32; ++k) v[i][k] = p >= 0 ? load4(x, hk * a.D, k * 32 + c0, a.D, p, a.KP) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < DP / 32; ++k) most = fmaxf(most, magnitude(v[i][k]));
+#pragma unroll
     for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-    if ((threadIdx.x & 31) == 0) most_s[threadIdx.x >> 5] = most;
+    if (lane == 0) most_s[threadIdx.x >> 5] = most;
     if (is_v)
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) values[r * (DP + 1) + (half * kMine + i) * 8 + u] = v[i][u];
+            for (int k = 0; k < DP / 32; ++k) {
+                float *w = values + (first + 4 * i) * (DP + 1) + k * 32 + c0;
+                w[0] = v[i][k].x; w[1] = v[i][k].y; w[2] = v[i][k].z; w[3] = v[i][k].w;
+            }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 8; ++i) most = fmaxf(most, most_s[i]);
     const int ex = top_exponent(most);
     const float up = lift(ex);
     if (threadIdx.x == 0) undo_scaling(a, tiles, kBytes)[tile * 2 + is_v] = drop(ex);
-    if (!is_v && hk == 0 && half == 0) key_places(a, tiles, kBytes)[((size_t)n * tiles + t) * kTile + r] = p >= 0 ? of_key(a, j / e.y, j % e.y) : 0;
-    auto store = [&](const float (&w)[8], int row, int c_hi, int c_lo, int rows) {
-        uint4 hi, lo;
-        split_finite(w[0] * up, w[1] * up, hi.x, lo.x); split_finite(w[2] * up, w[3] * up, hi.y, lo.y);
-        split_finite(w[4] * up, w[5] * up, hi.z, lo.z); split_finite(w[6] * up, w[7] * up, hi.w, lo.w);
-        *reinterpret_cast<uint4 *>(out + chunk_at(row, c_hi, rows)) = hi;
-        *reinterpret_cast<uint4 *>(out + chunk_at(row, c_lo, rows)) = lo;
-    };
     if (!is_v) {
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int c = (half * kMine + i) * 8;
-            store(v[i], r, c, DP + c, kTile);
+        if (hk == 0 && threadIdx.x < kTile) {
+            const int j = t * kTile + threadIdx.x;
+            key_places(a, tiles, kBytes)[((size_t)n * tiles + t) * kTile + threadIdx.x] = j < keys ? of_key(a, j / e.y, j % e.y) : 0;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < DP / 32; ++k) store4<DP>(out, first + 4 * i, k * 32 + c0, v[i][k], up);
         return;
     }
-    for (int i = threadIdx.x; i < DP * 16; i += 256) {
-        const int d = i % DP, k0 = i / DP * 8;
+    for (int i = threadIdx.x; i < DP * 16; i += 256) {   // eight lanes a channel's 128 bytes
+        const int d = (i >> 3) % DP, k0 = (i & 7) * 8 + i / (8 * DP) * 64;
         float w[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) w[u] = values[(k0 + u) * (DP + 1) + d];
-        store(w, d, k0, kTile + k0, DP);
+        for (int u = 0; u < 8; ++u) w[u] = values[(k0 + u) * (DP + 1) + d] * up;
+        uint4 hi, lo;
+        split_finite(w[0], w[1], hi.x, lo.x); split_finite(w[2], w[3], hi.y, lo.y);
+        split_finite(w[4], w[5], hi.z, lo.z); split_finite(w[6], w[7], hi.w, lo.w);
+        *reinterpret_cast<uint4 *>(out + chunk_at(d, k0, DP)) = hi;
+        *reinterpret_cast<uint4 *>(out + chunk_at(d, kTile + k0, DP)) = lo;
     }
 }
 
@@ -190,11 +199,20 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // Two floats as one operand of the packed FP32 instructions.
-__device__ __forceinline__ uint64_t pair(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
-__device__ __forceinline__ void unpair(uint64_t p, float &a, float &b) { a = __uint_as_float((uint32_t)p); b = __uint_as_float((uint32_t)(p >> 32)); }
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
@@ -212,7 +230,30 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
         : "r"(taddr) : "memory");
 }
 
+// A load that is waited for later; the wait takes the values, so that nothing uses them in front of it.
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, float (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]),
+          "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]),
+          "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+          "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+        :: "memory");
+}
+
 constexpr int kMaxRing = 4;
+constexpr int kPlaces = 8;               // tiles: one is used no longer when the keys of the eighth behind it are asked for
+// Threads of a row: one has registers for 64 sums and for scores under way; the table's reads want twice as many warps to hide behind.
+template <int DP, bool kGeneral> constexpr int kRowThreads = DP == 128 || kGeneral ? 2 : 1;
+template <int DP, bool kGeneral> constexpr int kBlock = (DP == 128 ? 1 : 2) * kTile * kRowThreads<DP, kGeneral> + 64;
 
 struct TcArgs {
     AttnArgs a;
@@ -228,68 +269,111 @@ struct Shared {
     uint64_t full[kMaxRing], empty[kMaxRing];            // a slot has its tile; its last product is done
     uint64_t scores[3], weights[3];                      // a buffer has a tile's scores; 256 threads have written their weights
     uint64_t part[2], taken[2];                          // a query tile's product with the values is there; 256 threads have added it
+    uint64_t placed[kPlaces];                            // a tile's keys' places in the bias table are there
     uint64_t drained;                                    // after a wait that ran out: all MMAs are done
     uint32_t tmem;
     int gave_up;
     float exchange[2][2][2][kTile];                      // [parity of the key tile][query tile][half of the keys][row]: maxima; at last sums
     float q_drop[2][kTile];
+    alignas(16) int places[kPlaces][kTile];
 };
+
+// A table entry for exponentials of two; finite values stay finite, those below -2.3e38 are taken as equally low.
+__device__ __forceinline__ float powers_of_two(float b) {
+    const float r = b * kLog2e;
+    return fabsf(r) < INFINITY || !(fabsf(b) < INFINITY) ? r : copysignf(FLT_MAX, b);
+}
 
 // kGeneral: scores pass through the cap and the bias table.
 template <int DP, bool kX3, bool kGeneral>
-__global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(const TcArgs c) {
+__global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(const TcArgs c) {
     constexpr int kBytes = DP * 512;                     // of a tile of queries, keys or values
-    constexpr int kHalf = kTile / 2, kOut = DP / 2;      // a thread's keys of a tile, and its channels of the result
+    constexpr int kShare = kRowThreads<DP, kGeneral>;            // threads of a row
+    constexpr int kKeys = kTile / kShare, kOut = DP / kShare;            // a thread's keys of a tile, and its channels of the result
+    constexpr int kWarps = 4 * kShare;                   // softmax warps of a query tile
     extern __shared__ char raw[];
     __shared__ Shared sh;
     const AttnArgs &a = c.a;
     const int n = blockIdx.z, h = blockIdx.y, hk = h / (a.heads / a.kv_heads);
     const int i0 = blockIdx.x * c.q_tiles * kTile, nq = min(c.q_tiles, (a.QP - i0 + kTile - 1) / kTile);
-    const int warp = warp_index(), loader = c.q_tiles * 8, issuer = loader + 1;
+    const int warp = warp_index(), loader = c.q_tiles * kWarps, issuer = loader + 1;
     char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     char *queries = base, *slots = base + c.q_tiles * kBytes;
     float *table = reinterpret_cast<float *>(slots + c.ring * kBytes);
     if (warp == issuer) tmem_alloc(smem_u32(&sh.tmem), 512);
-    if (threadIdx.x == 0) {
-        sh.gave_up = 0;
-        for (int i = 0; i < kMaxRing; ++i) { mbar_init(smem_u32(&sh.full[i]), 1); mbar_init(smem_u32(&sh.empty[i]), 1); }
-        for (int i = 0; i < 3; ++i) { mbar_init(smem_u32(&sh.scores[i]), 1); mbar_init(smem_u32(&sh.weights[i]), 2 * kTile); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh.part[i]), 1); mbar_init(smem_u32(&sh.taken[i]), 2 * kTile); }
-        mbar_init(smem_u32(&sh.drained), 1);
-        mbar_fence_init();
-    }
+    const uint32_t full = smem_u32(sh.full), empty = smem_u32(sh.empty), scores = smem_u32(sh.scores), weights = smem_u32(sh.weights),
+                   part = smem_u32(sh.part), taken = smem_u32(sh.taken), placed = smem_u32(sh.placed);
     // What this kernel reads besides the tiles is older than the kernel in front of it, which has waited for all before itself.
     const int2 qe = extent(a.q_ext, n, a.QH, a.QW), ke = extent(a.k_ext, n, a.KH, a.KW);
     const int keys = ke.x * ke.y, tiles = (keys + kTile - 1) / kTile, steps = tiles * nq;
-    const int wg = warp >> 3, half = warp >> 2 & 1, row = threadIdx.x & (kTile - 1);         // of the softmax warps: query tile, half of the keys, row
+    const int wg = warp / kWarps, half = warp / 4 % kShare, row = threadIdx.x & (kTile - 1);         // of the softmax warps: query tile, share of the keys, row
     const int TW = a.QW + a.KW - 1;
     const float *bias = a.bias ? a.bias + (size_t)h * (a.QH + a.KH - 1) * TW : nullptr;
     int qoff = 0;
     const int i = i0 + wg * kTile + row;
-    if (wg < nq) {                                       // two neighbouring threads convert a row of the queries
-        const int r = threadIdx.x >> 1 & (kTile - 1), first = (threadIdx.x & 1) * kOut, p = i0 + wg * kTile + r;
-        char *mine = queries + wg * kBytes;
-        float v[kOut / 8][8], most = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kOut / 8; ++k) {
-            if (p < a.QP) load8(a.q + n * a.q_stride, h * a.D, first + k * 8, a.D, p, a.QP, v[k]);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (p >= a.QP) v[k][u] = 0.0f;
-                most = fmaxf(most, magnitude(v[k][u]));
+    // The tiles, keys before values; without the low parts: values' lie in the second half of their tile, keys' too but for 32 channels, whose
+    // rows hold both.
+    const uint32_t k_bytes = kX3 || DP == 32 ? kBytes : kBytes / 2, v_bytes = kX3 ? kBytes : kBytes / 2;
+    const char *from_tiles = static_cast<const char *>(a.ws) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2 * kBytes;
+    const int *from_places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kTile;
+    int issued = 0;                                      // by the loading warp
+    auto load = [&](int slot) {
+        if (elect_one()) {
+            const uint32_t bytes = issued & 1 ? v_bytes : k_bytes;
+            mbar_expect_tx(full + slot * 8, bytes);
+            bulk_load(smem_u32(slots + slot * kBytes), from_tiles + (size_t)issued * kBytes, bytes, full + slot * 8);
+            if (kGeneral && !(issued & 1)) {
+                const int t = issued >> 1, at = t % kPlaces;
+                mbar_expect_tx(placed + at * 8, kTile * sizeof(int));
+                bulk_load(smem_u32(sh.places[at]), from_places + t * kTile, kTile * sizeof(int), placed + at * 8);
             }
         }
-        most = fmaxf(most, __shfl_xor_sync(~0u, most, 1));
-        const int ex = top_exponent(most);
-        const float up = a.scale < 0.0f ? -lift(ex) : lift(ex);          // the scale's sign goes with the queries: what is left is >= 0
-        if (first == 0) sh.q_drop[wg][r] = fabsf(a.scale) * drop(ex);
+        __syncwarp();
+        ++issued;
+    };
+    if (warp == loader) {                                // on their way before the queries are converted
+        if (elect_one()) {
+            sh.gave_up = 0;
+            for (int i = 0; i < kMaxRing; ++i) { mbar_init(full + i * 8, 1); mbar_init(empty + i * 8, 1); }
+            for (int i = 0; i < 3; ++i) { mbar_init(scores + i * 8, 1); mbar_init(weights + i * 8, kShare * kTile); }
+            for (int i = 0; i < 2; ++i) { mbar_init(part + i * 8, 1); mbar_init(taken + i * 8, kShare * kTile); }
+            for (int i = 0; i < kPlaces; ++i) mbar_init(placed + i * 8, 1);
+            mbar_init(smem_u32(&sh.drained), 1);
+            mbar_fence_init();
+        }
+        __syncwarp();
+        grid_dep_sync();
+        grid_dep_trigger();
+        while (issued < min(2 * tiles, c.ring)) load(issued);
+    }
+    if (wg < nq) {                                       // eight lanes a row
+        char *mine = queries + wg * kBytes;
+        constexpr int kRows = kTile / kWarps / 4;        // of a lane
+        const int lane = threadIdx.x & 31, c0 = (lane & 7) * 4, r0 = (warp % kWarps) * (kTile / kWarps) + (lane >> 3);
+        const float *q = a.q + n * a.q_stride;
+#pragma unroll 1
+        for (int i4 = 0; i4 < kRows; i4 += 4) {
+            float4 v[4][DP / 32];
 #pragma unroll
-        for (int k = 0; k < kOut / 8; ++k) {
-            uint4 hi, lo;
-            split_finite(v[k][0] * up, v[k][1] * up, hi.x, lo.x); split_finite(v[k][2] * up, v[k][3] * up, hi.y, lo.y);
-            split_finite(v[k][4] * up, v[k][5] * up, hi.z, lo.z); split_finite(v[k][6] * up, v[k][7] * up, hi.w, lo.w);
-            *reinterpret_cast<uint4 *>(mine + chunk_at(r, first + k * 8, kTile)) = hi;
-            *reinterpret_cast<uint4 *>(mine + chunk_at(r, DP + first + k * 8, kTile)) = lo;
+            for (int k = 0; k < 4; ++k) {
+                const int p = i0 + wg * kTile + r0 + 4 * (i4 + k);
+#pragma unroll
+                for (int ch = 0; ch < DP / 32; ++ch) v[k][ch] = p < a.QP ? load4(q, h * a.D, ch * 32 + c0, a.D, p, a.QP) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = r0 + 4 * (i4 + k);
+                float most = 0.0f;
+#pragma unroll
+                for (int ch = 0; ch < DP / 32; ++ch) most = fmaxf(most, magnitude(v[k][ch]));
+#pragma unroll
+                for (int o = 1; o < 8; o *= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+                const int ex = top_exponent(most);
+                const float up = a.scale < 0.0f ? -lift(ex) : lift(ex);          // the scale's sign goes with the queries: what is left is >= 0
+                if (c0 == 0) sh.q_drop[wg][r] = fabsf(a.scale) * drop(ex);
+#pragma unroll
+                for (int ch = 0; ch < DP / 32; ++ch) store4<DP>(mine, r, ch * 32 + c0, v[k][ch], up);
+            }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -300,7 +384,7 @@ __global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(
             const int count = (y1 / a.QW - y0 + a.KH) * TW;
             const float *from = bias + (size_t)y0 * TW;
 #pragma unroll 8
-            for (int e = threadIdx.x; e < count; e += loader * 32) table[e] = from[e];
+            for (int e = threadIdx.x; e < count; e += loader * 32) table[e] = powers_of_two(from[e]);
             qoff -= y0 * TW;
         }
     }
@@ -309,62 +393,60 @@ __global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     volatile int *stop = &sh.gave_up;
-    const uint32_t full = smem_u32(sh.full), empty = smem_u32(sh.empty), scores = smem_u32(sh.scores), weights = smem_u32(sh.weights),
-                   part = smem_u32(sh.part), taken = smem_u32(sh.taken);
-    int issued = 0;                                      // tiles, by the loading warp
     auto s_at = [&](int buffer) { return tmem + buffer * kTile; };
     auto o_at = [&](int tile) { return tmem + 3 * kTile + tile * DP; };
 
     if (warp == loader) {
-        grid_dep_sync();                                 // the tiles
-        grid_dep_trigger();
-        const char *from = static_cast<const char *>(a.ws) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2 * kBytes;
-        // without the low parts: values' lie in the second half of their tile, keys' too but for 32 channels, whose rows hold both
-        const uint32_t k_bytes = kX3 || DP == 32 ? kBytes : kBytes / 2, v_bytes = kX3 ? kBytes : kBytes / 2;
-        for (int x = 0; x < 2 * tiles; ++x) {
-            const int slot = x % c.ring, use = x / c.ring;
-            if (use && !mbar_wait_uniform(empty + slot * 8, (use - 1) & 1, stop, c.status, c.limit)) break;
-            const uint32_t bytes = x & 1 ? v_bytes : k_bytes;
-            if (elect_one()) {
-                mbar_expect_tx(full + slot * 8, bytes);
-                bulk_load(smem_u32(slots + slot * kBytes), from + (size_t)x * kBytes, bytes, full + slot * 8);
-            }
-            __syncwarp();
-            ++issued;
+        for (int slot = 0, phase = 0; issued < 2 * tiles;) {
+            if (!mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit)) break;
+            load(slot);
+            if (++slot == c.ring) { slot = 0; phase ^= 1; }
         }
     } else if (warp == issuer) {
         const uint32_t q_lo = smem_desc_lo(smem_u32(queries)), slot_lo = smem_desc_lo(smem_u32(slots));
         auto column = [&](int col, int rows) { return (uint32_t)(((col >> 6) * rows * 128 + (col & 63) * 2) >> 4); };
+        // Step s + 2's scores go in front of step s's product, so that the softmax finds its next scores at hand - unless their keys
+        // have to wait for a slot that this product gives free: with one query tile step s + 2 is two key tiles on.
+        const bool early = nq == 2 || c.ring >= 4;
+        // Places in the rings, kept as they go: a division in front of an MMA is time the tensor cores wait.  Steps go by query tile first.
+        const int two = nq - 1;
+        struct Place {
+            int at, phase;
+            __device__ void on(int by, int of) { if ((at += by) >= of) { at -= of; phase ^= 1; } }
+        } k_slot{0, 0}, v_slot{1, 0}, to{0, 0}, from{0, 0};              // slots of keys and values, buffers of scores and of weights
         auto score = [&](int s) -> bool {                // queries x keys of step s
-            const int j = s % nq, t = s / nq, slot = 2 * t % c.ring, use = 2 * t / c.ring;
-            if (j == 0 && !mbar_wait_uniform(full + slot * 8, use & 1, stop, c.status, c.limit)) return false;
-            // the buffer's last weights, those of step s - 3, are used up (with one query tile `taken` has said so in front of step s - 2's product)
-            if (nq == 2 && s >= 3 && !mbar_wait_uniform(part + ((s - 3) & 1) * 8, ((s - 3) >> 1) & 1, stop, c.status, c.limit)) return false;
+            const int j = s & two;
+            if (j == 0 && !mbar_wait_uniform(full + k_slot.at * 8, k_slot.phase, stop, c.status, c.limit)) return false;
+            // the buffer's last weights, those of step s - 3, are used up (else `taken` has said so in front of step s - 2's product)
+            if (early && s >= 3 && !mbar_wait_uniform(part + ((s - 3) & two) * 8, (s - 3) >> two & 1, stop, c.status, c.limit)) return false;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t d = s_at(s % 3), qa = q_lo + j * (kBytes >> 4), kb = slot_lo + slot * (kBytes >> 4), desc = f16_desc(kTile);
+                const uint32_t d = s_at(to.at), qa = q_lo + j * (kBytes >> 4), kb = slot_lo + k_slot.at * (kBytes >> 4), desc = f16_desc(kTile);
 #pragma unroll
                 for (int term = kX3 ? 0 : 2; term < 3; ++term)           // small terms first
 #pragma unroll
                     for (int k = 0; k < DP; k += 16)
                         mma_f16(d, qa + column(k + (term == 0 ? DP : 0), kTile), kb + column(k + (term == 1 ? DP : 0), kTile), desc, k > 0 || term > (kX3 ? 0 : 2));
-                mma_commit(scores + s % 3 * 8);
-                if (j == nq - 1) mma_commit(empty + slot * 8);
+                mma_commit(scores + to.at * 8);
+                if (j == two) mma_commit(empty + k_slot.at * 8);
             }
             __syncwarp();
+            to.on(1, 3);
+            if (j == two) k_slot.on(2, c.ring);
             return true;
         };
         bool ok = true;
         for (int s = 0; s < min(2, steps) && ok; ++s) ok = score(s);
         for (int s = 0; s < steps && ok; ++s) {
-            const int j = s % nq, t = s / nq, x = 2 * t + 1, slot = x % c.ring, use = x / c.ring;
-            ok = mbar_wait_uniform(weights + s % 3 * 8, (s / 3) & 1, stop, c.status, c.limit);
+            const int j = s & two, t = s >> two;
+            if (early && s + 2 < steps && !(ok = score(s + 2))) break;
+            ok = mbar_wait_uniform(weights + from.at * 8, from.phase, stop, c.status, c.limit);
             if (ok && t > 0) ok = mbar_wait_uniform(taken + j * 8, (t - 1) & 1, stop, c.status, c.limit);
-            if (ok && j == 0) ok = mbar_wait_uniform(full + slot * 8, use & 1, stop, c.status, c.limit);
+            if (ok && j == 0) ok = mbar_wait_uniform(full + v_slot.at * 8, v_slot.phase, stop, c.status, c.limit);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint32_t d = o_at(j), pa = s_at(s % 3), vb = slot_lo + slot * (kBytes >> 4), desc = f16_desc(DP);
+                const uint32_t d = o_at(j), pa = s_at(from.at), vb = slot_lo + v_slot.at * (kBytes >> 4), desc = f16_desc(DP);
 #pragma unroll
                 for (int term = kX3 ? 0 : 2; term < 3; ++term)
 #pragma unroll
@@ -372,10 +454,12 @@ __global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(
                         mma_f16_tmem(d, pa + (k >> 5) * 32 + (k & 16) / 2 + (term == 0 ? 16 : 0), vb + column(k + (term == 1 ? kTile : 0), DP), desc,
                                      k > 0 || term > (kX3 ? 0 : 2));
                 mma_commit(part + j * 8);
-                if (j == nq - 1) mma_commit(empty + slot * 8);
+                if (j == two) mma_commit(empty + v_slot.at * 8);
             }
             __syncwarp();
-            if (s + 2 < steps) ok = score(s + 2);
+            from.on(1, 3);
+            if (j == two) v_slot.on(2, c.ring);
+            if (!early && s + 2 < steps) ok = score(s + 2);
         }
         if (!ok) {
             if (elect_one()) mma_commit(smem_u32(&sh.drained));
@@ -385,130 +469,18 @@ __global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(
     } else if (wg < nq) {
         grid_dep_sync();
         const float *undo = undo_scaling(a, c.tiles, kBytes) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2;
-        const int *places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kTile + half * kHalf;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;               // this warp's 32 lanes of tensor memory
-        const float q_drop = sh.q_drop[wg][row], over_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+        const float q_drop = sh.q_drop[wg][row], cap2 = a.cap * kLog2e, over_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
         const float *at_table = (c.table_floats ? table : bias) + qoff;
         uint64_t o[kOut / 2];
-        float l = 0.0f, m = kGeneral ? -INFINITY : INFINITY;             // m: the running maximum, or 14 - that in powers of two
+        float l = 0.0f, m = INFINITY;                    // m: 14 less the running maximum, in powers of two
+        float2 drops = tiles ? *reinterpret_cast<const float2 *>(undo) : make_float2(0.f, 0.f), next = drops;
+        int buffer = wg, phase = 0;
 #pragma unroll
         for (int d = 0; d < kOut / 2; ++d) o[d] = 0;
-        // A wait that runs out ends the waits behind it at once; the loop goes on, so that the barrier of these 256 threads is met.
-        for (int t = 0; t < tiles; ++t) {
-            const int s = t * nq + wg, buffer = s % 3, left = keys - t * kTile - half * kHalf;
-            const float k_drop = undo[2 * t], v_drop = undo[2 * t + 1] * (1.0f / (1 << (int)kLift));
-            mbar_wait_uniform(scores + buffer * 8, (s / 3) & 1, stop, c.status, c.limit);
-            tc_fence_after();
-            const uint32_t st = s_at(buffer) + lanes + half * kHalf;
-            const float f = q_drop * k_drop;
-            // scores of 32 keys as the softmax takes them; the largest of each in `top`
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, v[32];
-            auto take = [&](int g) {
-                tmem_ld32(st + g, v);
-                if (kGeneral) {
-                    if (a.cap > 0.0f)
-#pragma unroll
-                        for (int u = 0; u < 32; ++u) v[u] = capped(v[u] * f, a.cap, over_cap);
-                    else if (!bias)
-#pragma unroll
-                        for (int u = 0; u < 32; ++u) v[u] *= f;
-                    if (bias) {
-                        const float f1 = a.cap > 0.0f ? 1.0f : f;
-                        const int *place = places + t * kTile + g;
-#pragma unroll
-                        for (int u = 0; u < 32; u += 8) {
-                            const int4 k0 = *reinterpret_cast<const int4 *>(place + u), k1 = *reinterpret_cast<const int4 *>(place + u + 4);
-                            if (k1.w - k0.x == 7) {      // one row of the plane: neighbours in the table
-                                const float *b = at_table - k1.w;
-#pragma unroll
-                                for (int w = 0; w < 8; ++w) v[u + w] = fmaf(v[u + w], f1, b[7 - w]);
-                            } else {
-                                v[u] = fmaf(v[u], f1, at_table[-k0.x]); v[u + 1] = fmaf(v[u + 1], f1, at_table[-k0.y]);
-                                v[u + 2] = fmaf(v[u + 2], f1, at_table[-k0.z]); v[u + 3] = fmaf(v[u + 3], f1, at_table[-k0.w]);
-                                v[u + 4] = fmaf(v[u + 4], f1, at_table[-k1.x]); v[u + 5] = fmaf(v[u + 5], f1, at_table[-k1.y]);
-                                v[u + 6] = fmaf(v[u + 6], f1, at_table[-k1.z]); v[u + 7] = fmaf(v[u + 7], f1, at_table[-k1.w]);
-                            }
-                        }
-                    }
-                }
-                if (left < kHalf)
-#pragma unroll
-                    for (int u = 0; u < 32; ++u) v[u] = g + u < left ? v[u] : -INFINITY;
-#pragma unroll
-                for (int u = 0; u < 32; ++u) top[u & 3] = fmaxf(top[u & 3], v[u]);
-            };
-            take(0);
-            if (kGeneral) {                              // kept where the scores were until their turn comes
-                uint32_t w[32];
-#pragma unroll
-                for (int u = 0; u < 32; ++u) w[u] = __float_as_uint(v[u]);
-                tmem_st32(st, w);
-            }
-            take(32);
-            const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-            sh.exchange[t & 1][wg][half][row] = mine;
-            asm volatile("bar.sync %0, 256;" ::"r"(1 + wg) : "memory");
-            const float most = fmaxf(mine, sh.exchange[t & 1][wg][half ^ 1][row]);
-            // weights are exp2(v * scale2 + m) or exp2((v - from) * log2(e) + 14)
-            const float scale2 = f * kLog2e;
-            float from = 0.0f, shrink;
-            if (kGeneral) {
-                const float now = fmaxf(m, most);
-                from = now == -INFINITY ? 0.0f : now;    // nothing to weigh yet
-                shrink = exp2_fast((m - from) * kLog2e);
-                m = now;
-            } else {
-                const float now = fminf(m, fmaf(-most, scale2, kLift));
-                shrink = exp2_fast(now - m);
-                m = now;
-            }
-            uint64_t sum[2] = {0, 0};
-#pragma unroll
-            for (int g = 32; g >= 0; g -= 32) {          // the second half's scores are at hand
-                uint32_t hi[8], lo[8];
-                if (g == 0) {
-                    if (kGeneral) tmem_st_wait();
-                    tmem_ld32(st, v);
-                }
-#pragma unroll
-                for (int u = 0; u < 32; u += 2) {
-                    uint64_t x = pair(v[u], v[u + 1]);
-                    if (kGeneral) x = fma2(add2(x, pair(-from, -from)), pair(kLog2e, kLog2e), pair(kLift, kLift));
-                    else x = fma2(x, pair(scale2, scale2), pair(m, m));
-                    float x0, x1;
-                    unpair(x, x0, x1);
-                    x0 = exp2_fast(x0);
-                    x1 = exp2_fast(x1);
-                    if (!kGeneral && left < kHalf) {     // -inf * 0, where the scores have no scale
-                        x0 = g + u < left ? x0 : 0.0f;
-                        x1 = g + u + 1 < left ? x1 : 0.0f;
-                    }
-                    const uint64_t e = pair(x0, x1);
-                    sum[u >> 1 & 1] = add2(sum[u >> 1 & 1], e);
-                    if (kX3) {
-                        const uint64_t lead = e & 0xffffe000ffffe000ull;
-                        float r0, r1;
-                        unpair(add2(e, lead ^ 0x8000000080000000ull), r0, r1);
-                        hi[u / 2 & 7] = pack_halves(__uint_as_float((uint32_t)lead), __uint_as_float((uint32_t)(lead >> 32)));
-                        lo[u / 2 & 7] = pack_halves(r0, r1);
-                    } else {
-                        hi[u / 2 & 7] = pack_halves(x0, x1);
-                    }
-                    if ((u & 15) == 14) {                // 16 keys are 8 columns of high parts and 8 of low ones, 16 columns on
-                        tmem_st8(st + g + (u & 16) / 2, hi);
-                        if (kX3) tmem_st8(st + g + 16 + (u & 16) / 2, lo);
-                    }
-                }
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            mbar_arrive(weights + buffer * 8);
-            float s0, s1;
-            unpair(add2(sum[0], sum[1]), s0, s1);
-            l = fmaf(l, shrink, s0 + s1);
-            if (__any_sync(~0u, shrink != 1.0f))
-#pragma unroll
-                for (int d = 0; d < kOut / 2; ++d) o[d] = fma2(o[d], pair(shrink, shrink), 0);
+        // Adds a tile's product with the values: after the next tile's weights are on their way, when it has long been there.
+        auto take_part = [&](int t, float v_drop) {
+            v_drop *= 1.0f / (1 << (int)kLift);
             mbar_wait_uniform(part + wg * 8, t & 1, stop, c.status, c.limit);
             tc_fence_after();
 #pragma unroll
@@ -520,40 +492,207 @@ __global__ void __launch_bounds__(DP == 128 ? 320 : 576, 1) attention_tc_kernel(
             }
             tc_fence_before();
             mbar_arrive(taken + wg * 8);
+        };
+        // A wait that runs out ends the waits behind it at once; the loop goes on, so that the barrier of these 256 threads is met.
+        auto tile = [&](int t, auto last) {              // last: keys may be missing (code of its own: the tests cost as much as the rest)
+            constexpr bool kLast = decltype(last)::value;
+            const int left = keys - t * kTile - half * kKeys;
+            const float last_v = drops.y;
+            drops = next;
+            if (!kLast) next = *reinterpret_cast<const float2 *>(undo + 2 * t + 2);
+            if (kGeneral && bias) mbar_wait_uniform(placed + t % kPlaces * 8, t / kPlaces & 1, stop, c.status, c.limit);
+            mbar_wait_uniform(scores + buffer * 8, phase, stop, c.status, c.limit);
+            tc_fence_after();
+            const uint32_t st = s_at(buffer) + lanes + half * kKeys;
+            const float f = q_drop * drops.x, scale2 = f * kLog2e;
+            // The scores, in chunks of 32 keys: the last two stay in registers between the maximum and the exponentials.
+            constexpr int kChunks = kKeys / 32;
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, one[32], two[32];
+            auto take = [&](float (&v)[32], int g) {     // scores as the softmax takes them; the largest of each in `top`
+                if (kGeneral) {
+                    if (a.cap > 0.0f)
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) v[u] = capped(v[u], cap2, f * over_cap);
+                    if (bias) {
+                        const float f1 = a.cap > 0.0f ? 1.0f : scale2;
+                        const int *place = sh.places[t % kPlaces] + half * kKeys + g;
+                        if (c.table_floats) {
+#pragma unroll
+                            for (int u = 0; u < 32; u += 8) {
+                                const int4 k0 = *reinterpret_cast<const int4 *>(place + u), k1 = *reinterpret_cast<const int4 *>(place + u + 4);
+                                if (k1.w - k0.x == 7) {  // one row of the plane: neighbours in the table
+                                    const float *b = at_table - k1.w;
+#pragma unroll
+                                    for (int w = 0; w < 8; ++w) v[u + w] = fmaf(v[u + w], f1, b[7 - w]);
+                                } else {
+                                    v[u] = fmaf(v[u], f1, at_table[-k0.x]); v[u + 1] = fmaf(v[u + 1], f1, at_table[-k0.y]);
+                                    v[u + 2] = fmaf(v[u + 2], f1, at_table[-k0.z]); v[u + 3] = fmaf(v[u + 3], f1, at_table[-k0.w]);
+                                    v[u + 4] = fmaf(v[u + 4], f1, at_table[-k1.x]); v[u + 5] = fmaf(v[u + 5], f1, at_table[-k1.y]);
+                                    v[u + 6] = fmaf(v[u + 6], f1, at_table[-k1.z]); v[u + 7] = fmaf(v[u + 7], f1, at_table[-k1.w]);
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 32; ++u) v[u] = fmaf(v[u], f1, powers_of_two(at_table[-place[u]]));
+                        }
+                    }
+                }
+                if (kLast)
+#pragma unroll
+                    for (int u = 0; u < 32; ++u) v[u] = g + u < left ? v[u] : -INFINITY;
+#pragma unroll
+                for (int u = 0; u < 32; u += 2) top[u >> 1 & 3] = max3(top[u >> 1 & 3], v[u], v[u + 1]);
+            };
+            auto keep = [&](const float (&v)[32], int g) {           // where the scores were, until their turn comes
+                uint32_t w[32];
+#pragma unroll
+                for (int u = 0; u < 32; ++u) w[u] = __float_as_uint(v[u]);
+                tmem_st32(st + g, w);
+            };
+            tmem_ld32_async(st, one);
+            if (kChunks == 4) {
+                tmem_ld32_async(st + 32, two);
+                tmem_ld_wait(one);
+                take(one, 0);
+                tmem_ld32_async(st + 64, one);
+                tmem_ld_wait(two);
+                take(two, 32);
+                tmem_ld32_async(st + 96, two);
+                tmem_ld_wait(one);
+                take(one, 64);
+                tmem_ld_wait(two);
+                take(two, 96);
+            } else {
+                tmem_ld_wait(one);
+                take(one, 0);
+                if (kGeneral) keep(one, 0);
+                tmem_ld32_async(st + 32, two);
+                tmem_ld_wait(two);
+                take(two, 32);
+            }
+            const float mine = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            float most = mine;
+            if (kShare == 2) {
+                sh.exchange[t & 1][wg][half][row] = mine;
+                asm volatile("bar.sync %0, 256;" ::"r"(1 + wg) : "memory");
+                most = fmaxf(mine, sh.exchange[t & 1][wg][half ^ 1][row]);
+            }
+            // weights are exp2(v * scale2 + m), or exp2(v + m) where the scale is already in
+            const float now = fminf(m, kGeneral ? kLift - most : fmaf(-most, scale2, kLift)), add = kGeneral && now == INFINITY ? 0.0f : now;       // nothing to weigh yet
+            const float shrink = kGeneral && now == INFINITY ? 1.0f : exp2_fast(now - m);
+            m = now;
+            uint64_t sum[2] = {0, 0};
+            auto weigh = [&](float (&v)[32], int g) {
+                uint32_t hi[8], lo[8];
+#pragma unroll
+                for (int u = 0; u < 32; u += 2) {
+                    uint64_t x = pair(v[u], v[u + 1]);
+                    x = kGeneral ? add2(x, pair(add, add)) : fma2(x, pair(scale2, scale2), pair(add, add));
+                    float x0, x1;
+                    unpair(x, x0, x1);
+                    x0 = exp2_fast(x0);
+                    x1 = exp2_fast(x1);
+                    if (!kGeneral && kLast) {             // -inf * 0, where the scores have no scale
+                        x0 = g + u < left ? x0 : 0.0f;
+                        x1 = g + u + 1 < left ? x1 : 0.0f;
+                    }
+                    const uint64_t e = pair(x0, x1);
+                    sum[u >> 1 & 1] = add2(sum[u >> 1 & 1], e);
+                    if (kX3) {
+                        const float h0 = __uint_as_float(__float_as_uint(x0) & 0xffffe000u), h1 = __uint_as_float(__float_as_uint(x1) & 0xffffe000u);
+                        float r0, r1;
+                        unpair(fma2(pair(h0, h1), pair(-1.0f, -1.0f), e), r0, r1);
+                        hi[u / 2 & 7] = pack_halves(h0, h1);
+                        lo[u / 2 & 7] = pack_halves(r0, r1);
+                    } else {
+                        hi[u / 2 & 7] = pack_halves(x0, x1);
+                    }
+                    if ((u & 15) == 14) {                // 16 keys are 8 columns of high parts and 8 of low ones, 16 columns on
+                        tmem_st8(st + g + (u & 16) / 2, hi);
+                        if (kX3) tmem_st8(st + g + 16 + (u & 16) / 2, lo);
+                    }
+                }
+            };
+            if (kChunks == 4) {
+                weigh(one, 64);
+                tmem_ld32_async(st, one);
+                weigh(two, 96);
+                tmem_ld32_async(st + 32, two);
+                tmem_ld_wait(one);
+                weigh(one, 0);
+                tmem_ld_wait(two);
+                weigh(two, 32);
+            } else {
+                weigh(two, 32);
+                if (kGeneral) tmem_st_wait();
+                tmem_ld32_async(st, one);
+                tmem_ld_wait(one);
+                weigh(one, 0);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(weights + buffer * 8);
+            float s0, s1;
+            unpair(add2(sum[0], sum[1]), s0, s1);
+            l = fmaf(l, shrink, s0 + s1);
+            if (t) take_part(t - 1, last_v);
+            if ((buffer += nq) >= 3) { buffer -= 3; phase ^= 1; }
+            if (__any_sync(~0u, shrink != 1.0f))
+#pragma unroll
+                for (int d = 0; d < kOut / 2; ++d) o[d] = fma2(o[d], pair(shrink, shrink), 0);
+        };
+        for (int t = 0; t < tiles - 1; ++t) tile(t, std::false_type());
+        if (tiles) {
+            tile(tiles - 1, std::true_type());
+            take_part(tiles - 1, drops.y);
         }
-        sh.exchange[tiles & 1][wg][half][row] = l;
-        asm volatile("bar.sync %0, 256;" ::"r"(1 + wg) : "memory");
-        l += sh.exchange[tiles & 1][wg][half ^ 1][row];
-        if (i < a.QP) {
-            const bool live = i / a.QW < qe.x && i % a.QW < qe.y && l != 0.0f;
-            const float inv = live ? (1 << (int)kLift) / l : 0.0f;
-            float *out = a.out + (size_t)n * a.CB * a.QP * 32;
-            const int first = h * a.D;
+        if (kShare == 2) {
+            sh.exchange[tiles & 1][wg][half][row] = l;
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + wg) : "memory");
+            l += sh.exchange[tiles & 1][wg][half ^ 1][row];
+        }
+        // Rows of the result where the queries were (all products with them are done), and out from there, eight lanes a row.
+        const bool live = i < a.QP && i / a.QW < qe.x && i % a.QW < qe.y && l != 0.0f;
+        const float inv = live ? (1 << (int)kLift) / l : 0.0f;
+        float4 *rows = reinterpret_cast<float4 *>(queries + wg * kBytes);
 #pragma unroll
-            for (int d = 0; d < kOut; d += 4) {
-                const int ch = half * kOut + d;
-                float x[4];
-                unpair(o[d / 2], x[0], x[1]);
-                unpair(o[d / 2 + 1], x[2], x[3]);
+        for (int d = 0; d < kOut; d += 4) {
+            float4 x;
+            unpair(o[d / 2], x.x, x.y);
+            unpair(o[d / 2 + 1], x.z, x.w);
+            rows[row * (DP / 4) + ((half * kOut + d) / 4 ^ (row & 7))] =
+                live ? make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + wg), "n"(kWarps * 32) : "memory");
+        float *out = a.out + (size_t)n * a.CB * a.QP * 32;
+        const int lane = threadIdx.x & 31, c0 = (lane & 7) * 4, first = h * a.D;
+#pragma unroll 4
+        for (int r = (warp % kWarps) * 4 + (lane >> 3); r < kTile; r += kWarps * 4) {
+            const int p = i0 + wg * kTile + r;
+            if (p >= a.QP) break;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) x[u] = live ? x[u] * inv : 0.0f;
+            for (int ch = c0; ch < DP; ch += 32) {
+                const float4 x = rows[r * (DP / 4) + (ch / 4 ^ (r & 7))];
                 if ((a.D & 3) == 0) {
-                    if (ch < a.D) *reinterpret_cast<float4 *>(out + at(first + ch, i, a.QP)) = make_float4(x[0], x[1], x[2], x[3]);
+                    if (ch < a.D) *reinterpret_cast<float4 *>(out + at(first + ch, p, a.QP)) = x;
                 } else {
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (ch + u < a.D) out[at(first + ch + u, i, a.QP)] = x[u];
+                    if (ch + 0 < a.D) out[at(first + ch + 0, p, a.QP)] = x.x;
+                    if (ch + 1 < a.D) out[at(first + ch + 1, p, a.QP)] = x.y;
+                    if (ch + 2 < a.D) out[at(first + ch + 2, p, a.QP)] = x.z;
+                    if (ch + 3 < a.D) out[at(first + ch + 3, p, a.QP)] = x.w;
                 }
             }
-            if (h == a.heads - 1 && half == 0)
-                for (int ch = a.heads * a.D; ch < a.CB * 32; ++ch) out[at(ch, i, a.QP)] = 0.0f;
+            if (h == a.heads - 1)
+                for (int ch = a.heads * a.D + (lane & 7); ch < a.CB * 32; ch += 8) out[at(ch, p, a.QP)] = 0.0f;
         }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (sh.gave_up && warp == loader)                    // what is still on its way must land before the block ends
+    if (sh.gave_up && warp == loader) {                  // what is still on its way must land before the block ends
         for (int x = max(0, issued - c.ring); x < issued; ++x) mbar_wait(full + x % c.ring * 8, (x / c.ring) & 1, c.limit);
+        for (int t = max(0, (issued + 1) / 2 - kPlaces); kGeneral && t < (issued + 1) / 2; ++t) mbar_wait(placed + t % kPlaces * 8, t / kPlaces & 1, c.limit);
+    }
     if (warp == issuer) tmem_dealloc(tmem, 512);
 }
 
@@ -568,7 +707,7 @@ int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
     launch_kernel(ctx, attention_tiles_kernel<DP>, dim3((unsigned)(2 * tiles), (unsigned)a.kv_heads, (unsigned)a.N), dim3(256), values, st, a, tiles);
     if (int s = check_launch(ctx)) return s;
     TcArgs c{a, tiles, 1, kMaxRing, 0, ctx->dev_status, ctx->wait_iters};
-    const size_t most = ctx->max_smem_optin - 8192, tile = (size_t)DP * 512;
+    const size_t most = ctx->max_smem_optin - 12288, tile = (size_t)DP * 512;
     if (DP < 128 && a.QP > kTile) c.q_tiles = 2;
     while (c.ring > 2 && 1024 + (c.q_tiles + c.ring) * tile > most) --c.ring;
     if (a.bias) {
@@ -582,13 +721,14 @@ int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
     }
     const size_t smem = 1024 + (c.q_tiles + c.ring) * tile + sizeof(float) * c.table_floats;
     const bool general = a.bias || a.cap > 0.0f;
-    auto run = [&](auto *kern, std::atomic<unsigned long long> &d) {
+    auto run = [&](auto *kern, int row_threads, std::atomic<unsigned long long> &d) {
         if (int s = allow_shared_memory(ctx, kern, d, most)) return s;
-        launch_kernel(ctx, kern, dim3((unsigned)ceil_div(a.QP, c.q_tiles * kTile), (unsigned)a.heads, (unsigned)a.N), dim3(c.q_tiles * 256 + 64), smem, st, c);
+        launch_kernel(ctx, kern, dim3((unsigned)ceil_div(a.QP, c.q_tiles * kTile), (unsigned)a.heads, (unsigned)a.N), dim3(c.q_tiles * kTile * row_threads + 64), smem, st, c);
         return check_launch(ctx);
     };
-    return x3 ? general ? run(attention_tc_kernel<DP, true, true>, done[0]) : run(attention_tc_kernel<DP, true, false>, done[1])
-              : general ? run(attention_tc_kernel<DP, false, true>, done[2]) : run(attention_tc_kernel<DP, false, false>, done[3]);
+    constexpr int kG = kRowThreads<DP, true>, kP = kRowThreads<DP, false>;
+    return x3 ? general ? run(attention_tc_kernel<DP, true, true>, kG, done[0]) : run(attention_tc_kernel<DP, true, false>, kP, done[1])
+              : general ? run(attention_tc_kernel<DP, false, true>, kG, done[2]) : run(attention_tc_kernel<DP, false, false>, kP, done[3]);
 }
 
 }  // namespace
