@@ -3,9 +3,6 @@
 // attention_fp32_kernel: a block takes 64 queries of one head and walks the keys 64 at a time.  Scores, maxima and sums of a row stay
 // in the 16 lanes that share it; the exponentials cross shared memory once to become the second product's operand.  Bound by FP32
 // multiply-adds: 4 x 4 scores a thread, then 4 rows x D / 16 columns of the result.
-#include <cfloat>
-#include <cmath>
-
 #include "attention.cuh"
 
 namespace small {
@@ -191,5 +188,5 @@ SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, co
                      q_stride, k_stride, v_stride, scale, cap};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (on_tensor_cores(QP, flags)) return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
-    return launch_attention_fp32(ctx, a, st);
+    return QP <= kFewQueries ? launch_attention_few(ctx, a, st) : launch_attention_fp32(ctx, a, st);
 }

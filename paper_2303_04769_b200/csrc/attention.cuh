@@ -1,6 +1,9 @@
 // What the attention kernels share: the call's arguments, where a head's channels and an image's valid pixels lie.
 #pragma once
 
+#include <cfloat>
+#include <cmath>
+
 #include "entry.cuh"
 
 namespace small {
@@ -29,6 +32,28 @@ __device__ __forceinline__ size_t at(int c, int p, int pixels) { return ((size_t
 __device__ __forceinline__ int of_query(const AttnArgs &a, int i) { return (i / a.QW + a.KH - 1) * (a.QW + a.KW - 1) + i % a.QW + a.KW - 1; }
 __device__ __forceinline__ int of_key(const AttnArgs &a, int y, int x) { return y * (a.QW + a.KW - 1) + x; }
 
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A table entry for exponentials of two; finite values stay finite, those below -2.3e38 are taken as equally low.
+__device__ __forceinline__ float powers_of_two(float b) {
+    const float r = b * kLog2e;
+    return fabsf(r) < INFINITY || !(fabsf(b) < INFINITY) ? r : copysignf(FLT_MAX, b);
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// Four consecutive channels from c on of a head's `D` at pixel p, 0 behind the last.  Eight lanes take a row's 128 bytes together.
+__device__ __forceinline__ float4 load4(const float *x, int first, int c, int D, int p, int pixels) {
+    if (((first | D) & 3) == 0) return c < D ? *reinterpret_cast<const float4 *>(x + at(first + c, p, pixels)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 v;
+    v.x = c + 0 < D ? x[at(first + c + 0, p, pixels)] : 0.0f; v.y = c + 1 < D ? x[at(first + c + 1, p, pixels)] : 0.0f;
+    v.z = c + 2 < D ? x[at(first + c + 2, p, pixels)] : 0.0f; v.w = c + 3 < D ? x[at(first + c + 3, p, pixels)] : 0.0f;
+    return v;
+}
+
 // cap * tanh(x / cap).  Below 1/2 by Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + x^2 / (7 + x^2 / 9)))), whose
 // relative error there is some x^10 / 1e7, 1e-10; above as (e - 1) / (e + 1), e = exp(2 x), where neither is a small difference.
 __device__ __forceinline__ float capped(float x, float cap, float over_cap) {
@@ -41,6 +66,9 @@ __device__ __forceinline__ float capped(float x, float cap, float over_cap) {
 
 // attention.cu
 int launch_attention_fp32(small_ctx *, const AttnArgs &, cudaStream_t);
+// attention_few.cu: few queries; a row is a query of a head that shares its keys
+constexpr int kFewQueries = 16;
+int launch_attention_few(small_ctx *, const AttnArgs &, cudaStream_t);
 // attention_tc.cu: the tensor-core form, and the workspace it takes
 size_t attention_tc_workspace(int N, int kv_heads, int D, int KP);
 int launch_attention_tc(small_ctx *, const AttnArgs &, bool x3, cudaStream_t);

@@ -17,8 +17,6 @@
 // added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
 // thousands of keys would add up (5e-8 a step), and no rescaling of tensor memory is needed when the maximum grows.
 #include <cuda_fp16.h>
-#include <cfloat>
-#include <cmath>
 #include <type_traits>
 
 #include "attention.cuh"
@@ -29,7 +27,6 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;               // queries and keys of a tile
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLift = 14.0f;           // weights are scaled by 2^14
 
 // The exponent that brings |x| <= most to below 2^15: x * lift(e) and back by drop(e).
@@ -66,14 +63,6 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c, int rows) {
     return (uint32_t)(c >> 6) * rows * 128 + r * 128 + ((((uint32_t)c >> 3 & 7) ^ (r & 7)) << 4);
 }
 
-// Four consecutive channels from c on of a head's `D` at pixel p, 0 behind the last.  Eight lanes take a row's 128 bytes together.
-__device__ __forceinline__ float4 load4(const float *x, int first, int c, int D, int p, int pixels) {
-    if (((first | D) & 3) == 0) return c < D ? *reinterpret_cast<const float4 *>(x + at(first + c, p, pixels)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    float4 v;
-    v.x = c + 0 < D ? x[at(first + c + 0, p, pixels)] : 0.0f; v.y = c + 1 < D ? x[at(first + c + 1, p, pixels)] : 0.0f;
-    v.z = c + 2 < D ? x[at(first + c + 2, p, pixels)] : 0.0f; v.w = c + 3 < D ? x[at(first + c + 3, p, pixels)] : 0.0f;
-    return v;
-}
 __device__ __forceinline__ float magnitude(float4 v) { return fmaxf(fmaxf(magnitude(v.x), magnitude(v.y)), fmaxf(magnitude(v.z), magnitude(v.w))); }
 // Their high and low parts to a tile of `DP` channels of high parts and as many of low ones.
 template <int DP>
@@ -192,12 +181,6 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
 // Two floats as one operand of the packed FP32 instructions.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
     uint64_t r;
@@ -277,12 +260,6 @@ struct Shared {
     float q_drop[2][kTile];
     alignas(16) int places[kPlaces][kTile];
 };
-
-// A table entry for exponentials of two; finite values stay finite, those below -2.3e38 are taken as equally low.
-__device__ __forceinline__ float powers_of_two(float b) {
-    const float r = b * kLog2e;
-    return fabsf(r) < INFINITY || !(fabsf(b) < INFINITY) ? r : copysignf(FLT_MAX, b);
-}
 
 // kGeneral: scores pass through the cap and the bias table.
 template <int DP, bool kX3, bool kGeneral>
