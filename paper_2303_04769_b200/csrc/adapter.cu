@@ -1,30 +1,18 @@
-// 1 x 1 convolution with a low-rank adapter for each image: out = act(W x + b + s_a Up_a (Down_a x)).
-// The shared product is small_conv2d; the adapters' part is added to its result by the kernels here.
-//
-// Packed adapters: Down as [adapters][CB][RP][32 channels], RP = R rounded up to 8 (rows of one channel block together, as
-// activations are), behind them Up as [adapters][RB][KB * 32 filters][32 ranks]; whatever is behind R, C or K is 0.
-#include "entry.cuh"
+// 1 x 1 convolution with a low-rank adapter for each image, out = act(W x + b + s_a Up_a (Down_a x)): entry points, and the form for few
+// pixels and for FP32 arithmetic - small_conv2d for the shared product, and two kernels for what the adapters add to it.
+#include "adapter.cuh"
 
 namespace small {
 namespace {
 
-constexpr int kMaxRank = 128;
-
-struct AdapterShape {
-    int C, K, R, CB, KB, RP, RB;
-    size_t down, up;                     // floats of one adapter's Down and Up
-    AdapterShape(int C, int K, int R) : C(C), K(K), R(R), CB(blocks_of(C)), KB(blocks_of(K)), RP((R + 7) / 8 * 8), RB(blocks_of(R)) {
-        down = (size_t)CB * RP * 32;
-        up = (size_t)RB * KB * 32 * 32;
-    }
-};
+constexpr int kMaxRank = 128, kThreads = 256;
 
 bool adapter_shape_ok(int adapters, int C, int K, int R) {
-    return adapters >= 1 && C >= 1 && K >= 1 && R >= 1 && R <= kMaxRank && C <= (1 << 20) && K <= (1 << 20);
+    return adapters >= 1 && C >= 1 && K >= 1 && R >= 1 && R <= kMaxRank && C <= (1 << 20) && K <= (1 << 20) && adapters <= (1 << 20);
 }
 
-__global__ void __launch_bounds__(256) pack_adapters_kernel(const float *__restrict__ down, const float *__restrict__ up, float *__restrict__ packed,
-                                                            int adapters, const AdapterShape s) {
+__global__ void __launch_bounds__(kThreads) pack_adapters_kernel(const float *__restrict__ down, const float *__restrict__ up, float *__restrict__ packed,
+                                                                 int adapters, const AdapterShape s) {
     grid_dep_sync();
     grid_dep_trigger();
     const size_t stride = (size_t)gridDim.x * blockDim.x, first = blockIdx.x * (size_t)blockDim.x + threadIdx.x;
@@ -34,65 +22,108 @@ __global__ void __launch_bounds__(256) pack_adapters_kernel(const float *__restr
         packed[i] = c < s.C && r < s.R ? down[(a * s.R + r) * s.C + c] : 0.0f;
     }
     for (size_t i = first; i < s.up * adapters; i += stride) {
-        const size_t a = i / s.up, e = i % s.up, rows = (size_t)s.KB * 32;
-        const int r = (int)(e / (rows * 32)) * 32 + (int)(e & 31), k = (int)(e / 32 % rows);
+        const size_t a = i / s.up, e = i % s.up;
+        const int k = (int)(e / (s.RP * 32)) * 32 + (int)(e & 31), r = (int)(e / 32 % s.RP);
         packed[s.down * adapters + i] = k < s.K && r < s.R ? up[(a * s.K + k) * s.R + r] : 0.0f;
     }
 }
 
-struct AdaptArgs {
-    const float *in, *packed, *scale;
-    const int32_t *adapter;
-    float *t, *out;                      // t: [N][pixels][RP], the products with Down
-    int N, HW, adapters;
-    bool relu;
-};
+__device__ __forceinline__ bool adapter_of(const AdaptArgs &a, int n, int &id) {
+    id = a.adapter[n];
+    return id >= 0 && id < a.adapters;
+}
 
-// t = scale Down x, a thread for each pixel and row.
-__global__ void __launch_bounds__(256) adapter_down_kernel(const AdaptArgs a, const AdapterShape s) {
+// t[n][pixel][rank] = scale Down x.  A warp takes kPixels pixels of an image and eight ranks, a lane a channel of each block: every load is a
+// whole line, and each serves kPixels or eight products.  The sums are dealt out over the lanes while they are added up.
+template <int kPixels>
+__global__ void __launch_bounds__(kThreads) adapter_down_kernel(const AdaptArgs a, const AdapterShape s) {
     grid_dep_sync();
     grid_dep_trigger();
-    const size_t total = (size_t)a.N * a.HW * s.RP, stride = (size_t)gridDim.x * blockDim.x;
-    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < total; i += stride) {
-        const int r = (int)(i % s.RP);
-        const size_t np = i / s.RP;
-        const int p = (int)(np % a.HW), n = (int)(np / a.HW), id = a.adapter[n];
-        if (id < 0 || id >= a.adapters) continue;
-        const float4 *x = reinterpret_cast<const float4 *>(a.in) + ((size_t)n * s.CB * a.HW + p) * 8;
-        const float4 *w = reinterpret_cast<const float4 *>(a.packed + id * s.down) + r * 8;
-        float acc = 0.0f;
-        for (int cb = 0; cb < s.CB; ++cb, x += (size_t)a.HW * 8, w += s.RP * 8)
+    const int lane = threadIdx.x & 31, rows = s.RP / 8, runs = (a.HW + kPixels - 1) / kPixels;
+    const long long tasks = (long long)a.N * runs * rows, stride = (long long)gridDim.x * (kThreads / 32);
+    for (long long i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i < tasks; i += stride) {
+        const int rg = (int)(i % rows), p0 = (int)(i / rows % runs) * kPixels, n = (int)(i / rows / runs);
+        int id;
+        if (!adapter_of(a, n, id)) continue;
+        const float *x = a.in + (size_t)n * s.CB * a.HW * 32 + lane, *w = a.packed + id * s.down + rg * 256 + lane;
+        float acc[kPixels * 8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float4 u = x[j], v = w[j];
-                acc = fmaf(u.x, v.x, fmaf(u.y, v.y, fmaf(u.z, v.z, fmaf(u.w, v.w, acc))));
+        for (int u = 0; u < kPixels * 8; ++u) acc[u] = 0.0f;
+#pragma unroll 4
+        for (int cb = 0; cb < s.CB; ++cb) {
+            float v[kPixels];
+#pragma unroll
+            for (int q = 0; q < kPixels; ++q) v[q] = p0 + q < a.HW && cb * 32 + lane < s.C ? x[((size_t)cb * a.HW + p0 + q) * 32] : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const float u = w[(cb * s.RP + r) * 32];
+#pragma unroll
+                for (int q = 0; q < kPixels; ++q) acc[q * 8 + r] = fmaf(v[q], u, acc[q * 8 + r]);
             }
-        a.t[i] = a.scale ? a.scale[id] * acc : acc;
+        }
+        // halves of the sums go to halves of the lanes, until a lane has kPixels / 4 of them left (or several lanes the same one)
+        int have = kPixels * 8;
+#pragma unroll
+        for (int bit = 16; bit; bit /= 2) {
+            const bool upper = lane & bit;
+            if (have > 1) {
+#pragma unroll
+                for (int u = 0; u < kPixels * 4; ++u)
+                    if (u < have / 2) {
+                        const float give = upper ? acc[u] : acc[u + have / 2], keep = upper ? acc[u + have / 2] : acc[u];
+                        acc[u] = keep + __shfl_xor_sync(~0u, give, bit);
+                    }
+                have /= 2;
+            } else {
+                acc[0] += __shfl_xor_sync(~0u, acc[0], bit);
+            }
+        }
+        const float factor = a.scale ? a.scale[id] : 1.0f;
+        const int e = kPixels == 4 ? lane : lane >> 2, p = p0 + e / 8;               // one pixel: four lanes have each rank's sum
+        if ((kPixels == 4 || (lane & 3) == 0) && p < a.HW) static_cast<float *>(a.ws)[((size_t)n * a.HW + p) * s.RP + rg * 8 + e % 8] = factor * acc[0];
     }
 }
 
-// out = act(out + Up t), a thread for each pixel and filter.
-__global__ void __launch_bounds__(256) adapter_up_kernel(const AdaptArgs a, const AdapterShape s) {
+// out = act(out + Up t).  A warp takes kPixels pixels and a block of filters, a lane a filter.
+template <int kPixels>
+__global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdaptArgs a, const AdapterShape s) {
     grid_dep_sync();
     grid_dep_trigger();
-    const size_t total = (size_t)a.N * s.KB * a.HW * 32, stride = (size_t)gridDim.x * blockDim.x;
-    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < total; i += stride) {
-        const size_t line = i >> 5;
-        const int p = (int)(line % a.HW), kb = (int)(line / a.HW % s.KB), n = (int)(line / a.HW / s.KB), id = a.adapter[n];
-        const int k = kb * 32 + (int)(i & 31);
-        const bool some = id >= 0 && id < a.adapters;
-        if (k >= s.K || (!some && !a.relu)) continue;
-        float v = a.out[i];
+    const int lane = threadIdx.x & 31, runs = (a.HW + kPixels - 1) / kPixels;
+    const long long tasks = (long long)a.N * s.KB * runs, stride = (long long)gridDim.x * (kThreads / 32);
+    for (long long i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i < tasks; i += stride) {
+        const int p0 = (int)(i % runs) * kPixels, kb = (int)(i / runs % s.KB), n = (int)(i / runs / s.KB);
+        int id;
+        const bool some = adapter_of(a, n, id);
+        if (!some && !a.relu) continue;
+        float *out = a.out + (((size_t)n * s.KB + kb) * a.HW + p0) * 32 + lane;
+        float acc[kPixels];
+#pragma unroll
+        for (int q = 0; q < kPixels; ++q) acc[q] = p0 + q < a.HW ? out[q * 32] : 0.0f;
         if (some) {
-            const float *t = a.t + ((size_t)n * a.HW + p) * s.RP;
-            const float *w = a.packed + s.down * a.adapters + id * s.up + (size_t)k * 32;
-            for (int r = 0; r < s.R; ++r) v = fmaf(t[r], w[(size_t)(r >> 5) * s.KB * 1024 + (r & 31)], v);
+            const float *w = a.packed + s.down * a.adapters + id * s.up + (size_t)kb * s.RP * 32 + lane;
+            const float4 *t = reinterpret_cast<const float4 *>(static_cast<const float *>(a.ws) + ((size_t)n * a.HW + p0) * s.RP);
+#pragma unroll 2
+            for (int r = 0; r < s.RP; r += 4) {
+                const float w0 = w[r * 32], w1 = w[r * 32 + 32], w2 = w[r * 32 + 64], w3 = w[r * 32 + 96];
+#pragma unroll
+                for (int q = 0; q < kPixels; ++q) {
+                    const float4 v = p0 + q < a.HW ? t[(q * s.RP + r) / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    acc[q] = fmaf(v.x, w0, fmaf(v.y, w1, fmaf(v.z, w2, fmaf(v.w, w3, acc[q]))));
+                }
+            }
         }
-        a.out[i] = a.relu && !(v > 0.0f) ? 0.0f : v;
+        if (kb * 32 + lane >= s.K) continue;             // pad lanes stay what the convolution has written
+#pragma unroll
+        for (int q = 0; q < kPixels; ++q)
+            if (p0 + q < a.HW) out[q * 32] = a.relu && !(acc[q] > 0.0f) ? 0.0f : acc[q];
     }
 }
 
-unsigned stream_blocks(size_t items) { return (unsigned)(items / 256 + 1 < 148 * 16 ? items / 256 + 1 : 148 * 16); }
+unsigned task_blocks(const small_ctx *ctx, long long tasks) {
+    const long long blocks = (tasks + kThreads / 32 - 1) / (kThreads / 32), most = (long long)ctx->sm_count * 16;
+    return (unsigned)(blocks < most ? blocks : most);
+}
 
 }  // namespace
 }  // namespace small
@@ -100,9 +131,7 @@ unsigned stream_blocks(size_t items) { return (unsigned)(items / 256 + 1 < 148 *
 using namespace small;
 
 SMALL_API size_t small_adapter_elems(int adapters, int C, int K, int R) {
-    if (!adapter_shape_ok(adapters, C, K, R)) return 0;
-    const AdapterShape s(C, K, R);
-    return (s.down + s.up) * adapters;
+    return adapter_shape_ok(adapters, C, K, R) ? AdapterShape(adapters, C, K, R).floats : 0;
 }
 
 SMALL_API int small_pack_adapters(small_ctx *ctx, const float *down, const float *up, float *packed, int adapters, int C, int K, int R, void *stream) {
@@ -115,14 +144,18 @@ SMALL_API int small_pack_adapters(small_ctx *ctx, const float *down, const float
         return SMALL_ERR_OVERLAP;
     const OnDevice on(ctx);
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
-    launch_kernel(ctx, pack_adapters_kernel, dim3(stream_blocks(bytes / 4)), dim3(256), 0, static_cast<cudaStream_t>(stream), down, up, packed, adapters,
-                  AdapterShape(C, K, R));
-    return check_launch(ctx);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const AdapterShape s(adapters, C, K, R);
+    launch_kernel(ctx, pack_adapters_kernel, dim3(task_blocks(ctx, (long long)((s.down + s.up) * adapters / 32))), dim3(kThreads), 0, st, down, up, packed, adapters, s);
+    if (int e = check_launch(ctx)) return e;
+    return launch_pack_up_halves(ctx, up, packed, adapters, s, st);
 }
 
 SMALL_API size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R) {
     if (N < 1 || H < 1 || W < 1 || (long long)H * W > (1ll << 24) || !adapter_shape_ok(1, C, K, R)) return 0;
-    return sizeof(float) * (size_t)N * H * W * AdapterShape(C, K, R).RP;
+    const size_t products = sizeof(float) * (size_t)N * H * W * AdapterShape(1, C, K, R).RP;
+    const size_t whole = adapted_tc_preferred(N, C, K, H * W, R, kSmCount) ? adapted_tc_workspace(N, C, K, H * W, R) : 0;
+    return whole > products ? whole : products;
 }
 
 SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,
@@ -137,9 +170,10 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     if (int s = make_geom(g, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0)) return s;
     const size_t ws = small_adapted_conv2d_workspace_bytes(N, C, K, H, W, R);
     if (!workspace) return SMALL_ERR_WORKSPACE;
+    const unsigned math = flags & SMALL_MATH_MASK;
     const size_t in_b = sizeof(float) * packed_elems(N, C, H, W), out_b = sizeof(float) * packed_elems(N, K, H, W);
     const struct { const void *p; size_t n; } read[] = {
-        {in, in_b}, {w_blk, sizeof(float) * small_conv_weight_elems(C, K, 1, 1, flags & SMALL_MATH_MASK)}, {bias, sizeof(float) * K},
+        {in, in_b}, {w_blk, sizeof(float) * small_conv_weight_elems(C, K, 1, 1, math)}, {bias, sizeof(float) * K},
         {packed, sizeof(float) * small_adapter_elems(adapters, C, K, R)}, {adapter, sizeof(int32_t) * N}, {scale, sizeof(float) * adapters}};
     for (const auto &r : read)
         if (r.p && (ranges_overlap(r.p, r.n, out, out_b) || ranges_overlap(r.p, r.n, workspace, ws))) return SMALL_ERR_OVERLAP;
@@ -147,11 +181,17 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     const OnDevice on(ctx);
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (int s = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return s;
-    const AdapterShape s(C, K, R);
-    const AdaptArgs a{in, packed, scale, adapter, static_cast<float *>(workspace), out, N, H * W, adapters, (flags & SMALL_RELU) != 0};
-    launch_kernel(ctx, adapter_down_kernel, dim3(stream_blocks((size_t)N * H * W * s.RP)), dim3(256), 0, st, a, s);
+    const AdapterShape s(adapters, C, K, R);
+    const AdaptArgs a{in, w_blk, bias, packed, scale, adapter, out, workspace, N, H * W, adapters, (flags & SMALL_RELU) != 0, (flags & SMALL_ACCUMULATE) != 0};
+    if (math != SMALL_MATH_FP32 && (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && adapted_tc_preferred(N, C, K, H * W, R, kSmCount))
+        return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
+    if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
+    const bool runs = H * W >= 4;                        // several pixels a warp where an image has them
+    const long long rows = (long long)N * (s.RP / 8), blocks = (long long)N * s.KB;
+    if (runs) launch_kernel(ctx, adapter_down_kernel<4>, dim3(task_blocks(ctx, rows * ceil_div(H * W, 4))), dim3(kThreads), 0, st, a, s);
+    else launch_kernel(ctx, adapter_down_kernel<1>, dim3(task_blocks(ctx, rows * H * W)), dim3(kThreads), 0, st, a, s);
     if (int e = check_launch(ctx)) return e;
-    launch_kernel(ctx, adapter_up_kernel, dim3(stream_blocks((size_t)N * H * W * s.KB * 32)), dim3(256), 0, st, a, s);
+    if (runs) launch_kernel(ctx, adapter_up_kernel<8>, dim3(task_blocks(ctx, blocks * ceil_div(H * W, 8))), dim3(kThreads), 0, st, a, s);
+    else launch_kernel(ctx, adapter_up_kernel<1>, dim3(task_blocks(ctx, blocks * H * W)), dim3(kThreads), 0, st, a, s);
     return check_launch(ctx);
 }

@@ -1,0 +1,44 @@
+// What the kernels of adapted 1 x 1 convolutions share: sizes of the packed adapters and the call's arguments.
+#pragma once
+
+#include "entry.cuh"
+
+namespace small {
+
+// Packed adapters (small_pack_adapters), whatever is behind R, C or K being 0:
+//   Down   float[adapters][CB][RP][32 channels]            RP = R rounded up to 8: rows of a channel block together, as activations are
+//   Up     float[adapters][KB][RP][32 filters]
+//   Up     [adapters][filter tiles][RB]{filters of the tile: 128 bytes, 32 high halves and 32 low ones of 32 ranks, swizzled}
+//   int    [adapters], the exponent that those were scaled by
+// Filter tiles have eight channel blocks, the last one what is left.
+struct AdapterShape {
+    int C, K, R, CB, KB, RP, RB;
+    size_t down, up, up_halves;          // floats of one adapter
+    size_t halves_at, exponents_at, floats;
+    AdapterShape(int adapters, int C, int K, int R) : C(C), K(K), R(R), CB(blocks_of(C)), KB(blocks_of(K)), RP((R + 7) / 8 * 8), RB(blocks_of(R)) {
+        down = (size_t)CB * RP * 32;
+        up = (size_t)KB * RP * 32;
+        up_halves = (size_t)RB * KB * 32 * 32;
+        halves_at = (down + up) * adapters;
+        exponents_at = halves_at + up_halves * adapters;
+        floats = exponents_at + (adapters + 3) / 4 * 4;
+    }
+};
+constexpr int kFilterTile = 8;           // channel blocks of filters
+
+struct AdaptArgs {
+    const float *in, *w, *bias, *packed, *scale;
+    const int32_t *adapter;
+    float *out;
+    void *ws;
+    int N, HW, adapters;
+    bool relu, accumulate;
+};
+
+// adapter_tc.cu: the whole layer on the tensor cores, whether it pays, its workspace, and Up as its operand
+bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms);
+size_t adapted_tc_workspace(int N, int C, int K, int HW, int R);
+int launch_adapted_tc(small_ctx *, const AdaptArgs &, const AdapterShape &, bool x3, cudaStream_t);
+int launch_pack_up_halves(small_ctx *, const float *up, float *packed, int adapters, const AdapterShape &, cudaStream_t);
+
+}  // namespace small

@@ -1,0 +1,404 @@
+// 1 x 1 convolution with an adapter for each image as one product on the tensor cores (tcgen05, kind::f16): the products t = Down_a x stand
+// behind an image's channels, and s_a Up_a behind the filters, so that the adapter costs some more steps of the reduction and the result is
+// written once.  Operands are pairs of halves (halves.cuh).
+//
+// adapter_filters_kernel: the filters as halves, 64 channels a chunk, one exponent for the layer (a cluster finds it).
+// adapter_pixels_kernel: 128 pixels of an image a block: t in FP32 and the largest value in one pass over them (from memory), halves in a second
+//   (from L2).  t shares the pixels' accumulator, so its exponent follows from theirs, the filters' and the adapter's; where that would pass
+//   half precision's range the pixels take a smaller scale, which loses nothing: the sum is the adapter's part then.
+// adapter_product_kernel: a block walks tiles of 128 pixels x 256 filters; warps for loading (plain bulk copies, two stages of 96 KB), MMAs
+//   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
+//   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
+#include "adapter.cuh"
+#include "halves.cuh"
+
+namespace small {
+namespace {
+using namespace halves;
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 64;               // channels
+constexpr uint32_t kPixelBytes = kTile * 256, kRankBytes = kTile * 128;          // of a chunk of channels, of 32 ranks
+constexpr int kCluster = 8;              // blocks of adapter_filters_kernel
+
+struct Layout {
+    int tiles, chunks, filter_tiles;     // pixel tiles of an image, chunks of channels
+    size_t ranks_at, filters_at, scales_at, bytes;
+    Layout(int N, int C, int K, int HW, int R)
+        : tiles(ceil_div(HW, kTile)), chunks(ceil_div(C, kChunk)), filter_tiles(ceil_div(blocks_of(K), kFilterTile)) {
+        ranks_at = (size_t)N * tiles * chunks * kPixelBytes;
+        filters_at = ranks_at + (size_t)N * tiles * blocks_of(R) * kRankBytes;
+        scales_at = filters_at + (size_t)chunks * blocks_of(K) * 32 * 256;
+        bytes = scales_at + sizeof(int) * ((size_t)N * tiles + 4);       // exponents: the filters', three words unused, each pixel tile's
+    }
+};
+
+struct TcArgs {
+    AdaptArgs a;
+    AdapterShape s;
+    Layout at;
+    int *status;
+    uint32_t limit;
+};
+
+__device__ __forceinline__ char *ws_of(const TcArgs &c) { return static_cast<char *>(c.a.ws); }
+__device__ __forceinline__ int *exponents(const TcArgs &c) { return reinterpret_cast<int *>(ws_of(c) + c.at.scales_at); }
+__device__ __forceinline__ int tile_rows(const TcArgs &c, int kt) { return min(kFilterTile, c.s.KB - kt * kFilterTile) * 32; }
+__device__ __forceinline__ float block_max(float v, float *s) {
+#pragma unroll
+    for (int o = 16; o; o /= 2) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = s[0];
+#pragma unroll
+    for (int i = 1; i < kThreads / 32; ++i) v = fmaxf(v, s[i]);
+    return v;
+}
+
+// The FP32 section of the packed filters, [KB][CB][32 channels][32 filters], as halves [filter tile][chunk]{high: rows x 128 bytes, low: the same}.
+__global__ void __launch_bounds__(kThreads) adapter_filters_kernel(const TcArgs c) {
+    __shared__ float most_s[kThreads / 32], top, block[32][33];
+    grid_dep_sync();
+    grid_dep_trigger();
+    const int items = c.s.KB * c.at.chunks * 2, tid = threadIdx.x;
+    float most = 0.0f;
+    for (int i = blockIdx.x; i < items; i += kCluster) {
+        const int kb = i / (c.at.chunks * 2), cb = i % (c.at.chunks * 2);
+        if (cb >= c.s.CB) continue;
+        const float4 v = reinterpret_cast<const float4 *>(c.a.w)[((size_t)kb * c.s.CB + cb) * 256 + tid];
+        most = fmaxf(most, magnitude(v));
+    }
+    most = block_max(most, most_s);
+    if (tid == 0) top = most;
+    cluster_arrive();
+    cluster_wait();
+#pragma unroll
+    for (int b = 0; b < kCluster; ++b) most = fmaxf(most, cluster_read(&top, b));
+    cluster_arrive();
+    const int ex = top_exponent(most);
+    const float up = lift(ex);
+    if (blockIdx.x == 0 && tid == 0) exponents(c)[0] = ex;
+    char *out = ws_of(c) + c.at.filters_at;
+    for (int i = blockIdx.x; i < items; i += kCluster) {
+        const int kb = i / (c.at.chunks * 2), cb = i % (c.at.chunks * 2), kt = kb / kFilterTile, rows = tile_rows(c, kt);
+        __syncthreads();
+        const float4 v = cb < c.s.CB ? reinterpret_cast<const float4 *>(c.a.w)[((size_t)kb * c.s.CB + cb) * 256 + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
+        const int ch = tid >> 3, f0 = (tid & 7) * 4;
+        block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
+        __syncthreads();
+        const int f = tid >> 3, c0 = (tid & 7) * 4, row = kb % kFilterTile * 32 + f, col = (cb & 1) * 32 + c0;
+        const bool real = kb * 32 + f < c.s.K;
+        uint2 hi, lo;
+        split_finite(real ? block[f][c0] * up : 0.0f, real ? block[f][c0 + 1] * up : 0.0f, hi.x, lo.x);
+        split_finite(real ? block[f][c0 + 2] * up : 0.0f, real ? block[f][c0 + 3] * up : 0.0f, hi.y, lo.y);
+        char *to = out + ((size_t)kt * c.at.chunks * kFilterTile * 32 + (size_t)(cb >> 1) * rows) * 256;
+        *reinterpret_cast<uint2 *>(to + chunk_at(row, col, rows) + (col & 4) * 2) = hi;
+        *reinterpret_cast<uint2 *>(to + chunk_at(row, kChunk + col, rows) + (col & 4) * 2) = lo;
+    }
+    cluster_wait();                                      // the others have read this block's maximum
+}
+
+__global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArgs c) {
+    extern __shared__ float t_s[];                       // [128 pixels][RB * 32 + 4]
+    __shared__ float most_s[2][kThreads / 32];
+    const AdaptArgs &a = c.a;
+    const AdapterShape &s = c.s;
+    const int n = blockIdx.x / c.at.tiles, pt = blockIdx.x % c.at.tiles, p0 = pt * kTile, pixels = min(kTile, a.HW - p0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = s.RB * 32 + 4;
+    // What is read here is older than the kernel in front of this one, which has waited for all before itself; its result comes after the wait.
+    const float *x = a.in + (size_t)n * s.CB * a.HW * 32 + (size_t)p0 * 32;
+    const int id = a.adapter[n];
+    const bool some = id >= 0 && id < a.adapters;
+    float most = 0.0f, most_t = 0.0f;
+    if (some) {
+        const float factor = a.scale ? a.scale[id] : 1.0f;
+        for (int i = threadIdx.x; i < kTile * pitch; i += kThreads) t_s[i] = 0.0f;
+        __syncthreads();
+        // a warp takes four pixels and eight ranks at a time, a lane a channel of each block
+        for (int i = warp; i < kTile / 4 * (s.RP / 8); i += kThreads / 32) {
+            const int q0 = i / (s.RP / 8) * 4, rg = i % (s.RP / 8);
+            if (q0 >= pixels) break;
+            const float *w = a.packed + id * s.down + rg * 256 + lane;
+            float acc[32];
+#pragma unroll
+            for (int u = 0; u < 32; ++u) acc[u] = 0.0f;
+#pragma unroll 2
+            for (int cb = 0; cb < s.CB; ++cb) {
+                float v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[q] = q0 + q < pixels && cb * 32 + lane < s.C ? x[((size_t)cb * a.HW + q0 + q) * 32 + lane] : 0.0f;
+                    most = fmaxf(most, magnitude(v[q]));
+                }
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float u = w[(cb * s.RP + r) * 32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[q * 8 + r] = fmaf(v[q], u, acc[q * 8 + r]);
+                }
+            }
+            // halves of the sums go to halves of the lanes: lane l ends with pixel l / 8, rank l % 8
+#pragma unroll
+            for (int bit = 16; bit; bit /= 2)
+#pragma unroll
+                for (int u = 0; u < bit; ++u) {
+                    const bool upper = lane & bit;
+                    const float give = upper ? acc[u] : acc[u + bit], keep = upper ? acc[u + bit] : acc[u];
+                    acc[u] = keep + __shfl_xor_sync(~0u, give, bit);
+                }
+            const float t = q0 + lane / 8 < pixels ? factor * acc[0] : 0.0f;
+            t_s[(q0 + lane / 8) * pitch + rg * 8 + lane % 8] = t;
+            most_t = fmaxf(most_t, magnitude(t));
+        }
+    } else {
+        for (int i = threadIdx.x; i < s.CB * pixels * 8; i += kThreads) {
+            const int cb = i / (pixels * 8), e = i % (pixels * 8);
+            most = fmaxf(most, magnitude(reinterpret_cast<const float4 *>(x + (size_t)cb * a.HW * 32)[e]));
+        }
+    }
+    grid_dep_sync();                                     // the filters' exponent
+    grid_dep_trigger();
+    int ex = top_exponent(block_max(most, most_s[0])), et = 0;
+    if (some) {
+        const int ew = exponents(c)[0], eu = reinterpret_cast<const int *>(a.packed + s.exponents_at)[id];
+        ex = min(max(ex, top_exponent(block_max(most_t, most_s[1])) + eu - ew), 254);
+        et = ex + ew - eu;                               // t * lift(et) beside halves of Up meets the pixels' scale beside halves of the filters
+    }
+    if (threadIdx.x == 0) exponents(c)[4 + blockIdx.x] = ex;
+    const float up = lift(ex);
+    char *out = ws_of(c) + (size_t)blockIdx.x * c.at.chunks * kPixelBytes;
+    const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
+    for (int cb = 0; cb < c.at.chunks * 2; ++cb) {
+        float4 v[kTile / 32];
+#pragma unroll
+        for (int i = 0; i < kTile / 32; ++i) {
+            const int r = r0 + i * 32, ch = cb * 32 + c0;
+            v[i] = r < pixels && cb < s.CB ? *reinterpret_cast<const float4 *>(x + ((size_t)cb * a.HW + r) * 32 + c0) : make_float4(0.f, 0.f, 0.f, 0.f);
+            if (ch + 4 > s.C) {                          // pad lanes, whatever lies there
+                if (ch + 0 >= s.C) v[i].x = 0.0f;
+                if (ch + 1 >= s.C) v[i].y = 0.0f;
+                if (ch + 2 >= s.C) v[i].z = 0.0f;
+                v[i].w = 0.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(out + (size_t)(cb >> 1) * kPixelBytes, r0 + i * 32, (cb & 1) * 32 + c0, v[i], up);
+    }
+    if (!some) return;
+    const float up_t = et <= 254 ? lift(max(et, 15)) : 0.0f;         // 2^-100 of the sum and less: nothing
+    for (int rb = 0; rb < s.RB; ++rb)
+#pragma unroll
+        for (int i = 0; i < kTile / 32; ++i) {
+            const int r = r0 + i * 32;
+            store4<32>(ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes, r, c0, *reinterpret_cast<const float4 *>(t_s + r * pitch + rb * 32 + c0), up_t);
+        }
+}
+
+constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, kProductThreads = 320;
+
+template <bool kX3>
+__global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(const TcArgs c) {
+    extern __shared__ char raw[];
+    __shared__ uint64_t full_s[kStages], empty_s[kStages], done_s[2], free_s[2], drained;
+    __shared__ uint32_t tmem_s;
+    __shared__ int gave_up;
+    const AdaptArgs &a = c.a;
+    const AdapterShape &s = c.s;
+    const int warp = warp_index();
+    char *stages = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    const uint32_t full = smem_u32(full_s), empty = smem_u32(empty_s), done = smem_u32(done_s), free = smem_u32(free_s);
+    if (warp == 9) tmem_alloc(smem_u32(&tmem_s), 512);
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int i = 0; i < kStages; ++i) { mbar_init(full + i * 8, 1); mbar_init(empty + i * 8, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(done + i * 8, 1); mbar_init(free + i * 8, 256); }
+        mbar_init(smem_u32(&drained), 1);
+        mbar_fence_init();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    grid_dep_sync();
+    grid_dep_trigger();
+    const uint32_t tmem = tmem_s;
+    volatile int *stop = &gave_up;
+    const int pixel_tiles = a.N * c.at.tiles, work = pixel_tiles * c.at.filter_tiles;
+    auto ranks_of = [&](int np) {                        // rank blocks of a pixel tile
+        const int id = a.adapter[np / c.at.tiles];
+        return id >= 0 && id < a.adapters ? s.RB : 0;
+    };
+    int issued = 0;                                      // stages, by warp 8
+    if (warp == 8) {
+        int slot = 0, phase = 1;
+        bool ok = true;
+        for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
+            const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, rows = tile_rows(c, kt), ranks = ranks_of(np);
+            const int id = ranks ? a.adapter[np / c.at.tiles] : 0;
+            const char *x = ws_of(c) + (size_t)np * c.at.chunks * kPixelBytes, *t = ws_of(c) + c.at.ranks_at + (size_t)np * s.RB * kRankBytes;
+            const char *w = ws_of(c) + c.at.filters_at + (size_t)kt * c.at.chunks * kFilterTile * 32 * 256;
+            const char *u = reinterpret_cast<const char *>(a.packed + s.halves_at + id * s.up_halves) + (size_t)kt * s.RB * kFilterTile * 32 * 128;
+            for (int k = 0; k < c.at.chunks + ranks; ++k) {
+                if (issued >= kStages && !(ok = mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit))) break;
+                const int rb = k - c.at.chunks;
+                // high parts lie in front: without the low ones half of a chunk is enough (32 ranks have both in a row)
+                const uint32_t nx = rb >= 0 ? kRankBytes : kX3 ? kPixelBytes : kPixelBytes / 2, nw = rb >= 0 ? rows * 128 : kX3 ? rows * 256 : rows * 128;
+                if (elect_one()) {
+                    const uint32_t to = smem_u32(stages + slot * kStageBytes);
+                    mbar_expect_tx(full + slot * 8, nx + nw);
+                    bulk_load(to, rb >= 0 ? t + (size_t)rb * kRankBytes : x + (size_t)k * kPixelBytes, nx, full + slot * 8);
+                    bulk_load(to + kPixelBytes, rb >= 0 ? u + (size_t)rb * rows * 128 : w + (size_t)k * rows * 256, nw, full + slot * 8);
+                }
+                __syncwarp();
+                ++issued;
+                if (++slot == kStages) { slot = 0; phase ^= 1; }
+            }
+        }
+    } else if (warp == 9) {
+        const uint32_t first = smem_desc_lo(smem_u32(stages));
+        int slot = 0, phase = 0, buffer = 0, buffer_phase = 1;
+        bool ok = true;
+        for (int i = blockIdx.x, turn = 0; i < work && ok; i += gridDim.x, ++turn) {
+            const int np = i / c.at.filter_tiles, rows = tile_rows(c, i % c.at.filter_tiles), ranks = ranks_of(np);
+            const uint32_t desc = f16_desc(rows), d = tmem + buffer * 256;
+            if (turn >= 2 && !(ok = mbar_wait_uniform(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
+            for (int k = 0; k < c.at.chunks + ranks; ++k) {
+                if (!(ok = mbar_wait_uniform(full + slot * 8, phase, stop, c.status, c.limit))) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
+                    if (k < c.at.chunks) {
+#pragma unroll
+                        for (int term = kX3 ? 0 : 2; term < 3; ++term)           // small terms first
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                mma_f16(d, x + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), w + e * 2 + (term == 1 ? rows * 8 : 0), desc, k > 0 || e > 0 || term > (kX3 ? 0 : 2));
+                    } else {
+                        const int steps = (min(s.R - (k - c.at.chunks) * 32, 32) + 15) / 16;
+#pragma unroll
+                        for (int term = kX3 ? 0 : 2; term < 3; ++term)
+                            for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, 1);
+                    }
+                    mma_commit(empty + slot * 8);
+                    if (k == c.at.chunks + ranks - 1) mma_commit(done + buffer * 8);
+                }
+                __syncwarp();
+                if (++slot == kStages) { slot = 0; phase ^= 1; }
+            }
+            if (++buffer == 2) { buffer = 0; buffer_phase ^= 1; }
+        }
+        if (!ok) {
+            if (elect_one()) mma_commit(smem_u32(&drained));
+            __syncwarp();
+            mbar_wait(smem_u32(&drained), 0, c.limit);
+        }
+    } else {
+        const int lane = threadIdx.x & 31, half = warp >> 2;
+        const float w_drop = drop(exponents(c)[0]);
+        int buffer = 0, phase = 0;
+        for (int i = blockIdx.x; i < work; i += gridDim.x) {
+            const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p = np % c.at.tiles * kTile + (warp & 3) * 32 + lane;
+            const float x_drop = drop(exponents(c)[4 + np]);
+            if (!mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit)) break;
+            tc_fence_after();
+            const int blocks = tile_rows(c, kt) / 32;
+            for (int b = half; b < blocks; b += 2) {
+                float v[32];
+                tmem_ld32(tmem + buffer * 256 + b * 32 + ((uint32_t)(warp & 3) << 21), v);
+                const int k0 = (kt * kFilterTile + b) * 32;
+                if (p < a.HW) {
+                    float *out = a.out + (((size_t)n * s.KB + k0 / 32) * a.HW + p) * 32;
+#pragma unroll
+                    for (int u = 0; u < 32; u += 8) {
+                        float before[8];
+                        if (a.accumulate) ld_global_v8(out + u, before);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float y = v[u + e] * x_drop * w_drop;
+                            const bool real = k0 + u + e < s.K;
+                            if (a.bias && real) y += a.bias[k0 + u + e];
+                            if (a.accumulate) y += before[e];
+                            if (a.relu) y = y > 0.0f ? y : 0.0f;
+                            v[u + e] = real ? y : 0.0f;
+                        }
+                        st_global_v8(out + u, v + u);
+                    }
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(free + buffer * 8);
+            if (++buffer == 2) { buffer = 0; phase ^= 1; }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (gave_up && warp == 8)                            // what is still on its way must land before the block ends
+        for (int x = max(0, issued - kStages); x < issued; ++x) mbar_wait(full + x % kStages * 8, (x / kStages) & 1, c.limit);
+    if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// Up as halves; a block an adapter.
+__global__ void __launch_bounds__(kThreads) pack_up_halves_kernel(const float *__restrict__ up, float *__restrict__ packed, int adapters, const AdapterShape s) {
+    __shared__ float most_s[kThreads / 32];
+    grid_dep_sync();
+    grid_dep_trigger();
+    const int a = blockIdx.x;
+    const float *w = up + (size_t)a * s.K * s.R;
+    float most = 0.0f;
+    for (size_t i = threadIdx.x; i < (size_t)s.K * s.R; i += kThreads) most = fmaxf(most, magnitude(w[i]));
+    const int ex = top_exponent(block_max(most, most_s));
+    const float by = lift(ex);
+    if (threadIdx.x == 0) reinterpret_cast<int *>(packed + s.exponents_at)[a] = ex;
+    char *out = reinterpret_cast<char *>(packed + s.halves_at + a * s.up_halves);
+    for (size_t i = threadIdx.x; i < (size_t)s.KB * 32 * s.RB * 8; i += kThreads) {          // four ranks each
+        const int r = (int)(i & 7) * 4, rb = (int)(i / 8 % s.RB), k = (int)(i / 8 / s.RB), kt = k / (kFilterTile * 32);
+        const int rows = min(kFilterTile, s.KB - kt * kFilterTile) * 32, row = k % (kFilterTile * 32);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = k < s.K && rb * 32 + r + e < s.R ? w[(size_t)k * s.R + rb * 32 + r + e] * by : 0.0f;
+        uint2 hi, lo;
+        split_finite(v[0], v[1], hi.x, lo.x);
+        split_finite(v[2], v[3], hi.y, lo.y);
+        char *to = out + ((size_t)kt * s.RB * kFilterTile * 32 + (size_t)rb * rows) * 128;
+        *reinterpret_cast<uint2 *>(to + chunk_at(row, r, rows) + (r & 4) * 2) = hi;
+        *reinterpret_cast<uint2 *>(to + chunk_at(row, 32 + r, rows) + (r & 4) * 2) = lo;
+    }
+}
+
+}  // namespace
+
+bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms) {
+    (void)C; (void)R;
+    const long long tiles = (long long)N * ceil_div(HW, kTile) * ceil_div(blocks_of(K), kFilterTile);
+    return HW >= 64 && tiles >= sms / 2 && tiles < (1 << 28);
+}
+
+size_t adapted_tc_workspace(int N, int C, int K, int HW, int R) { return Layout(N, C, K, HW, R).bytes; }
+
+int launch_pack_up_halves(small_ctx *ctx, const float *up, float *packed, int adapters, const AdapterShape &s, cudaStream_t st) {
+    launch_kernel(ctx, pack_up_halves_kernel, dim3((unsigned)adapters), dim3(kThreads), 0, st, up, packed, adapters, s);
+    return check_launch(ctx);
+}
+
+int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s, bool x3, cudaStream_t st) {
+    const TcArgs c{a, s, Layout(a.N, s.C, s.K, a.HW, s.R), ctx->dev_status, ctx->wait_iters};
+    launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads), kCluster, 0, st, c);
+    if (int e = check_launch(ctx)) return e;
+    static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
+    const size_t t = sizeof(float) * kTile * (s.RB * 32 + 4), stages = 1024 + (size_t)kStages * kStageBytes;
+    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, sizeof(float) * kTile * (128 + 4))) return e;
+    launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), t, st, c);
+    if (int e = check_launch(ctx)) return e;
+    const int work = a.N * c.at.tiles * c.at.filter_tiles;
+    const dim3 grid((unsigned)(work < ctx->sm_count ? work : ctx->sm_count));
+    if (x3) {
+        if (int e = allow_shared_memory(ctx, adapter_product_kernel<true>, exact, stages)) return e;
+        launch_kernel(ctx, adapter_product_kernel<true>, grid, dim3(kProductThreads), stages, st, c);
+    } else {
+        if (int e = allow_shared_memory(ctx, adapter_product_kernel<false>, fast, stages)) return e;
+        launch_kernel(ctx, adapter_product_kernel<false>, grid, dim3(kProductThreads), stages, st, c);
+    }
+    return check_launch(ctx);
+}
+
+}  // namespace small

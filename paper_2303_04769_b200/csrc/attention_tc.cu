@@ -1,9 +1,7 @@
 // Attention over the pixels of a plane on the tensor cores (tcgen05, kind::f16), at TF32's or FP32's accuracy.
 //
-// Operands.  A float x is x_hi + x_lo, two halves of 11 significant bits each after a power of two has brought the largest value of its
-// row (queries) or tile (keys, values) to 2^14 .. 2^15, so nothing the sums can see is lost to half precision's range.  3xTF32 forms
-// hi*hi + hi*lo + lo*hi, TF32 hi*hi alone: a half has TF32's 11 bits, and kind::f16 runs at twice kind::tf32's rate and reads half
-// the bytes.  Weights exp(x - m) are scaled by 2^14 for the same reason; the sum of weights too, so that it cancels.
+// Operands are pairs of halves (halves.cuh); weights exp(x - m) are scaled by 2^14 so that theirs are exact far down, and the sum of
+// weights too, so that it cancels.
 //
 // attention_tiles_kernel lays the valid keys and values of each image out once, 128 keys a tile, as the MMAs read them: keys
 // [key][hi | lo channels], values transposed [channel][hi keys | lo keys], rows of 128 bytes swizzled, so that a tile is two plain
@@ -16,63 +14,16 @@
 // they are the second product's A operand.  While one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
 // added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
 // thousands of keys would add up (5e-8 a step), and no rescaling of tensor memory is needed when the maximum grows.
-#include <cuda_fp16.h>
 #include <type_traits>
 
 #include "attention.cuh"
-#include "sm100.cuh"
+#include "halves.cuh"
 
 namespace small {
 namespace {
-using namespace sm100;
+using namespace halves;
 
-constexpr int kTile = 128;               // queries and keys of a tile
 constexpr float kLift = 14.0f;           // weights are scaled by 2^14
-
-// The exponent that brings |x| <= most to below 2^15: x * lift(e) and back by drop(e).
-__device__ __forceinline__ int top_exponent(float most) { return min(max((int)(__float_as_uint(most) >> 23), 15), 254); }     // most >= 0
-__device__ __forceinline__ float lift(int e) { return __uint_as_float((uint32_t)(268 - e) << 23); }
-__device__ __forceinline__ float drop(int e) { return __uint_as_float((uint32_t)(e - 14) << 23); }
-
-// |x|; what is not finite does not count: it stays what it is at any scale, and must not take its tile's other values with it.
-__device__ __forceinline__ float magnitude(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
-
-__device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-// Two floats -> their leading halves and what these leave.
-__device__ __forceinline__ void split(float a, float b, uint32_t &hi, uint32_t &lo) {
-    const float ah = __uint_as_float(__float_as_uint(a) & 0xffffe000u), bh = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
-    hi = pack_halves(ah, bh);
-    lo = pack_halves(a - ah, b - bh);
-}
-// The same for operands: what is left of a value that is not finite is 0, or it would turn infinities into NaN in every product.
-__device__ __forceinline__ void split_finite(float a, float b, uint32_t &hi, uint32_t &lo) {
-    split(a, b, hi, lo);
-    if (!(fabsf(a) <= 65504.0f) || !(fabsf(b) <= 65504.0f)) {
-        const float ah = __uint_as_float(__float_as_uint(a) & 0xffffe000u), bh = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
-        hi = pack_halves(fabsf(a) <= 65504.0f ? ah : a, fabsf(b) <= 65504.0f ? bh : b);
-        lo = pack_halves(fabsf(a) <= 65504.0f ? a - ah : 0.0f, fabsf(b) <= 65504.0f ? b - bh : 0.0f);
-    }
-}
-
-// Byte of the 16-byte chunk that holds columns c .. c + 7 of row r: atoms of 64 columns, `rows` rows of 128 bytes each, swizzled.
-__device__ __forceinline__ uint32_t chunk_at(int r, int c, int rows) {
-    return (uint32_t)(c >> 6) * rows * 128 + r * 128 + ((((uint32_t)c >> 3 & 7) ^ (r & 7)) << 4);
-}
-
-__device__ __forceinline__ float magnitude(float4 v) { return fmaxf(fmaxf(magnitude(v.x), magnitude(v.y)), fmaxf(magnitude(v.z), magnitude(v.w))); }
-// Their high and low parts to a tile of `DP` channels of high parts and as many of low ones.
-template <int DP>
-__device__ __forceinline__ void store4(char *tile, int r, int c, float4 v, float up) {
-    uint2 hi, lo;
-    split_finite(v.x * up, v.y * up, hi.x, lo.x);
-    split_finite(v.z * up, v.w * up, hi.y, lo.y);
-    *reinterpret_cast<uint2 *>(tile + chunk_at(r, c, kTile) + (c & 4) * 2) = hi;
-    *reinterpret_cast<uint2 *>(tile + chunk_at(r, DP + c, kTile) + (c & 4) * 2) = lo;
-}
 
 // Workspace: [N][kv_heads][tiles]{keys: DP * 512 bytes, values: DP * 512 bytes}; int[N][tiles][128], the keys' places in the bias table
 // (of_key); float[N][kv_heads][tiles][2], how to undo the scaling.
@@ -151,21 +102,6 @@ __global__ void __launch_bounds__(256) attention_tiles_kernel(const AttnArgs a, 
         *reinterpret_cast<uint4 *>(out + chunk_at(d, kTile + k0, DP)) = lo;
     }
 }
-
-// D[tmem] (+)= A * B^T in halves, FP32 accumulate, M = 128, K = 16; A from shared memory, or from tensor memory (two halves a column).
-__device__ __forceinline__ void mma_f16(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}"
-        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
-        ::"r"(d), "r"(a), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ uint32_t f16_desc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
 
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(
