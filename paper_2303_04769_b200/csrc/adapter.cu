@@ -148,7 +148,7 @@ SMALL_API int small_pack_adapters(small_ctx *ctx, const float *down, const float
     const AdapterShape s(adapters, C, K, R);
     launch_kernel(ctx, pack_adapters_kernel, dim3(task_blocks(ctx, (long long)((s.down + s.up) * adapters / 32))), dim3(kThreads), 0, st, down, up, packed, adapters, s);
     if (int e = check_launch(ctx)) return e;
-    return launch_pack_up_halves(ctx, up, packed, adapters, s, st);
+    return launch_pack_halves(ctx, down, up, packed, adapters, s, st);
 }
 
 SMALL_API size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R) {

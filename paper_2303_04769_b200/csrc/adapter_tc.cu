@@ -3,9 +3,11 @@
 // written once.  Operands are pairs of halves (halves.cuh).
 //
 // adapter_filters_kernel: the filters as halves, 64 channels a chunk, one exponent for the layer (a cluster finds it).
-// adapter_pixels_kernel: 128 pixels of an image a block: t in FP32 and the largest value in one pass over them (from memory), halves in a second
-//   (from L2).  t shares the pixels' accumulator, so its exponent follows from theirs, the filters' and the adapter's; where that would pass
-//   half precision's range the pixels take a smaller scale, which loses nothing: the sum is the adapter's part then.
+// adapter_pixels_kernel: 128 pixels of an image a block: the largest value in one pass over them (from memory), halves in a second (from
+//   L2), which pass through shared memory, where the product with Down is taken from them.  t shares the pixels' accumulator later, so its
+//   exponent follows from theirs, the filters' and the adapter's; where t could pass half precision's range - it is at most the largest value
+//   times the largest sum of a Down row's magnitudes - the pixels take a smaller scale, 2 to 5 powers of two as a rule, of 17 that halves of both
+//   kinds have to spare.
 // adapter_product_kernel: a block walks tiles of 128 pixels x 256 filters; warps for loading (plain bulk copies, two stages of 96 KB), MMAs
 //   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
@@ -19,13 +21,14 @@ using namespace halves;
 constexpr int kThreads = 256;
 constexpr int kChunk = 64;               // channels
 constexpr uint32_t kPixelBytes = kTile * 256, kRankBytes = kTile * 128;          // of a chunk of channels, of 32 ranks
-constexpr int kCluster = 8;              // blocks of adapter_filters_kernel
+constexpr int kCluster = 8, kTeams = 4;  // blocks of adapter_filters_kernel, teams of 256 threads of a block
 
 struct Layout {
-    int tiles, chunks, filter_tiles;     // pixel tiles of an image, chunks of channels
+    int tiles, filter_tiles;             // pixel tiles of an image
     size_t ranks_at, filters_at, scales_at, bytes;
     Layout(int N, int C, int K, int HW, int R)
-        : tiles(ceil_div(HW, kTile)), chunks(ceil_div(C, kChunk)), filter_tiles(ceil_div(blocks_of(K), kFilterTile)) {
+        : tiles(ceil_div(HW, kTile)), filter_tiles(ceil_div(blocks_of(K), kFilterTile)) {
+        const int chunks = ceil_div(C, kChunk);
         ranks_at = (size_t)N * tiles * chunks * kPixelBytes;
         filters_at = ranks_at + (size_t)N * tiles * blocks_of(R) * kRankBytes;
         scales_at = filters_at + (size_t)chunks * blocks_of(K) * 32 * 256;
@@ -51,25 +54,22 @@ __device__ __forceinline__ float block_max(float v, float *s) {
     __syncthreads();
     v = s[0];
 #pragma unroll
-    for (int i = 1; i < kThreads / 32; ++i) v = fmaxf(v, s[i]);
+    for (int i = 1; i < (int)blockDim.x / 32; ++i) v = fmaxf(v, s[i]);
     return v;
 }
 
 // The FP32 section of the packed filters, [KB][CB][32 channels][32 filters], as halves [filter tile][chunk]{high: rows x 128 bytes, low: the same}.
-__global__ void __launch_bounds__(kThreads) adapter_filters_kernel(const TcArgs c) {
-    __shared__ float most_s[kThreads / 32], top, block[32][33];
+__global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const TcArgs c) {
+    __shared__ float most_s[kThreads * kTeams / 32], top, blocks[kTeams][32][33];
     grid_dep_sync();
     grid_dep_trigger();
-    const int items = c.s.KB * c.at.chunks * 2, tid = threadIdx.x;
+    const int items = c.s.KB * c.s.chunks * 2, tid = threadIdx.x % kThreads, team = blockIdx.x * kTeams + threadIdx.x / kThreads;
+    const float4 *w = reinterpret_cast<const float4 *>(c.a.w);
     float most = 0.0f;
-    for (int i = blockIdx.x; i < items; i += kCluster) {
-        const int kb = i / (c.at.chunks * 2), cb = i % (c.at.chunks * 2);
-        if (cb >= c.s.CB) continue;
-        const float4 v = reinterpret_cast<const float4 *>(c.a.w)[((size_t)kb * c.s.CB + cb) * 256 + tid];
-        most = fmaxf(most, magnitude(v));
-    }
+#pragma unroll 4
+    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < (size_t)c.s.KB * c.s.CB * 256; i += kCluster * kThreads * kTeams) most = fmaxf(most, magnitude(w[i]));
     most = block_max(most, most_s);
-    if (tid == 0) top = most;
+    if (threadIdx.x == 0) top = most;
     cluster_arrive();
     cluster_wait();
 #pragma unroll
@@ -77,121 +77,181 @@ __global__ void __launch_bounds__(kThreads) adapter_filters_kernel(const TcArgs 
     cluster_arrive();
     const int ex = top_exponent(most);
     const float up = lift(ex);
-    if (blockIdx.x == 0 && tid == 0) exponents(c)[0] = ex;
+    if (blockIdx.x == 0 && threadIdx.x == 0) exponents(c)[0] = ex;
     char *out = ws_of(c) + c.at.filters_at;
-    for (int i = blockIdx.x; i < items; i += kCluster) {
-        const int kb = i / (c.at.chunks * 2), cb = i % (c.at.chunks * 2), kt = kb / kFilterTile, rows = tile_rows(c, kt);
+    float (*block)[33] = blocks[threadIdx.x / kThreads];
+    for (int i0 = 0; i0 < items; i0 += kCluster * kTeams) {
+        const int i = i0 + team, kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2), kt = kb / kFilterTile;
         __syncthreads();
-        const float4 v = cb < c.s.CB ? reinterpret_cast<const float4 *>(c.a.w)[((size_t)kb * c.s.CB + cb) * 256 + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
-        const int ch = tid >> 3, f0 = (tid & 7) * 4;
-        block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
+        if (i < items) {
+            const float4 v = cb < c.s.CB ? w[((size_t)kb * c.s.CB + cb) * 256 + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
+            const int ch = tid >> 3, f0 = (tid & 7) * 4;
+            block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
+        }
         __syncthreads();
-        const int f = tid >> 3, c0 = (tid & 7) * 4, row = kb % kFilterTile * 32 + f, col = (cb & 1) * 32 + c0;
+        if (i >= items) continue;
+        const int f = tid >> 3, c0 = (tid & 7) * 4, rows = tile_rows(c, kt), row = kb % kFilterTile * 32 + f, col = (cb & 1) * 32 + c0;
         const bool real = kb * 32 + f < c.s.K;
         uint2 hi, lo;
         split_finite(real ? block[f][c0] * up : 0.0f, real ? block[f][c0 + 1] * up : 0.0f, hi.x, lo.x);
         split_finite(real ? block[f][c0 + 2] * up : 0.0f, real ? block[f][c0 + 3] * up : 0.0f, hi.y, lo.y);
-        char *to = out + ((size_t)kt * c.at.chunks * kFilterTile * 32 + (size_t)(cb >> 1) * rows) * 256;
+        char *to = out + ((size_t)kt * c.s.chunks * kFilterTile * 32 + (size_t)(cb >> 1) * rows) * 256;
         *reinterpret_cast<uint2 *>(to + chunk_at(row, col, rows) + (col & 4) * 2) = hi;
         *reinterpret_cast<uint2 *>(to + chunk_at(row, kChunk + col, rows) + (col & 4) * 2) = lo;
     }
     cluster_wait();                                      // the others have read this block's maximum
 }
 
+__device__ __forceinline__ void bulk_store(void *to, uint32_t from, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+}
+template <int kLeft>
+__device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
+
 __global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArgs c) {
-    extern __shared__ float t_s[];                       // [128 pixels][RB * 32 + 4]
-    __shared__ float most_s[2][kThreads / 32];
+    extern __shared__ char raw[];                        // two chunks of pixels, two of Down
+    __shared__ float most_s[kThreads / 32];
+    __shared__ uint64_t down_s[2], used_s[2];
+    __shared__ uint32_t tmem_s;
+    __shared__ int gave_up;
     const AdaptArgs &a = c.a;
     const AdapterShape &s = c.s;
     const int n = blockIdx.x / c.at.tiles, pt = blockIdx.x % c.at.tiles, p0 = pt * kTile, pixels = min(kTile, a.HW - p0);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pitch = s.RB * 32 + 4;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
+    char *chunks = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u), *downs = chunks + 2 * kPixelBytes;
+    const uint32_t down_bytes = s.RQ * 256, down = smem_u32(down_s), used = smem_u32(used_s);
+    const uint32_t columns = s.RQ <= 32 ? 32 : s.RQ <= 64 ? 64 : 128;
     // What is read here is older than the kernel in front of this one, which has waited for all before itself; its result comes after the wait.
     const float *x = a.in + (size_t)n * s.CB * a.HW * 32 + (size_t)p0 * 32;
     const int id = a.adapter[n];
     const bool some = id >= 0 && id < a.adapters;
-    float most = 0.0f, most_t = 0.0f;
-    if (some) {
-        const float factor = a.scale ? a.scale[id] : 1.0f;
-        for (int i = threadIdx.x; i < kTile * pitch; i += kThreads) t_s[i] = 0.0f;
-        __syncthreads();
-        // a warp takes four pixels and eight ranks at a time, a lane a channel of each block
-        for (int i = warp; i < kTile / 4 * (s.RP / 8); i += kThreads / 32) {
-            const int q0 = i / (s.RP / 8) * 4, rg = i % (s.RP / 8);
-            if (q0 >= pixels) break;
-            const float *w = a.packed + id * s.down + rg * 256 + lane;
-            float acc[32];
-#pragma unroll
-            for (int u = 0; u < 32; ++u) acc[u] = 0.0f;
-#pragma unroll 2
-            for (int cb = 0; cb < s.CB; ++cb) {
-                float v[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] = q0 + q < pixels && cb * 32 + lane < s.C ? x[((size_t)cb * a.HW + q0 + q) * 32 + lane] : 0.0f;
-                    most = fmaxf(most, magnitude(v[q]));
-                }
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const float u = w[(cb * s.RP + r) * 32];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[q * 8 + r] = fmaf(v[q], u, acc[q * 8 + r]);
-                }
-            }
-            // halves of the sums go to halves of the lanes: lane l ends with pixel l / 8, rank l % 8
-#pragma unroll
-            for (int bit = 16; bit; bit /= 2)
-#pragma unroll
-                for (int u = 0; u < bit; ++u) {
-                    const bool upper = lane & bit;
-                    const float give = upper ? acc[u] : acc[u + bit], keep = upper ? acc[u + bit] : acc[u];
-                    acc[u] = keep + __shfl_xor_sync(~0u, give, bit);
-                }
-            const float t = q0 + lane / 8 < pixels ? factor * acc[0] : 0.0f;
-            t_s[(q0 + lane / 8) * pitch + rg * 8 + lane % 8] = t;
-            most_t = fmaxf(most_t, magnitude(t));
+    const char *halves = reinterpret_cast<const char *>(a.packed + s.down_halves_at + (some ? id : 0) * s.down_halves);
+    auto load_down = [&](int k) {
+        if (elect_one()) {
+            mbar_expect_tx(down + (k & 1) * 8, down_bytes);
+            bulk_load(smem_u32(downs + (k & 1) * down_bytes), halves + (size_t)k * down_bytes, down_bytes, down + (k & 1) * 8);
         }
-    } else {
-        for (int i = threadIdx.x; i < s.CB * pixels * 8; i += kThreads) {
-            const int cb = i / (pixels * 8), e = i % (pixels * 8);
-            most = fmaxf(most, magnitude(reinterpret_cast<const float4 *>(x + (size_t)cb * a.HW * 32)[e]));
+        __syncwarp();
+    };
+    if (warp == 0) {
+        if (elect_one()) {
+            gave_up = 0;
+            for (int i = 0; i < 2; ++i) { mbar_init(down + i * 8, 1); mbar_init(used + i * 8, 1); }
+            mbar_fence_init();
+        }
+        __syncwarp();
+        if (some) {
+            tmem_alloc(smem_u32(&tmem_s), columns);
+            for (int k = 0; k < min(2, s.chunks); ++k) load_down(k);
         }
     }
+    float most = 0.0f;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < s.CB * pixels * 8; i += kThreads) {
+        const int cb = i / (pixels * 8), e = i % (pixels * 8);
+        most = fmaxf(most, magnitude(reinterpret_cast<const float4 *>(x + (size_t)cb * a.HW * 32)[e]));
+    }
+    most = block_max(most, most_s);
     grid_dep_sync();                                     // the filters' exponent
     grid_dep_trigger();
-    int ex = top_exponent(block_max(most, most_s[0])), et = 0;
+    int ex = top_exponent(most), et = 0;
+    float factor = 1.0f;
     if (some) {
-        const int ew = exponents(c)[0], eu = reinterpret_cast<const int *>(a.packed + s.exponents_at)[id];
-        ex = min(max(ex, top_exponent(block_max(most_t, most_s[1])) + eu - ew), 254);
+        const float *info = a.packed + s.info_at + 4 * (size_t)id;
+        const int ew = exponents(c)[0], eu = __float_as_int(info[0]), ed = __float_as_int(info[1]);
+        const float by = a.scale ? a.scale[id] : 1.0f;
+        ex = min(max(ex, top_exponent(fmaxf(most * info[2] * magnitude(by), 0.0f)) + eu - ew), 254);
         et = ex + ew - eu;                               // t * lift(et) beside halves of Up meets the pixels' scale beside halves of the filters
+        factor = et <= 254 ? by * drop(ed) : 0.0f;       // (beyond: 2^-100 of the sum and less, nothing)
+        et = min(max(et, 15), 254);
     }
     if (threadIdx.x == 0) exponents(c)[4 + blockIdx.x] = ex;
     const float up = lift(ex);
-    char *out = ws_of(c) + (size_t)blockIdx.x * c.at.chunks * kPixelBytes;
+    char *out = ws_of(c) + (size_t)blockIdx.x * s.chunks * kPixelBytes;
     const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
-    for (int cb = 0; cb < c.at.chunks * 2; ++cb) {
-        float4 v[kTile / 32];
+    const uint32_t tmem = tmem_s, desc = f16_desc(s.RQ);
+    for (int k = 0; k < s.chunks; ++k) {
+        char *chunk = chunks + (k & 1) * kPixelBytes;
+        if (k >= 2) {                                    // the chunk before the last is out, and its product is done
+            if (warp == 0) {
+                bulk_store_wait<1>();
+                if (some) {
+                    mbar_wait_uniform(used + (k & 1) * 8, (k >> 1) - 1 & 1, &gave_up, c.status, c.limit);
+                    load_down(k);
+                }
+            }
+            __syncthreads();
+        }
 #pragma unroll
-        for (int i = 0; i < kTile / 32; ++i) {
-            const int r = r0 + i * 32, ch = cb * 32 + c0;
-            v[i] = r < pixels && cb < s.CB ? *reinterpret_cast<const float4 *>(x + ((size_t)cb * a.HW + r) * 32 + c0) : make_float4(0.f, 0.f, 0.f, 0.f);
-            if (ch + 4 > s.C) {                          // pad lanes, whatever lies there
-                if (ch + 0 >= s.C) v[i].x = 0.0f;
-                if (ch + 1 >= s.C) v[i].y = 0.0f;
-                if (ch + 2 >= s.C) v[i].z = 0.0f;
-                v[i].w = 0.0f;
+        for (int g = 0; g < 2; ++g) {
+            const int cb = k * 2 + g, ch = cb * 32 + c0;
+            float4 v[kTile / 32];
+#pragma unroll
+            for (int i = 0; i < kTile / 32; ++i) {
+                const int r = r0 + i * 32;
+                v[i] = r < pixels && cb < s.CB ? *reinterpret_cast<const float4 *>(x + ((size_t)cb * a.HW + r) * 32 + c0) : make_float4(0.f, 0.f, 0.f, 0.f);
+                if (ch + 4 > s.C) {                      // pad lanes, whatever lies there
+                    if (ch + 0 >= s.C) v[i].x = 0.0f;
+                    if (ch + 1 >= s.C) v[i].y = 0.0f;
+                    if (ch + 2 >= s.C) v[i].z = 0.0f;
+                    v[i].w = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v[i], up);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        if (warp == 0) {
+            if (some) mbar_wait_uniform(down + (k & 1) * 8, k >> 1 & 1, &gave_up, c.status, c.limit);
+            tc_fence_after();
+            if (elect_one()) {
+                bulk_store(out + (size_t)k * kPixelBytes, smem_u32(chunk), kPixelBytes);
+                if (some) {
+                    const uint32_t xa = smem_desc_lo(smem_u32(chunk)), wa = smem_desc_lo(smem_u32(downs + (k & 1) * down_bytes));
+                    for (int term = 0; term < 3; ++term)             // small terms first
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            mma_f16(tmem, xa + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), wa + e * 2 + (term == 1 ? s.RQ * 8 : 0), desc, k > 0 || e > 0 || term > 0);
+                    mma_commit(used + (k & 1) * 8);
+                }
+            }
+            __syncwarp();
+        }
+    }
+    if (some) {
+        const int last = s.chunks - 1;
+        if (s.chunks > 1) mbar_wait_uniform(used + (last - 1 & 1) * 8, last - 1 >> 1 & 1, &gave_up, c.status, c.limit);
+        mbar_wait_uniform(used + (last & 1) * 8, last >> 1 & 1, &gave_up, c.status, c.limit);
+        tc_fence_after();
+        const int row = (warp & 3) * 32 + lane;
+        for (int rb = warp >> 2; rb < s.RB; rb += 2) {   // a thread a pixel and 32 ranks
+            char *to = ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes;
+            float v[32];
+            tmem_ld32(tmem + rb * 32 + ((uint32_t)(warp & 3) << 21), v);
+#pragma unroll
+            for (int u = 0; u < 32; u += 4) {
+                // columns behind RQ have no product in them
+                const bool real = rb * 32 + u < s.RQ && row < pixels;
+                const float4 t = real ? make_float4(v[u] * drop(ex) * factor, v[u + 1] * drop(ex) * factor, v[u + 2] * drop(ex) * factor, v[u + 3] * drop(ex) * factor)
+                                      : make_float4(0.f, 0.f, 0.f, 0.f);
+                store4<32>(to, row, u, t, lift(et));
             }
         }
-#pragma unroll
-        for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(out + (size_t)(cb >> 1) * kPixelBytes, r0 + i * 32, (cb & 1) * 32 + c0, v[i], up);
     }
+    if (warp == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     if (!some) return;
-    const float up_t = et <= 254 ? lift(max(et, 15)) : 0.0f;         // 2^-100 of the sum and less: nothing
-    for (int rb = 0; rb < s.RB; ++rb)
-#pragma unroll
-        for (int i = 0; i < kTile / 32; ++i) {
-            const int r = r0 + i * 32;
-            store4<32>(ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes, r, c0, *reinterpret_cast<const float4 *>(t_s + r * pitch + rb * 32 + c0), up_t);
-        }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) {
+        if (gave_up)                                     // what is still on its way must land before the block ends
+            for (int k = max(0, s.chunks - 2); k < s.chunks; ++k) {
+                mbar_wait(down + (k & 1) * 8, k >> 1 & 1, c.limit);
+                mbar_wait(used + (k & 1) * 8, k >> 1 & 1, c.limit);
+            }
+        tmem_dealloc(tmem, columns);
+    }
 }
 
 constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, kProductThreads = 320;
@@ -234,19 +294,20 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, rows = tile_rows(c, kt), ranks = ranks_of(np);
             const int id = ranks ? a.adapter[np / c.at.tiles] : 0;
-            const char *x = ws_of(c) + (size_t)np * c.at.chunks * kPixelBytes, *t = ws_of(c) + c.at.ranks_at + (size_t)np * s.RB * kRankBytes;
-            const char *w = ws_of(c) + c.at.filters_at + (size_t)kt * c.at.chunks * kFilterTile * 32 * 256;
-            const char *u = reinterpret_cast<const char *>(a.packed + s.halves_at + id * s.up_halves) + (size_t)kt * s.RB * kFilterTile * 32 * 128;
-            for (int k = 0; k < c.at.chunks + ranks; ++k) {
+            const char *x = ws_of(c) + (size_t)np * c.s.chunks * kPixelBytes, *t = ws_of(c) + c.at.ranks_at + (size_t)np * s.RB * kRankBytes;
+            const char *w = ws_of(c) + c.at.filters_at + (size_t)kt * c.s.chunks * kFilterTile * 32 * 256;
+            const char *u = reinterpret_cast<const char *>(a.packed + s.up_halves_at + id * s.up_halves) + (size_t)kt * s.RB * kFilterTile * 32 * 128;
+            for (int k = 0; k < c.s.chunks + ranks; ++k) {
                 if (issued >= kStages && !(ok = mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit))) break;
-                const int rb = k - c.at.chunks;
+                const int rb = k - c.s.chunks;
                 // high parts lie in front: without the low ones half of a chunk is enough (32 ranks have both in a row)
                 const uint32_t nx = rb >= 0 ? kRankBytes : kX3 ? kPixelBytes : kPixelBytes / 2, nw = rb >= 0 ? rows * 128 : kX3 ? rows * 256 : rows * 128;
                 if (elect_one()) {
                     const uint32_t to = smem_u32(stages + slot * kStageBytes);
                     mbar_expect_tx(full + slot * 8, nx + nw);
-                    bulk_load(to, rb >= 0 ? t + (size_t)rb * kRankBytes : x + (size_t)k * kPixelBytes, nx, full + slot * 8);
-                    bulk_load(to + kPixelBytes, rb >= 0 ? u + (size_t)rb * rows * 128 : w + (size_t)k * rows * 256, nw, full + slot * 8);
+                    const char *fx = rb >= 0 ? t + (size_t)rb * kRankBytes : x + (size_t)k * kPixelBytes, *fw = rb >= 0 ? u + (size_t)rb * rows * 128 : w + (size_t)k * rows * 256;
+                    for (uint32_t e = 0; e < nx; e += 8192) bulk_load(to + e, fx + e, min(8192u, nx - e), full + slot * 8);
+                    for (uint32_t e = 0; e < nw; e += 8192) bulk_load(to + kPixelBytes + e, fw + e, min(8192u, nw - e), full + slot * 8);
                 }
                 __syncwarp();
                 ++issued;
@@ -261,25 +322,25 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
             const int np = i / c.at.filter_tiles, rows = tile_rows(c, i % c.at.filter_tiles), ranks = ranks_of(np);
             const uint32_t desc = f16_desc(rows), d = tmem + buffer * 256;
             if (turn >= 2 && !(ok = mbar_wait_uniform(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
-            for (int k = 0; k < c.at.chunks + ranks; ++k) {
+            for (int k = 0; k < c.s.chunks + ranks; ++k) {
                 if (!(ok = mbar_wait_uniform(full + slot * 8, phase, stop, c.status, c.limit))) break;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
-                    if (k < c.at.chunks) {
+                    if (k < c.s.chunks) {
 #pragma unroll
                         for (int term = kX3 ? 0 : 2; term < 3; ++term)           // small terms first
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 mma_f16(d, x + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), w + e * 2 + (term == 1 ? rows * 8 : 0), desc, k > 0 || e > 0 || term > (kX3 ? 0 : 2));
                     } else {
-                        const int steps = (min(s.R - (k - c.at.chunks) * 32, 32) + 15) / 16;
+                        const int steps = (min(s.R - (k - c.s.chunks) * 32, 32) + 15) / 16;
 #pragma unroll
                         for (int term = kX3 ? 0 : 2; term < 3; ++term)
                             for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, 1);
                     }
                     mma_commit(empty + slot * 8);
-                    if (k == c.at.chunks + ranks - 1) mma_commit(done + buffer * 8);
+                    if (k == c.s.chunks + ranks - 1) mma_commit(done + buffer * 8);
                 }
                 __syncwarp();
                 if (++slot == kStages) { slot = 0; phase ^= 1; }
@@ -307,21 +368,30 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                 const int k0 = (kt * kFilterTile + b) * 32;
                 if (p < a.HW) {
                     float *out = a.out + (((size_t)n * s.KB + k0 / 32) * a.HW + p) * 32;
+                    if (k0 + 32 <= s.K && a.bias)
 #pragma unroll
-                    for (int u = 0; u < 32; u += 8) {
-                        float before[8];
-                        if (a.accumulate) ld_global_v8(out + u, before);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float y = v[u + e] * x_drop * w_drop;
-                            const bool real = k0 + u + e < s.K;
-                            if (a.bias && real) y += a.bias[k0 + u + e];
-                            if (a.accumulate) y += before[e];
-                            if (a.relu) y = y > 0.0f ? y : 0.0f;
-                            v[u + e] = real ? y : 0.0f;
+                        for (int u = 0; u < 32; u += 4) {
+                            const float4 b = *reinterpret_cast<const float4 *>(a.bias + k0 + u);
+                            v[u] = fmaf(v[u] * x_drop, w_drop, b.x); v[u + 1] = fmaf(v[u + 1] * x_drop, w_drop, b.y);
+                            v[u + 2] = fmaf(v[u + 2] * x_drop, w_drop, b.z); v[u + 3] = fmaf(v[u + 3] * x_drop, w_drop, b.w);
                         }
-                        st_global_v8(out + u, v + u);
-                    }
+                    else
+#pragma unroll
+                        for (int u = 0; u < 32; ++u)     // +0 in pad lanes
+                            v[u] = k0 + u < s.K ? fmaf(v[u] * x_drop, w_drop, a.bias ? a.bias[k0 + u] : 0.0f) : 0.0f;
+                    if (a.accumulate)
+#pragma unroll
+                        for (int u = 0; u < 32; u += 8) {
+                            float before[8];
+                            ld_global_v8(out + u, before);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[u + e] += before[e];
+                        }
+                    if (a.relu)
+#pragma unroll
+                        for (int u = 0; u < 32; ++u) v[u] = fmaxf(v[u], 0.0f);
+#pragma unroll
+                    for (int u = 0; u < 32; u += 8) st_global_v8(out + u, v + u);
                 }
             }
             tc_fence_before();
@@ -337,31 +407,48 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// Up as halves; a block an adapter.
-__global__ void __launch_bounds__(kThreads) pack_up_halves_kernel(const float *__restrict__ up, float *__restrict__ packed, int adapters, const AdapterShape s) {
-    __shared__ float most_s[kThreads / 32];
+// Up and Down as halves, a block an adapter each.
+__global__ void __launch_bounds__(kThreads) pack_halves_kernel(const float *__restrict__ down, const float *__restrict__ up, float *__restrict__ packed, const AdapterShape s) {
+    __shared__ float most_s[kThreads / 32], sum_s[kThreads / 32];
     grid_dep_sync();
     grid_dep_trigger();
-    const int a = blockIdx.x;
-    const float *w = up + (size_t)a * s.K * s.R;
-    float most = 0.0f;
-    for (size_t i = threadIdx.x; i < (size_t)s.K * s.R; i += kThreads) most = fmaxf(most, magnitude(w[i]));
+    const int a = blockIdx.x, cols = blockIdx.y ? s.C : s.R;             // of a row: Up is [K][R], Down [R][C]
+    const float *w = blockIdx.y ? down + (size_t)a * s.R * s.C : up + (size_t)a * s.K * s.R;
+    float most = 0.0f, sums = 0.0f;
+    for (size_t i = threadIdx.x; i < (size_t)(blockIdx.y ? s.C : s.K) * s.R; i += kThreads) most = fmaxf(most, magnitude(w[i]));
     const int ex = top_exponent(block_max(most, most_s));
     const float by = lift(ex);
-    if (threadIdx.x == 0) reinterpret_cast<int *>(packed + s.exponents_at)[a] = ex;
-    char *out = reinterpret_cast<char *>(packed + s.halves_at + a * s.up_halves);
-    for (size_t i = threadIdx.x; i < (size_t)s.KB * 32 * s.RB * 8; i += kThreads) {          // four ranks each
-        const int r = (int)(i & 7) * 4, rb = (int)(i / 8 % s.RB), k = (int)(i / 8 / s.RB), kt = k / (kFilterTile * 32);
-        const int rows = min(kFilterTile, s.KB - kt * kFilterTile) * 32, row = k % (kFilterTile * 32);
+    if (blockIdx.y) {
+        for (int r = threadIdx.x >> 5; r < s.R; r += kThreads / 32) {    // a warp a row
+            float sum = 0.0f;
+            for (int ch = threadIdx.x & 31; ch < s.C; ch += 32) sum += magnitude(w[(size_t)r * s.C + ch]);
+#pragma unroll
+            for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+            sums = fmaxf(sums, sum);
+        }
+        sums = block_max(sums, sum_s);
+    }
+    if (threadIdx.x == 0) {
+        float *info = packed + s.info_at + 4 * (size_t)a;
+        info[blockIdx.y] = __int_as_float(ex);
+        if (blockIdx.y) info[2] = sums;
+    }
+    char *out = reinterpret_cast<char *>(blockIdx.y ? packed + s.down_halves_at + a * s.down_halves : packed + s.up_halves_at + a * s.up_halves);
+    // four columns at a time; a row of 128 bytes holds 64 channels' high (or low) halves, or both of 32 ranks
+    const int wide = blockIdx.y ? 64 : 32, runs = blockIdx.y ? s.chunks : s.RB, all = blockIdx.y ? s.RQ : s.KB * 32;
+    for (size_t i = threadIdx.x; i < (size_t)all * runs * (wide / 4); i += kThreads) {
+        const int e = (int)(i % (wide / 4)) * 4, run = (int)(i / (wide / 4) % runs), r = (int)(i / (wide / 4) / runs);
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = k < s.K && rb * 32 + r + e < s.R ? w[(size_t)k * s.R + rb * 32 + r + e] * by : 0.0f;
+        for (int u = 0; u < 4; ++u) v[u] = r < (blockIdx.y ? s.R : s.K) && run * wide + e + u < cols ? w[(size_t)r * cols + run * wide + e + u] * by : 0.0f;
         uint2 hi, lo;
         split_finite(v[0], v[1], hi.x, lo.x);
         split_finite(v[2], v[3], hi.y, lo.y);
-        char *to = out + ((size_t)kt * s.RB * kFilterTile * 32 + (size_t)rb * rows) * 128;
-        *reinterpret_cast<uint2 *>(to + chunk_at(row, r, rows) + (r & 4) * 2) = hi;
-        *reinterpret_cast<uint2 *>(to + chunk_at(row, 32 + r, rows) + (r & 4) * 2) = lo;
+        const int kt = blockIdx.y ? 0 : r / (kFilterTile * 32), row = blockIdx.y ? r : r % (kFilterTile * 32);
+        const int rows = blockIdx.y ? s.RQ : min(kFilterTile, s.KB - kt * kFilterTile) * 32;
+        char *to = blockIdx.y ? out + (size_t)run * rows * 256 : out + ((size_t)kt * s.RB * kFilterTile * 32 + (size_t)run * rows) * 128;
+        *reinterpret_cast<uint2 *>(to + chunk_at(row, e, rows) + (e & 4) * 2) = hi;
+        *reinterpret_cast<uint2 *>(to + chunk_at(row, wide + e, rows) + (e & 4) * 2) = lo;
     }
 }
 
@@ -375,19 +462,19 @@ bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms) {
 
 size_t adapted_tc_workspace(int N, int C, int K, int HW, int R) { return Layout(N, C, K, HW, R).bytes; }
 
-int launch_pack_up_halves(small_ctx *ctx, const float *up, float *packed, int adapters, const AdapterShape &s, cudaStream_t st) {
-    launch_kernel(ctx, pack_up_halves_kernel, dim3((unsigned)adapters), dim3(kThreads), 0, st, up, packed, adapters, s);
+int launch_pack_halves(small_ctx *ctx, const float *down, const float *up, float *packed, int adapters, const AdapterShape &s, cudaStream_t st) {
+    launch_kernel(ctx, pack_halves_kernel, dim3((unsigned)adapters, 2), dim3(kThreads), 0, st, down, up, packed, s);
     return check_launch(ctx);
 }
 
 int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s, bool x3, cudaStream_t st) {
     const TcArgs c{a, s, Layout(a.N, s.C, s.K, a.HW, s.R), ctx->dev_status, ctx->wait_iters};
-    launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads), kCluster, 0, st, c);
+    launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads * kTeams), kCluster, 0, st, c);
     if (int e = check_launch(ctx)) return e;
     static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
-    const size_t t = sizeof(float) * kTile * (s.RB * 32 + 4), stages = 1024 + (size_t)kStages * kStageBytes;
-    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, sizeof(float) * kTile * (128 + 4))) return e;
-    launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), t, st, c);
+    const size_t passing = 1024 + 2 * (size_t)kPixelBytes + 2 * (size_t)s.RQ * 256, stages = 1024 + (size_t)kStages * kStageBytes;
+    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + 2 * kPixelBytes + 2 * 128 * 256)) return e;
+    launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), passing, st, c);
     if (int e = check_launch(ctx)) return e;
     const int work = a.N * c.at.tiles * c.at.filter_tiles;
     const dim3 grid((unsigned)(work < ctx->sm_count ? work : ctx->sm_count));
