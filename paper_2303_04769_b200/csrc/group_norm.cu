@@ -21,33 +21,47 @@ struct NormArgs {
     float *out, *stats;                 // stats: [N][units][splits][kMaxGroups][2], of the form in two kernels
     int C, CB, cpg, HW;                 // channels, channel blocks, channels of a group, pixels
     int unit_blocks, units;             // channel blocks of a unit (the last one's may be fewer), units of an image
-    int splits;                         // thread blocks that share a unit's pixels
+    int splits, part;                   // thread blocks that share a unit's pixels, pixels of each (the last ones' may be fewer)
     int warps_per_block;                // warps that share a channel block
-    float eps;
-    unsigned act;
+    int fold;                           // 1 << fold channels of a group where those are lanes of a warp, else -1
+    float eps, over_count;              // 1 / (channels of a group * pixels)
 };
 
-__device__ __forceinline__ float activate(float y, unsigned act) {
-    if (act == SMALL_RELU) return y > 0.0f ? y : 0.0f;
-    if (act == SMALL_SILU) return __fdividef(y, 1.0f + __expf(-y));      // exp to inf: -0, as the limit has it
+template <unsigned kAct>
+__device__ __forceinline__ float activate(float y) {
+    if (kAct == SMALL_RELU) return y > 0.0f ? y : 0.0f;
+    if (kAct == SMALL_SILU) return __fdividef(y, 1.0f + __expf(-y));     // exp to inf: -0, as the limit has it
     return y;
+}
+template <unsigned kAct>
+__device__ __forceinline__ float4 normalise(float4 v, float4 m, float4 s, float4 t) {
+    return make_float4(activate<kAct>(fmaf(v.x - m.x, s.x, t.x)), activate<kAct>(fmaf(v.y - m.y, s.y, t.y)), activate<kAct>(fmaf(v.z - m.z, s.z, t.z)),
+                       activate<kAct>(fmaf(v.w - m.w, s.w, t.w)));
+}
+__device__ __forceinline__ float4 clear_pad(float4 v, int c, int channels) {         // pad lanes: +0 whatever lies there
+    if (c + 4 <= channels) return v;
+    return make_float4(c < channels ? v.x : 0.0f, c + 1 < channels ? v.y : 0.0f, c + 2 < channels ? v.z : 0.0f, 0.0f);
+}
+// 1 / sqrt(x): the approximation and one step of Newton's.
+__device__ __forceinline__ float over_sqrt(float x) {
+    const float r = rsqrtf(x);
+    return r * fmaf(-0.5f * x * r, r, 1.5f);
 }
 
 // The unit of this thread block and the part of its pixels that the block holds.
 struct Part {
     int n, unit, split, b0, blocks, c0, channels, groups, p0, pixels;
-    __device__ Part(const NormArgs &a, int block) {
-        split = block % a.splits;
-        const int u = block / a.splits;
-        unit = u % a.units;
-        n = u / a.units;
+    __device__ Part(const NormArgs &a, int block, int y) {
+        n = a.splits == 1 ? block : block / a.splits;
+        split = block - n * a.splits;
+        unit = y;
         b0 = unit * a.unit_blocks;
         blocks = min(a.unit_blocks, a.CB - b0);
         c0 = b0 * 32;
         channels = min(blocks * 32, a.C - c0);
-        groups = channels / a.cpg;
-        p0 = (int)((long long)a.HW * split / a.splits);
-        pixels = (int)((long long)a.HW * (split + 1) / a.splits) - p0;
+        groups = a.fold >= 0 ? channels >> a.fold : channels / a.cpg;
+        p0 = min(a.HW, split * a.part);
+        pixels = min(a.HW - p0, a.part);
     }
 };
 
@@ -59,6 +73,7 @@ __device__ __forceinline__ void channel_sums(const Part &p, int wpb, const float
         const int b = i / wpb, share = i % wpb;
         const float4 *x = tile + (size_t)b * p.pixels * 8 + j;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
         for (int q = share * 4 + (lane >> 3); q < p.pixels; q += wpb * 4) {
             const float4 v = f(x[(size_t)q * 8], b * 32 + j * 4);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -72,37 +87,71 @@ __device__ __forceinline__ void channel_sums(const Part &p, int wpb, const float
     }
 }
 
-// Sums by channel -> sums by group, a warp for each group.
-__device__ __forceinline__ void group_sums(const Part &p, int cpg, int wpb, const float *sums, float *out) {
-    const int lane = threadIdx.x & 31;
-    for (int g = threadIdx.x >> 5; g < p.groups; g += kWarps) {
+// Sums by channel and share -> use(channel of the unit, the sum of its group), called by one thread for each channel; groups whose channels are
+// neighbouring lanes need no memory for it.  kCluster: summed over the cluster's blocks too, through `total`, which the others read until the next
+// cluster_wait().  A barrier of the block is behind `sums` already; use() is followed by none.
+template <bool kCluster, typename U>
+__device__ __forceinline__ void group_sums(const NormArgs &a, const Part &p, const float *sums, float *total, U use) {
+    const int lane = threadIdx.x & 31, wpb = a.warps_per_block, channels = p.blocks * 32;
+    if (a.fold >= 0 && (!kCluster || a.splits == 1)) {
+        for (int c = threadIdx.x; c < channels; c += kThreads) {
+            float s = 0.0f;
+#pragma unroll
+            for (int share = 0; share < kWarps; ++share) s += share < wpb ? sums[share * channels + c] : 0.0f;
+            for (int o = 1; o < 1 << a.fold; o *= 2) s += __shfl_xor_sync(~0u, s, o);
+            use(c, s);
+        }
+        return;
+    }
+    for (int g = threadIdx.x >> 5; g < p.groups; g += kWarps) {          // a warp a group
         float s = 0.0f;
-        for (int share = 0; share < wpb; ++share)
-            for (int c = lane; c < cpg; c += 32) s += sums[share * p.blocks * 32 + g * cpg + c];
+        for (int c = lane; c < a.cpg; c += 32) {
+            float t = 0.0f;
+#pragma unroll
+            for (int share = 0; share < kWarps; ++share) t += share < wpb ? sums[share * channels + g * a.cpg + c] : 0.0f;
+            s += t;
+        }
 #pragma unroll
         for (int o = 16; o; o /= 2) s += __shfl_xor_sync(~0u, s, o);
-        if (lane == 0) out[g] = s;
+        if (lane == 0) total[g] = s;
+    }
+    if (kCluster && a.splits > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+    for (int c = threadIdx.x; c < channels; c += kThreads) {
+        const int g = a.fold >= 0 ? c >> a.fold : c / a.cpg;
+        float s = 0.0f;
+        if (g < p.groups) {
+            if (kCluster && a.splits > 1) {
+                float part[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) part[r] = r < a.splits ? cluster_read(total + g, r) : 0.0f;         // all on their way at once
+#pragma unroll
+                for (int r = 0; r < 8; ++r) s += part[r];
+            } else {
+                s = total[g];
+            }
+        }
+        use(c, s);
     }
 }
 
 // kApply: a cluster holds the whole unit and writes the result; else a block writes its part's mean and deviations by group.
-template <bool kApply>
+template <bool kApply, unsigned kAct>
 __global__ void __launch_bounds__(kThreads) group_norm_kernel(const NormArgs a) {
     extern __shared__ float4 tile[];                     // [blocks][pixels][8]
-    __shared__ float total[kMaxGroups], dev[kMaxGroups], mean_s[kMaxGroups], rstd_s[kMaxGroups];
+    __shared__ float total[kMaxGroups], dev[kMaxGroups];
     grid_dep_sync();
-    const Part p(a, blockIdx.x);
+    const Part p(a, blockIdx.x, blockIdx.y);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & 7, wpb = a.warps_per_block;
     const size_t plane4 = (size_t)a.HW * 8;
     const size_t first4 = ((size_t)p.n * a.CB + p.b0) * plane4 + (size_t)p.p0 * 8;
     const float4 *in = reinterpret_cast<const float4 *>(a.in) + first4;
-    const int most = (a.HW + a.splits - 1) / a.splits;
-    float *sums = reinterpret_cast<float *>(tile + (size_t)a.unit_blocks * most * 8);      // [warps of a block][blocks * 32]
+    float *sums = reinterpret_cast<float *>(tile + (size_t)a.unit_blocks * a.part * 8);      // [warps of a block][blocks * 32]
     float *cmean = sums + wpb * a.unit_blocks * 32, *cscale = cmean + a.unit_blocks * 32, *cshift = cscale + a.unit_blocks * 32;
 
     // each warp copies what it sums, so that its own wait is enough
     for (int i = warp; i < p.blocks * wpb; i += kWarps) {
         const int b = i / wpb, share = i % wpb;
+#pragma unroll 4
         for (int q = share * 4 + (lane >> 3); q < p.pixels; q += wpb * 4)
             copy16_async(tile + ((size_t)b * p.pixels + q) * 8 + j, in + (size_t)b * plane4 + (size_t)q * 8 + j);
     }
@@ -117,19 +166,8 @@ __global__ void __launch_bounds__(kThreads) group_norm_kernel(const NormArgs a) 
     __syncwarp();
     channel_sums(p, wpb, tile, sums, [](float4 v, int) { return v; });
     __syncthreads();
-    group_sums(p, a.cpg, wpb, sums, total);
-    if (kApply) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-
-    if (threadIdx.x < p.groups) {
-        float s = 0.0f;
-        if (kApply)
-            for (int r = 0; r < a.splits; ++r) s += cluster_read(total + threadIdx.x, r);
-        else
-            s = total[threadIdx.x];
-        mean_s[threadIdx.x] = s / ((float)a.cpg * (float)(kApply ? a.HW : p.pixels));
-    }
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.blocks * 32; c += kThreads) cmean[c] = c < p.channels ? mean_s[c / a.cpg] : 0.0f;
+    const float over = kApply ? a.over_count : 1.0f / ((float)a.cpg * (float)p.pixels);
+    group_sums<kApply>(a, p, sums, total, [&](int c, float s) { cmean[c] = s * over; });
     __syncthreads();
     channel_sums(p, wpb, tile, sums, [&](float4 v, int c) {
         const float4 m = *reinterpret_cast<const float4 *>(cmean + c);
@@ -137,69 +175,66 @@ __global__ void __launch_bounds__(kThreads) group_norm_kernel(const NormArgs a) 
         return make_float4(v.x * v.x, v.y * v.y, v.z * v.z, v.w * v.w);
     });
     __syncthreads();
-    group_sums(p, a.cpg, wpb, sums, dev);
     if (!kApply) {
-        __syncthreads();
-        if (threadIdx.x < p.groups) {
-            float *s = a.stats + ((size_t)blockIdx.x * kMaxGroups + threadIdx.x) * 2;
-            s[0] = mean_s[threadIdx.x];
-            s[1] = dev[threadIdx.x];
-        }
+        float *stats = a.stats + (((size_t)p.n * a.units + p.unit) * a.splits + p.split) * kMaxGroups * 2;
+        group_sums<false>(a, p, sums, dev, [&](int c, float s) {
+            const int g = a.fold >= 0 ? c >> a.fold : c / a.cpg;
+            if (c >= p.channels || c != g * a.cpg) return;               // the group's first channel
+            stats[g * 2] = cmean[c];
+            stats[g * 2 + 1] = s;
+        });
         return;
     }
-    cluster_arrive();
-    cluster_wait();
-    if (threadIdx.x < p.groups) {
-        float s = 0.0f;
-        for (int r = 0; r < a.splits; ++r) s += cluster_read(dev + threadIdx.x, r);
-        rstd_s[threadIdx.x] = 1.0f / sqrtf(s / ((float)a.cpg * (float)a.HW) + a.eps);
-    }
-    cluster_arrive();                                    // the others' sums are read: waited for before the block ends
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.channels; c += kThreads) cscale[c] *= rstd_s[c / a.cpg];
+    group_sums<true>(a, p, sums, dev, [&](int c, float s) { cscale[c] *= over_sqrt(fmaf(s, over, a.eps)); });
+    if (a.splits > 1) cluster_arrive();                  // the others' sums are read: waited for before the block ends
     __syncthreads();
     float4 *out = reinterpret_cast<float4 *>(a.out) + first4;
     for (int i = warp; i < p.blocks * wpb; i += kWarps) {
         const int b = i / wpb, share = i % wpb, c = b * 32 + j * 4;
         const float4 m = *reinterpret_cast<const float4 *>(cmean + c), s = *reinterpret_cast<const float4 *>(cscale + c),
                      t = *reinterpret_cast<const float4 *>(cshift + c);
-        for (int q = share * 4 + (lane >> 3); q < p.pixels; q += wpb * 4) {
-            float4 v = tile[((size_t)b * p.pixels + q) * 8 + j];
-            v.x = activate(fmaf(v.x - m.x, s.x, t.x), a.act); v.y = activate(fmaf(v.y - m.y, s.y, t.y), a.act);
-            v.z = activate(fmaf(v.z - m.z, s.z, t.z), a.act); v.w = activate(fmaf(v.w - m.w, s.w, t.w), a.act);
-            if (c + 4 > p.channels) {                    // pad lanes: +0 whatever lies there
-                if (c + 0 >= p.channels) v.x = 0.0f;
-                if (c + 1 >= p.channels) v.y = 0.0f;
-                if (c + 2 >= p.channels) v.z = 0.0f;
-                v.w = 0.0f;
-            }
-            __stcs(out + (size_t)b * plane4 + (size_t)q * 8 + j, v);
-        }
+        const float4 *x = tile + (size_t)b * p.pixels * 8 + j;
+        float4 *y = out + (size_t)b * plane4 + j;
+#pragma unroll 4
+        for (int q = share * 4 + (lane >> 3); q < p.pixels; q += wpb * 4) __stcs(y + (size_t)q * 8, clear_pad(normalise<kAct>(x[(size_t)q * 8], m, s, t), c, p.channels));
     }
-    cluster_wait();
+    if (a.splits > 1) cluster_wait();
 }
 
 // The second kernel: merges the parts' statistics (count-weighted means; deviations plus those of the means) and normalises.
+template <unsigned kAct>
 __global__ void __launch_bounds__(kThreads) group_norm_apply_kernel(const NormArgs a) {
     extern __shared__ float4 tile[];
     __shared__ float mean_s[kMaxGroups], rstd_s[kMaxGroups];
     grid_dep_sync();
     grid_dep_trigger();
-    const Part p(a, gridDim.x - 1 - blockIdx.x);         // what the first kernel read last is the likeliest to be in L2
+    const Part p(a, gridDim.x - 1 - blockIdx.x, gridDim.y - 1 - blockIdx.y);         // what the first kernel read last is the likeliest to be in L2
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = lane & 7, wpb = a.warps_per_block;
     float *cmean = reinterpret_cast<float *>(tile), *cscale = cmean + a.unit_blocks * 32, *cshift = cscale + a.unit_blocks * 32;
-    if (threadIdx.x < p.groups) {
-        const float *s = a.stats + ((size_t)((size_t)p.n * a.units + p.unit) * a.splits * kMaxGroups + threadIdx.x) * 2;
-        float mean = s[0], dev = s[1], count = (float)(int)((long long)a.HW / a.splits);
-        for (int r = 1; r < a.splits; ++r) {
-            const float n = (float)((int)((long long)a.HW * (r + 1) / a.splits) - (int)((long long)a.HW * r / a.splits));
-            const float m = s[(size_t)r * kMaxGroups * 2], d = m - mean, all = count + n;
-            dev += s[(size_t)r * kMaxGroups * 2 + 1] + d * d * (count * n / all) * (float)a.cpg;
-            mean += d * (n / all);
+    // a warp a group, a lane the parts l, l + 32, ...; then the lanes' parts two by two
+    for (int g = warp; g < p.groups; g += kWarps) {
+        const float2 *s = reinterpret_cast<const float2 *>(a.stats) + ((size_t)p.n * a.units + p.unit) * a.splits * kMaxGroups + g;
+        float mean = 0.0f, dev = 0.0f, count = 0.0f;
+        auto join = [&](float m, float d2, float n) {
+            if (n == 0.0f) return;
+            const float d = m - mean, all = count + n, share = n / all;
+            dev += d2 + d * d * (count * share) * (float)a.cpg;
+            mean += d * share;
             count = all;
+        };
+        for (int r = lane; r < a.splits; r += 32) {
+            const float2 v = s[(size_t)r * kMaxGroups];
+            join(v.x, v.y, (float)min(a.HW - r * a.part, a.part));
         }
-        mean_s[threadIdx.x] = mean;
-        rstd_s[threadIdx.x] = 1.0f / sqrtf(dev / ((float)a.cpg * (float)a.HW) + a.eps);
+#pragma unroll
+        for (int o = 16; o; o /= 2) {
+            const float m = __shfl_down_sync(~0u, mean, o), d2 = __shfl_down_sync(~0u, dev, o), n = __shfl_down_sync(~0u, count, o);
+            if (lane < o) join(m, d2, n);
+        }
+        if (lane == 0) {
+            mean_s[g] = mean;
+            rstd_s[g] = over_sqrt(fmaf(dev, a.over_count, a.eps));
+        }
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.blocks * 32; c += kThreads) {
@@ -226,19 +261,8 @@ __global__ void __launch_bounds__(kThreads) group_norm_apply_kernel(const NormAr
             for (int u = 0; u < kAhead; ++u)
                 if (q + u * wpb * 4 < p.pixels) v[u] = __ldcs(x + (size_t)(q + u * wpb * 4) * 8);
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                if (q + u * wpb * 4 >= p.pixels) break;
-                float4 r;
-                r.x = activate(fmaf(v[u].x - m.x, s.x, t.x), a.act); r.y = activate(fmaf(v[u].y - m.y, s.y, t.y), a.act);
-                r.z = activate(fmaf(v[u].z - m.z, s.z, t.z), a.act); r.w = activate(fmaf(v[u].w - m.w, s.w, t.w), a.act);
-                if (c + 4 > p.channels) {
-                    if (c + 0 >= p.channels) r.x = 0.0f;
-                    if (c + 1 >= p.channels) r.y = 0.0f;
-                    if (c + 2 >= p.channels) r.z = 0.0f;
-                    r.w = 0.0f;
-                }
-                __stcs(y + (size_t)(q + u * wpb * 4) * 8, r);
-            }
+            for (int u = 0; u < kAhead; ++u)
+                if (q + u * wpb * 4 < p.pixels) __stcs(y + (size_t)(q + u * wpb * 4) * 8, clear_pad(normalise<kAct>(v[u], m, s, t), c, p.channels));
         }
     }
 }
@@ -251,7 +275,9 @@ struct NormPlan {
 
 int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
 
-constexpr size_t kBlockBytes = 104u << 10;        // shared memory where two blocks share an SM
+// Shared memory of a block: a unit that leaves room for two blocks on an SM stays whole (28 x 28, 100 KB: 12.7 us, as two halves 14.1), a larger
+// one is cut until three share one (56 x 56, 400 KB, batch 128, 256 channels: 181 us in eighths or in parts of 70 KB, 208 in quarters).
+constexpr size_t kBlockBytes = 104u << 10, kSplitBytes = 70u << 10;
 constexpr size_t kMostBytes = 220u << 10;         // at all
 
 size_t block_bytes(const NormPlan &p, int HW) {   // the tile, the sums of channels, their means, scales and shifts
@@ -267,7 +293,8 @@ NormPlan plan_norm(int N, int C, int HW, int groups) {
     p.warps_per_block = p.unit_blocks < kWarps ? kWarps / p.unit_blocks : 1;
     const size_t bytes = (size_t)p.unit_blocks * HW * 128;
     p.splits = 1;
-    while (p.splits < 8 && block_bytes(p, HW) > kBlockBytes) p.splits *= 2;
+    if (block_bytes(p, HW) > kBlockBytes)
+        while (p.splits < 8 && block_bytes(p, HW) > kSplitBytes) p.splits *= 2;
     p.on_chip = block_bytes(p, HW) <= kMostBytes;
     if (p.on_chip) {
         // few units: more blocks, down to 16 KB each
@@ -275,9 +302,28 @@ NormPlan plan_norm(int N, int C, int HW, int groups) {
     } else {
         p.splits = (int)((bytes + kBlockBytes / 2 - 1) / (kBlockBytes / 2));
         if (p.splits > HW) p.splits = HW;
+        p.splits = ceil_div(HW, ceil_div(HW, p.splits));         // none without a pixel
     }
     p.smem = block_bytes(p, HW);
     return p;
+}
+
+template <unsigned kAct>
+int launch_norm(small_ctx *ctx, const NormArgs &a, const NormPlan &p, int N, cudaStream_t st) {
+    static std::atomic<unsigned long long> whole{0}, part{0};
+    const size_t most = ctx->max_smem_optin - 2048;
+    const dim3 grid((unsigned)(N * p.splits), (unsigned)p.units), block(kThreads);
+    if (p.on_chip) {
+        if (int s = allow_shared_memory(ctx, group_norm_kernel<true, kAct>, whole, most)) return s;
+        if (p.splits > 1) launch_clusters(ctx, group_norm_kernel<true, kAct>, grid, block, p.splits, p.smem, st, a);
+        else launch_kernel(ctx, group_norm_kernel<true, kAct>, grid, block, p.smem, st, a);
+        return check_launch(ctx);
+    }
+    if (int s = allow_shared_memory(ctx, group_norm_kernel<false, 0>, part, most)) return s;
+    launch_kernel(ctx, group_norm_kernel<false, 0>, grid, block, p.smem, st, a);
+    if (int s = check_launch(ctx)) return s;
+    launch_kernel(ctx, group_norm_apply_kernel<kAct>, grid, block, 3 * (size_t)p.unit_blocks * 128, st, a);
+    return check_launch(ctx);
 }
 
 bool norm_shape_ok(int N, int C, int H, int W, int groups) {
@@ -306,7 +352,7 @@ SMALL_API int small_group_norm(small_ctx *ctx, const float *in, const float *gam
     if (!norm_shape_ok(N, C, H, W, groups)) return SMALL_ERR_SHAPE;
     const NormPlan p = plan_norm(N, C, H * W, groups);
     const long long blocks = (long long)N * p.units * p.splits;
-    if (blocks > 0x7fffffffLL) return SMALL_ERR_SHAPE;
+    if (blocks > 0x7fffffffLL || p.units > 65535) return SMALL_ERR_SHAPE;
     const size_t bytes = sizeof(float) * packed_elems(N, C, H, W), ws = small_group_norm_workspace_bytes(N, C, H, W, groups);
     if (in != out && ranges_overlap(in, bytes, out, bytes)) return SMALL_ERR_OVERLAP;
     for (const float *q : {gamma, beta})
@@ -319,20 +365,10 @@ SMALL_API int small_group_norm(small_ctx *ctx, const float *in, const float *gam
     }
     const OnDevice on(ctx);
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
-    const NormArgs a{in, gamma, beta, out, static_cast<float *>(workspace), C, blocks_of(C), C / groups, H * W,
-                     p.unit_blocks, p.units, p.splits, p.warps_per_block, eps, flags};
+    const int cpg = C / groups, part = ceil_div(H * W, p.splits);
+    const NormArgs a{in, gamma, beta, out, static_cast<float *>(workspace), C, blocks_of(C), cpg, H * W, p.unit_blocks, p.units, p.splits, part, p.warps_per_block,
+                     cpg <= 32 && (cpg & (cpg - 1)) == 0 ? __builtin_ctz(cpg) : -1, eps, (float)(1.0 / ((double)cpg * H * W))};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    static std::atomic<unsigned long long> whole{0}, part{0};
-    const size_t most = ctx->max_smem_optin - 2048;              // the kernels have static shared memory too
-    if (p.smem > most) return SMALL_ERR_UNSUPPORTED;
-    if (p.on_chip) {
-        if (int s = allow_shared_memory(ctx, group_norm_kernel<true>, whole, most)) return s;
-        launch_clusters(ctx, group_norm_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), p.splits, p.smem, st, a);
-        return check_launch(ctx);
-    }
-    if (int s = allow_shared_memory(ctx, group_norm_kernel<false>, part, most)) return s;
-    launch_kernel(ctx, group_norm_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), p.smem, st, a);
-    if (int s = check_launch(ctx)) return s;
-    launch_kernel(ctx, group_norm_apply_kernel, dim3((unsigned)blocks), dim3(kThreads), 3 * (size_t)p.unit_blocks * 128, st, a);
-    return check_launch(ctx);
+    if (p.smem > ctx->max_smem_optin - 2048) return SMALL_ERR_UNSUPPORTED;           // the kernels have static shared memory too
+    return flags == SMALL_RELU ? launch_norm<SMALL_RELU>(ctx, a, p, N, st) : flags == SMALL_SILU ? launch_norm<SMALL_SILU>(ctx, a, p, N, st) : launch_norm<0>(ctx, a, p, N, st);
 }
