@@ -25,13 +25,14 @@ using namespace halves;
 
 constexpr float kLift = 14.0f;           // weights are scaled by 2^14
 
-// Workspace: [N][kv_heads][tiles]{keys: DP * 512 bytes, values: DP * 512 bytes}; int[N][tiles][128], the keys' places in the bias table
-// (of_key); float[N][kv_heads][tiles][2], how to undo the scaling.
+// Workspace: [N][kv_heads][tiles]{keys: DP * 512 bytes, values: DP * 512 bytes}; int[N][tiles][128 + 16], the keys' places in the bias table
+// (of_key), and of each eight keys the last one's if they are neighbours there, else -1; float[N][kv_heads][tiles][2], how to undo the scaling.
+constexpr int kRun = 8, kPlaceInts = kTile + kTile / kRun;
 __device__ __forceinline__ int *key_places(const AttnArgs &a, int tiles, int tile_bytes) {
     return reinterpret_cast<int *>(static_cast<char *>(a.ws) + (size_t)a.N * a.kv_heads * tiles * 2 * tile_bytes);
 }
 __device__ __forceinline__ float *undo_scaling(const AttnArgs &a, int tiles, int tile_bytes) {
-    return reinterpret_cast<float *>(key_places(a, tiles, tile_bytes) + (size_t)a.N * tiles * kTile);
+    return reinterpret_cast<float *>(key_places(a, tiles, tile_bytes) + (size_t)a.N * tiles * kPlaceInts);
 }
 template <int DP>
 __global__ void __launch_bounds__(256) attention_tiles_kernel(const AttnArgs a, int tiles) {
@@ -82,7 +83,10 @@ __global__ void __launch_bounds__(256) attention_tiles_kernel(const AttnArgs a, 
     if (!is_v) {
         if (hk == 0 && threadIdx.x < kTile) {
             const int j = t * kTile + threadIdx.x;
-            key_places(a, tiles, kBytes)[((size_t)n * tiles + t) * kTile + threadIdx.x] = j < keys ? of_key(a, j / e.y, j % e.y) : 0;
+            int *places = key_places(a, tiles, kBytes) + ((size_t)n * tiles + t) * kPlaceInts;
+            const int place = j < keys ? of_key(a, j / e.y, j % e.y) : 0, first_of = __shfl_sync(~0u, place, threadIdx.x & 24);
+            places[threadIdx.x] = place;
+            if (threadIdx.x % kRun == kRun - 1) places[kTile + threadIdx.x / kRun] = place - first_of == kRun - 1 ? place : -1;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -168,6 +172,26 @@ __device__ __forceinline__ void tmem_ld_wait(float (&v)[32]) {
         :: "memory");
 }
 
+// v = cap * tanh(v * over_cap), as `capped` in attention.cuh: both quotients with the argument's sign, one reciprocal.
+__device__ __forceinline__ void capped(float &v0, float &v1, float cap, float over_cap) {
+    const uint64_t t = fma2(pair(v0, v1), pair(over_cap, over_cap), 0), s = fma2(t, t, 0);
+    const uint64_t num = fma2(t, fma2(s, add2(s, pair(105.0f, 105.0f)), pair(945.0f, 945.0f)), 0);
+    const uint64_t den = fma2(s, fma2(s, pair(15.0f, 15.0f), pair(420.0f, 420.0f)), pair(945.0f, 945.0f));
+    float a0, a1, s0, s1, n0, n1, d0, d1, p0, p1, q0, q1;
+    unpair(fma2(t, pair(2.0f * kLog2e, 2.0f * kLog2e), 0), a0, a1);
+    const uint64_t e = pair(exp2_fast(fminf(a0, 64.0f)), exp2_fast(fminf(a1, 64.0f)));
+    unpair(s, s0, s1);
+    unpair(num, n0, n1);
+    unpair(den, d0, d1);
+    unpair(add2(e, pair(-1.0f, -1.0f)), p0, p1);
+    unpair(add2(e, pair(1.0f, 1.0f)), q0, q1);
+    const bool far0 = s0 >= 0.25f, far1 = s1 >= 0.25f;               // (a NaN goes with the near ones, and through)
+    float r0, r1;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(far0 ? q0 : d0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(far1 ? q1 : d1));
+    unpair(fma2(fma2(pair(far0 ? p0 : n0, far1 ? p1 : n1), pair(r0, r1), 0), pair(cap, cap), 0), v0, v1);
+}
+
 constexpr int kMaxRing = 4;
 constexpr int kPlaces = 8;               // tiles: one is used no longer when the keys of the eighth behind it are asked for
 // Threads of a row: one has registers for 64 sums and for scores under way; the table's reads want twice as many warps to hide behind.
@@ -194,7 +218,7 @@ struct Shared {
     int gave_up;
     float exchange[2][2][2][kTile];                      // [parity of the key tile][query tile][half of the keys][row]: maxima; at last sums
     float q_drop[2][kTile];
-    alignas(16) int places[kPlaces][kTile];
+    alignas(16) int places[kPlaces][kPlaceInts];
 };
 
 // kGeneral: scores pass through the cap and the bias table.
@@ -228,7 +252,7 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
     // rows hold both.
     const uint32_t k_bytes = kX3 || DP == 32 ? kBytes : kBytes / 2, v_bytes = kX3 ? kBytes : kBytes / 2;
     const char *from_tiles = static_cast<const char *>(a.ws) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2 * kBytes;
-    const int *from_places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kTile;
+    const int *from_places = key_places(a, c.tiles, kBytes) + (size_t)n * c.tiles * kPlaceInts;
     int issued = 0;                                      // by the loading warp
     auto load = [&](int slot) {
         if (elect_one()) {
@@ -237,8 +261,8 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
             bulk_load(smem_u32(slots + slot * kBytes), from_tiles + (size_t)issued * kBytes, bytes, full + slot * 8);
             if (kGeneral && !(issued & 1)) {
                 const int t = issued >> 1, at = t % kPlaces;
-                mbar_expect_tx(placed + at * 8, kTile * sizeof(int));
-                bulk_load(smem_u32(sh.places[at]), from_places + t * kTile, kTile * sizeof(int), placed + at * 8);
+                mbar_expect_tx(placed + at * 8, kPlaceInts * sizeof(int));
+                bulk_load(smem_u32(sh.places[at]), from_places + t * kPlaceInts, kPlaceInts * sizeof(int), placed + at * 8);
             }
         }
         __syncwarp();
@@ -425,23 +449,22 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
                 if (kGeneral) {
                     if (a.cap > 0.0f)
 #pragma unroll
-                        for (int u = 0; u < 32; ++u) v[u] = capped(v[u], cap2, f * over_cap);
+                        for (int u = 0; u < 32; u += 2) capped(v[u], v[u + 1], cap2, f * over_cap);
                     if (bias) {
                         const float f1 = a.cap > 0.0f ? 1.0f : scale2;
                         const int *place = sh.places[t % kPlaces] + half * kKeys + g;
                         if (c.table_floats) {
+                            const int4 runs = *reinterpret_cast<const int4 *>(sh.places[t % kPlaces] + kTile + (half * kKeys + g) / kRun);
+                            const int run[4] = {runs.x, runs.y, runs.z, runs.w};
 #pragma unroll
-                            for (int u = 0; u < 32; u += 8) {
-                                const int4 k0 = *reinterpret_cast<const int4 *>(place + u), k1 = *reinterpret_cast<const int4 *>(place + u + 4);
-                                if (k1.w - k0.x == 7) {  // one row of the plane: neighbours in the table
-                                    const float *b = at_table - k1.w;
+                            for (int u = 0; u < 32; u += kRun) {
+                                if (run[u / kRun] >= 0) {            // one row of the plane: neighbours in the table
+                                    const float *b = at_table - run[u / kRun];
 #pragma unroll
-                                    for (int w = 0; w < 8; ++w) v[u + w] = fmaf(v[u + w], f1, b[7 - w]);
+                                    for (int w = 0; w < kRun; ++w) v[u + w] = fmaf(v[u + w], f1, b[kRun - 1 - w]);
                                 } else {
-                                    v[u] = fmaf(v[u], f1, at_table[-k0.x]); v[u + 1] = fmaf(v[u + 1], f1, at_table[-k0.y]);
-                                    v[u + 2] = fmaf(v[u + 2], f1, at_table[-k0.z]); v[u + 3] = fmaf(v[u + 3], f1, at_table[-k0.w]);
-                                    v[u + 4] = fmaf(v[u + 4], f1, at_table[-k1.x]); v[u + 5] = fmaf(v[u + 5], f1, at_table[-k1.y]);
-                                    v[u + 6] = fmaf(v[u + 6], f1, at_table[-k1.z]); v[u + 7] = fmaf(v[u + 7], f1, at_table[-k1.w]);
+#pragma unroll
+                                    for (int w = 0; w < kRun; ++w) v[u + w] = fmaf(v[u + w], f1, at_table[-place[u + w]]);
                                 }
                             }
                         } else {
@@ -621,7 +644,8 @@ int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
     if (int s = check_launch(ctx)) return s;
     TcArgs c{a, tiles, 1, kMaxRing, 0, ctx->dev_status, ctx->wait_iters};
     const size_t most = ctx->max_smem_optin - 12288, tile = (size_t)DP * 512;
-    if (DP < 128 && a.QP > kTile) c.q_tiles = 2;
+    // One tile a block where that still fits the SMs (batch 1, 8 heads of 64, 28 x 28: 31.5 -> 24.3 us; batch 4, 4 heads, 32 x 32 47.9 -> 38.8)
+    if (DP < 128 && (long long)a.N * a.heads * ceil_div(a.QP, kTile) > ctx->sm_count) c.q_tiles = 2;
     while (c.ring > 2 && 1024 + (c.q_tiles + c.ring) * tile > most) --c.ring;
     if (a.bias) {
         const int rows = c.q_tiles * kTile, y = (rows + a.QW - 2) / a.QW + 1;        // rows of the plane that such a run of pixels can touch
@@ -647,7 +671,7 @@ int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
 }  // namespace
 
 size_t attention_tc_workspace(int N, int kv_heads, int D, int KP) {
-    return (size_t)N * kv_heads * ceil_div(KP, kTile) * ((size_t)padded(D) * 1024 + 2 * sizeof(float)) + (size_t)N * ceil_div(KP, kTile) * kTile * sizeof(int);
+    return (size_t)N * kv_heads * ceil_div(KP, kTile) * ((size_t)padded(D) * 1024 + 2 * sizeof(float)) + (size_t)N * ceil_div(KP, kTile) * kPlaceInts * sizeof(int);
 }
 
 int launch_attention_tc(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {

@@ -65,6 +65,7 @@ static inline void launch_clusters(small_ctx *ctx, void (*kern)(KArgs...), dim3 
 
 // The other blocks of a cluster: barrier and a float of block `rank`'s shared memory.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }       // orders no memory
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float cluster_read(const float *p, int rank) {
     uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads) group_norm_kernel(const NormArgs a) 
         return;
     }
     group_sums<true>(a, p, sums, dev, [&](int c, float s) { cscale[c] *= over_sqrt(fmaf(s, over, a.eps)); });
-    if (a.splits > 1) cluster_arrive();                  // the others' sums are read: waited for before the block ends
+    if (a.splits > 1) cluster_arrive_relaxed();          // the others' sums are read: waited for before the block ends
     __syncthreads();
     float4 *out = reinterpret_cast<float4 *>(a.out) + first4;
     for (int i = warp; i < p.blocks * wpb; i += kWarps) {
