@@ -359,9 +359,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     } else {
         const int lane = threadIdx.x & 31, half = warp >> 2;
         const float w_drop = drop(exponents(c)[0]);
+        float4 *rows = reinterpret_cast<float4 *>(stages + kStages * kStageBytes) + warp * 256;
         int buffer = 0, phase = 0;
         for (int i = blockIdx.x; i < work; i += gridDim.x) {
-            const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p = np % c.at.tiles * kTile + (warp & 3) * 32 + lane;
+            const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
             const float x_drop = drop(exponents(c)[4 + np]);
             const float grown = w_drop * (1.0f + kCutOff * (float)((kX3 ? 3 : 1) * (s.chunks * (kChunk / 16) + (ranks_of(np) ? (s.R + 15) / 16 : 0))));
             if (!mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit)) break;
@@ -370,34 +371,33 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
             for (int b = half; b < blocks; b += 2) {
                 float v[32];
                 tmem_ld32(tmem + buffer * 256 + b * 32 + ((uint32_t)(warp & 3) << 21), v);
-                const int k0 = (kt * kFilterTile + b) * 32;
-                if (p < a.HW) {
-                    float *out = a.out + (((size_t)n * s.KB + k0 / 32) * a.HW + p) * 32;
-                    if (k0 + 32 <= s.K && a.bias)
+                // through shared memory, so that a store is whole lines: eight lanes a pixel
 #pragma unroll
-                        for (int u = 0; u < 32; u += 4) {
-                            const float4 b = *reinterpret_cast<const float4 *>(a.bias + k0 + u);
-                            v[u] = fmaf(v[u] * x_drop, grown, b.x); v[u + 1] = fmaf(v[u + 1] * x_drop, grown, b.y);
-                            v[u + 2] = fmaf(v[u + 2] * x_drop, grown, b.z); v[u + 3] = fmaf(v[u + 3] * x_drop, grown, b.w);
-                        }
-                    else
-#pragma unroll
-                        for (int u = 0; u < 32; ++u)     // +0 in pad lanes
-                            v[u] = k0 + u < s.K ? fmaf(v[u] * x_drop, grown, a.bias ? a.bias[k0 + u] : 0.0f) : 0.0f;
-                    if (a.accumulate)
-#pragma unroll
-                        for (int u = 0; u < 32; u += 8) {
-                            float before[8];
-                            ld_global_v8(out + u, before);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) v[u + e] += before[e];
-                        }
-                    if (a.relu)
-#pragma unroll
-                        for (int u = 0; u < 32; ++u) v[u] = fmaxf(v[u], 0.0f);
-#pragma unroll
-                    for (int u = 0; u < 32; u += 8) st_global_v8(out + u, v + u);
+                for (int u = 0; u < 8; ++u)
+                    rows[lane * 8 + (u ^ (lane & 7))] = make_float4(v[u * 4] * x_drop, v[u * 4 + 1] * x_drop, v[u * 4 + 2] * x_drop, v[u * 4 + 3] * x_drop);
+                __syncwarp();
+                const int k0 = (kt * kFilterTile + b) * 32 + (lane & 7) * 4;
+                float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (a.bias) {
+                    if (k0 + 4 <= s.K) add = *reinterpret_cast<const float4 *>(a.bias + k0);
+                    else add = make_float4(k0 < s.K ? a.bias[k0] : 0.0f, k0 + 1 < s.K ? a.bias[k0 + 1] : 0.0f, k0 + 2 < s.K ? a.bias[k0 + 2] : 0.0f, 0.0f);
                 }
+                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8 + lane;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int r = u * 4 + (lane >> 3);
+                    float4 y = rows[r * 8 + ((lane & 7) ^ (r & 7))];
+                    y.x = fmaf(y.x, grown, add.x); y.y = fmaf(y.y, grown, add.y); y.z = fmaf(y.z, grown, add.z); y.w = fmaf(y.w, grown, add.w);
+                    if (p0 + r >= a.HW) continue;
+                    if (a.accumulate) {
+                        const float4 before = out[u * 32];
+                        y.x += before.x; y.y += before.y; y.z += before.z; y.w += before.w;
+                    }
+                    if (a.relu) y = make_float4(fmaxf(y.x, 0.0f), fmaxf(y.y, 0.0f), fmaxf(y.z, 0.0f), fmaxf(y.w, 0.0f));
+                    if (k0 + 4 > s.K) y = make_float4(k0 < s.K ? y.x : 0.0f, k0 + 1 < s.K ? y.y : 0.0f, k0 + 2 < s.K ? y.z : 0.0f, 0.0f);       // +0 in pad lanes
+                    out[u * 32] = y;
+                }
+                __syncwarp();
             }
             tc_fence_before();
             mbar_arrive(free + buffer * 8);
@@ -477,7 +477,7 @@ int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s,
     launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads * kTeams), kCluster, 0, st, c);
     if (int e = check_launch(ctx)) return e;
     static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
-    const size_t passing = 1024 + 2 * (size_t)kPixelBytes + 2 * (size_t)s.RQ * 256, stages = 1024 + (size_t)kStages * kStageBytes;
+    const size_t passing = 1024 + 2 * (size_t)kPixelBytes + 2 * (size_t)s.RQ * 256, stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;
     if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + 2 * kPixelBytes + 2 * 128 * 256)) return e;
     launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), passing, st, c);
     if (int e = check_launch(ctx)) return e;
