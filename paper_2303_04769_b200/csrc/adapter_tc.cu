@@ -80,14 +80,17 @@ __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const
     if (blockIdx.x == 0 && threadIdx.x == 0) exponents(c)[0] = ex;
     char *out = ws_of(c) + c.at.filters_at;
     float (*block)[33] = blocks[threadIdx.x / kThreads];
+    auto fetch = [&](int i) {
+        const int kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2);
+        return i < items && cb < c.s.CB ? w[((size_t)kb * c.s.CB + cb) * 256 + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    float4 v = fetch(team);
     for (int i0 = 0; i0 < items; i0 += kCluster * kTeams) {
         const int i = i0 + team, kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2), kt = kb / kFilterTile;
         __syncthreads();
-        if (i < items) {
-            const float4 v = cb < c.s.CB ? w[((size_t)kb * c.s.CB + cb) * 256 + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
-            const int ch = tid >> 3, f0 = (tid & 7) * 4;
-            block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
-        }
+        const int ch = tid >> 3, f0 = (tid & 7) * 4;
+        block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
+        v = fetch(i + kCluster * kTeams);
         __syncthreads();
         if (i >= items) continue;
         const int f = tid >> 3, c0 = (tid & 7) * 4, rows = tile_rows(c, kt), row = kb % kFilterTile * 32 + f, col = (cb & 1) * 32 + c0;
@@ -108,18 +111,18 @@ __device__ __forceinline__ void bulk_store(void *to, uint32_t from, uint32_t byt
 template <int kLeft>
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
 
-__global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArgs c) {
-    extern __shared__ char raw[];                        // two chunks of pixels, two of Down
+__global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArgs c) {
+    extern __shared__ char raw[];                        // a chunk of pixels and one of Down: four blocks a SM hide what each waits for
     __shared__ float most_s[kThreads / 32];
-    __shared__ uint64_t down_s[2], used_s[2];
+    __shared__ uint64_t down_s, used_s;
     __shared__ uint32_t tmem_s;
     __shared__ int gave_up;
     const AdaptArgs &a = c.a;
     const AdapterShape &s = c.s;
     const int n = blockIdx.x / c.at.tiles, pt = blockIdx.x % c.at.tiles, p0 = pt * kTile, pixels = min(kTile, a.HW - p0);
     const int warp = warp_index(), lane = threadIdx.x & 31;
-    char *chunks = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u), *downs = chunks + 2 * kPixelBytes;
-    const uint32_t down_bytes = s.RQ * 256, down = smem_u32(down_s), used = smem_u32(used_s);
+    char *chunk = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u), *down_chunk = chunk + kPixelBytes;
+    const uint32_t down_bytes = s.RQ * 256, down = smem_u32(&down_s), used = smem_u32(&used_s);
     const uint32_t columns = s.RQ <= 32 ? 32 : s.RQ <= 64 ? 64 : 128;
     // What is read here is older than the kernel in front of this one, which has waited for all before itself; its result comes after the wait.
     const float *x = a.in + (size_t)n * s.CB * a.HW * 32 + (size_t)p0 * 32;
@@ -128,28 +131,31 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArg
     const char *halves = reinterpret_cast<const char *>(a.packed + s.down_halves_at + (some ? id : 0) * s.down_halves);
     auto load_down = [&](int k) {
         if (elect_one()) {
-            mbar_expect_tx(down + (k & 1) * 8, down_bytes);
-            bulk_load(smem_u32(downs + (k & 1) * down_bytes), halves + (size_t)k * down_bytes, down_bytes, down + (k & 1) * 8);
+            mbar_expect_tx(down, down_bytes);
+            bulk_load(smem_u32(down_chunk), halves + (size_t)k * down_bytes, down_bytes, down);
         }
         __syncwarp();
     };
     if (warp == 0) {
         if (elect_one()) {
             gave_up = 0;
-            for (int i = 0; i < 2; ++i) { mbar_init(down + i * 8, 1); mbar_init(used + i * 8, 1); }
+            mbar_init(down, 1);
+            mbar_init(used, 1);
             mbar_fence_init();
         }
         __syncwarp();
         if (some) {
             tmem_alloc(smem_u32(&tmem_s), columns);
-            for (int k = 0; k < min(2, s.chunks); ++k) load_down(k);
+            load_down(0);
         }
     }
     float most = 0.0f;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < s.CB * pixels * 8; i += kThreads) {
-        const int cb = i / (pixels * 8), e = i % (pixels * 8);
-        most = fmaxf(most, magnitude(reinterpret_cast<const float4 *>(x + (size_t)cb * a.HW * 32)[e]));
+#pragma unroll 2
+    for (int cb = 0; cb < s.CB; ++cb) {
+        const float4 *line = reinterpret_cast<const float4 *>(x + (size_t)cb * a.HW * 32) + threadIdx.x;
+#pragma unroll
+        for (int e = 0; e < kTile * 8; e += kThreads)
+            if ((int)threadIdx.x + e < pixels * 8) most = fmaxf(most, magnitude(line[e]));
     }
     most = block_max(most, most_s);
     grid_dep_sync();                                     // the filters' exponent
@@ -171,21 +177,11 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArg
     const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
     const uint32_t tmem = tmem_s, desc = f16_desc(s.RQ);
     for (int k = 0; k < s.chunks; ++k) {
-        char *chunk = chunks + (k & 1) * kPixelBytes;
-        if (k >= 2) {                                    // the chunk before the last is out, and its product is done
-            if (warp == 0) {
-                bulk_store_wait<1>();
-                if (some) {
-                    mbar_wait_uniform(used + (k & 1) * 8, (k >> 1) - 1 & 1, &gave_up, c.status, c.limit);
-                    load_down(k);
-                }
-            }
-            __syncthreads();
-        }
+        float4 v2[2][kTile / 32];                        // on its way while the chunk before is written out and multiplied
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const int cb = k * 2 + g, ch = cb * 32 + c0;
-            float4 v[kTile / 32];
+            float4 (&v)[kTile / 32] = v2[g];
 #pragma unroll
             for (int i = 0; i < kTile / 32; ++i) {
                 const int r = r0 + i * 32;
@@ -197,32 +193,42 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArg
                     v[i].w = 0.0f;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v[i], up);
         }
+        if (k) {
+            if (warp == 0) {
+                bulk_store_wait<0>();
+                if (some) {
+                    mbar_wait_uniform(used, k - 1 & 1, &gave_up, c.status, c.limit);
+                    load_down(k);
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v2[g][i], up);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
         if (warp == 0) {
-            if (some) mbar_wait_uniform(down + (k & 1) * 8, k >> 1 & 1, &gave_up, c.status, c.limit);
+            if (some) mbar_wait_uniform(down, k & 1, &gave_up, c.status, c.limit);
             tc_fence_after();
             if (elect_one()) {
                 bulk_store(out + (size_t)k * kPixelBytes, smem_u32(chunk), kPixelBytes);
                 if (some) {
-                    const uint32_t xa = smem_desc_lo(smem_u32(chunk)), wa = smem_desc_lo(smem_u32(downs + (k & 1) * down_bytes));
+                    const uint32_t xa = smem_desc_lo(smem_u32(chunk)), wa = smem_desc_lo(smem_u32(down_chunk));
                     for (int term = 0; term < 3; ++term)             // small terms first
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             mma_f16(tmem, xa + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), wa + e * 2 + (term == 1 ? s.RQ * 8 : 0), desc, k > 0 || e > 0 || term > 0);
-                    mma_commit(used + (k & 1) * 8);
+                    mma_commit(used);
                 }
             }
             __syncwarp();
         }
     }
     if (some) {
-        const int last = s.chunks - 1;
-        if (s.chunks > 1) mbar_wait_uniform(used + (last - 1 & 1) * 8, last - 1 >> 1 & 1, &gave_up, c.status, c.limit);
-        mbar_wait_uniform(used + (last & 1) * 8, last >> 1 & 1, &gave_up, c.status, c.limit);
+        mbar_wait_uniform(used, s.chunks - 1 & 1, &gave_up, c.status, c.limit);
         tc_fence_after();
         const int row = (warp & 3) * 32 + lane;
         for (int rb = warp >> 2; rb < s.RB; rb += 2) {   // a thread a pixel and 32 ranks
@@ -245,11 +251,10 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_pixels_kernel(const TcArg
     __syncthreads();
     tc_fence_after();
     if (warp == 0) {
-        if (gave_up)                                     // what is still on its way must land before the block ends
-            for (int k = max(0, s.chunks - 2); k < s.chunks; ++k) {
-                mbar_wait(down + (k & 1) * 8, k >> 1 & 1, c.limit);
-                mbar_wait(used + (k & 1) * 8, k >> 1 & 1, c.limit);
-            }
+        if (gave_up) {                                   // what is still on its way must land before the block ends
+            mbar_wait(down, s.chunks - 1 & 1, c.limit);
+            mbar_wait(used, s.chunks - 1 & 1, c.limit);
+        }
         tmem_dealloc(tmem, columns);
     }
 }
@@ -477,8 +482,8 @@ int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s,
     launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads * kTeams), kCluster, 0, st, c);
     if (int e = check_launch(ctx)) return e;
     static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
-    const size_t passing = 1024 + 2 * (size_t)kPixelBytes + 2 * (size_t)s.RQ * 256, stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;
-    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + 2 * kPixelBytes + 2 * 128 * 256)) return e;
+    const size_t passing = 1024 + (size_t)kPixelBytes + (size_t)s.RQ * 256, stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;
+    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + kPixelBytes + 128 * 256)) return e;
     launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), passing, st, c);
     if (int e = check_launch(ctx)) return e;
     const int work = a.N * c.at.tiles * c.at.filter_tiles;
