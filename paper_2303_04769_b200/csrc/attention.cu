@@ -185,7 +185,7 @@ SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, co
     const OnDevice on(ctx);
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
     const AttnArgs a{q, k, v, bias, q_extents, k_extents, out, workspace, N, heads, kv_heads, D, QH, QW, KH, KW, QP, KP, blocks_of(heads * D),
-                     q_stride, k_stride, v_stride, scale, cap};
+                     q_stride, k_stride, v_stride, scale, cap, QW + KW - 1};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (on_tensor_cores(QP, flags)) return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
     return QP <= kFewQueries ? launch_attention_few(ctx, a, st) : launch_attention_fp32(ctx, a, st);

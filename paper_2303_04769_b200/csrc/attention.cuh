@@ -17,6 +17,7 @@ struct AttnArgs {
     int QP, KP, CB;                                      // pixels of the planes, channel blocks of q and out
     long long q_stride, k_stride, v_stride;              // floats between images
     float scale, cap;
+    int pitch;                                           // of the bias table's rows as it is read: QW + KW - 1, or more where a copy of it is
 };
 
 #ifdef __CUDACC__
@@ -29,8 +30,8 @@ __device__ __forceinline__ int2 extent(const int32_t *e, int n, int h, int w) {
 __device__ __forceinline__ size_t at(int c, int p, int pixels) { return ((size_t)(c >> 5) * pixels + p) * 32 + (c & 31); }
 
 // Places in the bias table: of_query(i) - of_key(j) is that of the pair's displacement.
-__device__ __forceinline__ int of_query(const AttnArgs &a, int i) { return (i / a.QW + a.KH - 1) * (a.QW + a.KW - 1) + i % a.QW + a.KW - 1; }
-__device__ __forceinline__ int of_key(const AttnArgs &a, int y, int x) { return y * (a.QW + a.KW - 1) + x; }
+__device__ __forceinline__ int of_query(const AttnArgs &a, int i) { return (i / a.QW + a.KH - 1) * a.pitch + i % a.QW + a.KW - 1; }
+__device__ __forceinline__ int of_key(const AttnArgs &a, int y, int x) { return y * a.pitch + x; }
 
 constexpr float kLog2e = 1.4426950408889634f;
 

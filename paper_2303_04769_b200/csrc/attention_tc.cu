@@ -318,11 +318,12 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
         qoff = of_query(a, min(i, a.QP - 1));
         if (c.table_floats) {                            // the table's rows that these queries meet
             const int y0 = i0 / a.QW, y1 = min(i0 + nq * kTile, a.QP) - 1;
-            const int count = (y1 / a.QW - y0 + a.KH) * TW;
+            const int rows = y1 / a.QW - y0 + a.KH;
             const float *from = bias + (size_t)y0 * TW;
-#pragma unroll 8
-            for (int e = threadIdx.x; e < count; e += loader * 32) table[e] = powers_of_two(from[e]);
-            qoff -= y0 * TW;
+            for (int r = warp; r < rows; r += loader)
+#pragma unroll 4
+                for (int e = threadIdx.x & 31; e < TW; e += 32) table[r * a.pitch + e] = powers_of_two(from[r * TW + e]);
+            qoff -= y0 * a.pitch;
         }
     }
     tc_fence_before();
@@ -638,24 +639,27 @@ template <int DP>
 int launch(small_ctx *ctx, const AttnArgs &a, bool x3, cudaStream_t st) {
     static std::atomic<unsigned long long> tiled{0}, done[4] = {};
     const int tiles = ceil_div(a.KP, kTile);
-    const size_t values = sizeof(float) * kTile * (DP + 1);
-    if (int s = allow_shared_memory(ctx, attention_tiles_kernel<DP>, tiled, values)) return s;
-    launch_kernel(ctx, attention_tiles_kernel<DP>, dim3((unsigned)(2 * tiles), (unsigned)a.kv_heads, (unsigned)a.N), dim3(256), values, st, a, tiles);
-    if (int s = check_launch(ctx)) return s;
     TcArgs c{a, tiles, 1, kMaxRing, 0, ctx->dev_status, ctx->wait_iters};
     const size_t most = ctx->max_smem_optin - 12288, tile = (size_t)DP * 512;
     // One tile a block where that still fits the SMs (batch 1, 8 heads of 64, 28 x 28: 31.5 -> 24.3 us; batch 4, 4 heads, 32 x 32 47.9 -> 38.8)
     if (DP < 128 && (long long)a.N * a.heads * ceil_div(a.QP, kTile) > ctx->sm_count) c.q_tiles = 2;
     while (c.ring > 2 && 1024 + (c.q_tiles + c.ring) * tile > most) --c.ring;
     if (a.bias) {
+        // Rows of the copy lie so far apart that a warp's queries read different banks where their row of the plane ends, too.
+        const int pitch = a.QW + (a.KW - 1 + 31) / 32 * 32;
         const int rows = c.q_tiles * kTile, y = (rows + a.QW - 2) / a.QW + 1;        // rows of the plane that such a run of pixels can touch
-        const size_t table = sizeof(float) * ((size_t)(y < a.QH ? y : a.QH) + a.KH - 1) * (a.QW + a.KW - 1);
+        const size_t table = sizeof(float) * ((size_t)(y < a.QH ? y : a.QH) + a.KH - 1) * pitch;
         const int fewest = 3 < c.ring ? 3 : c.ring;
         if (1024 + (c.q_tiles + fewest) * tile + table <= most) {
             while (1024 + (c.q_tiles + c.ring) * tile + table > most) --c.ring;
             c.table_floats = (int)(table / 4);
+            c.a.pitch = pitch;
         }
     }
+    const size_t values = sizeof(float) * kTile * (DP + 1);
+    if (int s = allow_shared_memory(ctx, attention_tiles_kernel<DP>, tiled, values)) return s;
+    launch_kernel(ctx, attention_tiles_kernel<DP>, dim3((unsigned)(2 * tiles), (unsigned)a.kv_heads, (unsigned)a.N), dim3(256), values, st, c.a, tiles);
+    if (int s = check_launch(ctx)) return s;
     const size_t smem = 1024 + (c.q_tiles + c.ring) * tile + sizeof(float) * c.table_floats;
     const bool general = a.bias || a.cap > 0.0f;
     auto run = [&](auto *kern, int row_threads, std::atomic<unsigned long long> &d) {
