@@ -183,7 +183,7 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const AdapterShape s(adapters, C, K, R);
     const AdaptArgs a{in, w_blk, bias, packed, scale, adapter, out, workspace, N, H * W, adapters, (flags & SMALL_RELU) != 0, (flags & SMALL_ACCUMULATE) != 0};
-    if (math != SMALL_MATH_FP32 && (reinterpret_cast<uintptr_t>(out) & 31u) == 0 && adapted_tc_preferred(N, C, K, H * W, R, kSmCount))
+    if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, C, K, H * W, R, kSmCount))
         return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
     if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
     const bool runs = H * W >= 4;                        // several pixels a warp where an image has them

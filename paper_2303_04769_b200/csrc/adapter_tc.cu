@@ -3,10 +3,10 @@
 // written once.  Operands are pairs of halves (halves.cuh).
 //
 // adapter_filters_kernel: the filters as halves, 64 channels a chunk, one exponent for the layer (a cluster finds it).
-// adapter_pixels_kernel: 128 pixels of an image a block: the largest value in one pass over them (from memory), halves in a second (from
+// adapter_pixels_kernel: 128 pixels of an image a block: each one's largest value in one pass over them (from memory), halves in a second (from
 //   L2), which pass through shared memory, where the product with Down is taken from them.  t shares the pixels' accumulator later, so its
 //   exponent follows from theirs, the filters' and the adapter's; where t could pass half precision's range - it is at most the largest value
-//   times the largest sum of a Down row's magnitudes - the pixels take a smaller scale, 2 to 5 powers of two as a rule, of 17 that halves of both
+//   times the largest sum of a Down row's magnitudes - the pixel takes a smaller scale, 2 to 5 powers of two as a rule, of 17 that halves of both
 //   kinds have to spare.
 // adapter_product_kernel: a block walks tiles of 128 pixels x 256 filters; warps for loading (plain bulk copies, two stages of 96 KB), MMAs
 //   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
@@ -32,7 +32,7 @@ struct Layout {
         ranks_at = (size_t)N * tiles * chunks * kPixelBytes;
         filters_at = ranks_at + (size_t)N * tiles * blocks_of(R) * kRankBytes;
         scales_at = filters_at + (size_t)chunks * blocks_of(K) * 32 * 256;
-        bytes = scales_at + sizeof(int) * ((size_t)N * tiles + 4);       // exponents: the filters', three words unused, each pixel tile's
+        bytes = scales_at + sizeof(int) * ((size_t)N * tiles * kTile + 4);       // exponents: the filters', three words unused, each pixel's
     }
 };
 
@@ -113,7 +113,7 @@ __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.
 
 __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArgs c) {
     extern __shared__ char raw[];                        // a chunk of pixels and one of Down: four blocks a SM hide what each waits for
-    __shared__ float most_s[kThreads / 32];
+    __shared__ int ex_s[kTile], full_s[kTile];           // the pixels' exponents, and what they would be without t
     __shared__ uint64_t down_s, used_s;
     __shared__ uint32_t tmem_s;
     __shared__ int gave_up;
@@ -149,34 +149,49 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
             load_down(0);
         }
     }
-    float most = 0.0f;
+    // the largest value of each pixel: eight lanes take a pixel's 128 bytes, a thread four pixels
+    const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
+    float most[kTile / 32] = {};
 #pragma unroll 2
-    for (int cb = 0; cb < s.CB; ++cb) {
-        const float4 *line = reinterpret_cast<const float4 *>(x + (size_t)cb * a.HW * 32) + threadIdx.x;
+    for (int cb = 0; cb < s.CB; ++cb)
 #pragma unroll
-        for (int e = 0; e < kTile * 8; e += kThreads)
-            if ((int)threadIdx.x + e < pixels * 8) most = fmaxf(most, magnitude(line[e]));
-    }
-    most = block_max(most, most_s);
+        for (int i = 0; i < kTile / 32; ++i)
+            if (r0 + i * 32 < pixels) most[i] = fmaxf(most[i], magnitude(*reinterpret_cast<const float4 *>(x + ((size_t)cb * a.HW + r0 + i * 32) * 32 + c0)));
+#pragma unroll
+    for (int i = 0; i < kTile / 32; ++i)
+#pragma unroll
+        for (int o = 1; o < 8; o *= 2) most[i] = fmaxf(most[i], __shfl_xor_sync(~0u, most[i], o));
+    __syncthreads();                                     // (tensor memory is allocated)
     grid_dep_sync();                                     // the filters' exponent
     grid_dep_trigger();
-    int ex = top_exponent(most), et = 0;
-    float factor = 1.0f;
-    if (some) {
-        const float *info = a.packed + s.info_at + 4 * (size_t)id;
-        const int ew = exponents(c)[0], eu = __float_as_int(info[0]), ed = __float_as_int(info[1]);
-        const float by = a.scale ? a.scale[id] : 1.0f;
-        ex = min(max(ex, top_exponent(fmaxf(most * info[2] * magnitude(by), 0.0f)) + eu - ew), 254);
-        et = ex + ew - eu;                               // t * lift(et) beside halves of Up meets the pixels' scale beside halves of the filters
-        factor = et <= 254 ? by * drop(ed) : 0.0f;       // (beyond: 2^-100 of the sum and less, nothing)
-        et = min(max(et, 15), 254);
+    const float *info = a.packed + s.info_at + 4 * (size_t)(some ? id : 0);
+    const float by = some && a.scale ? a.scale[id] : 1.0f, sums = info[2] * magnitude(by);
+    const int ew = exponents(c)[0], eu = __float_as_int(info[0]), ed = __float_as_int(info[1]);
+    float up[kTile / 32];
+    int shrunk = 0;                                      // by how much a pixel's scale is smaller for t's sake
+#pragma unroll
+    for (int i = 0; i < kTile / 32; ++i) {
+        int ex = top_exponent(most[i]);
+        if (some) {
+            const int room = min(max(ex, top_exponent(most[i] * sums) + eu - ew), 254);
+            shrunk = max(shrunk, room - ex);
+            ex = room;
+        }
+        up[i] = lift(ex);
+        if (c0 == 0) {
+            ex_s[r0 + i * 32] = ex;
+            full_s[r0 + i * 32] = top_exponent(most[i]);
+            exponents(c)[4 + (size_t)blockIdx.x * kTile + r0 + i * 32] = ex;
+        }
     }
-    if (threadIdx.x == 0) exponents(c)[4 + blockIdx.x] = ex;
-    const float up = lift(ex);
+    // t is taken from the halves that are written - unless so little is left of them (an adapter far larger than the filters) that t would suffer:
+    // then from halves of their own, at the pixels' full scale, in a pass in front.
+    const bool apart = __syncthreads_or(shrunk > 8);
+    const int steps = apart ? 2 * s.chunks : s.chunks;
     char *out = ws_of(c) + (size_t)blockIdx.x * s.chunks * kPixelBytes;
-    const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
     const uint32_t tmem = tmem_s, desc = f16_desc(s.RQ);
-    for (int k = 0; k < s.chunks; ++k) {
+    for (int step = 0, k = 0; step < steps; ++step, k = k == s.chunks - 1 ? 0 : k + 1) {
+        const bool multiply = some && step < s.chunks, keep = step >= steps - s.chunks;
         float4 v2[2][kTile / 32];                        // on its way while the chunk before is written out and multiplied
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -194,28 +209,26 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
                 }
             }
         }
-        if (k) {
+        if (step) {
             if (warp == 0) {
                 bulk_store_wait<0>();
-                if (some) {
-                    mbar_wait_uniform(used, k - 1 & 1, &gave_up, c.status, c.limit);
-                    load_down(k);
-                }
+                if (some && step <= s.chunks) mbar_wait_uniform(used, step - 1 & 1, &gave_up, c.status, c.limit);
+                if (multiply) load_down(k);
             }
             __syncthreads();
         }
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v2[g][i], up);
+            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v2[g][i], keep ? up[i] : lift(top_exponent(most[i])));
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
         if (warp == 0) {
-            if (some) mbar_wait_uniform(down, k & 1, &gave_up, c.status, c.limit);
+            if (multiply) mbar_wait_uniform(down, k & 1, &gave_up, c.status, c.limit);
             tc_fence_after();
             if (elect_one()) {
-                bulk_store(out + (size_t)k * kPixelBytes, smem_u32(chunk), kPixelBytes);
-                if (some) {
+                if (keep) bulk_store(out + (size_t)k * kPixelBytes, smem_u32(chunk), kPixelBytes);
+                if (multiply) {
                     const uint32_t xa = smem_desc_lo(smem_u32(chunk)), wa = smem_desc_lo(smem_u32(down_chunk));
                     for (int term = 0; term < 3; ++term)             // small terms first
 #pragma unroll
@@ -230,7 +243,10 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     if (some) {
         mbar_wait_uniform(used, s.chunks - 1 & 1, &gave_up, c.status, c.limit);
         tc_fence_after();
-        const int row = (warp & 3) * 32 + lane;
+        const int row = (warp & 3) * 32 + lane, ex = ex_s[row];
+        const int et = ex + ew - eu;                     // t * lift(et) beside halves of Up meets the pixel's scale beside halves of the filters
+        const float x_drop = drop(apart ? full_s[row] : ex);
+        const float factor = et <= 254 ? by * drop(ed) : 0.0f, up_t = lift(min(max(et, 15), 254));       // (beyond: 2^-100 of the sum and less, nothing)
         for (int rb = warp >> 2; rb < s.RB; rb += 2) {   // a thread a pixel and 32 ranks
             char *to = ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes;
             float v[32];
@@ -239,9 +255,9 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
             for (int u = 0; u < 32; u += 4) {
                 // columns behind RQ have no product in them
                 const bool real = rb * 32 + u < s.RQ && row < pixels;
-                const float4 t = real ? make_float4(v[u] * drop(ex) * factor, v[u + 1] * drop(ex) * factor, v[u + 2] * drop(ex) * factor, v[u + 3] * drop(ex) * factor)
+                const float4 t = real ? make_float4(v[u] * x_drop * factor, v[u + 1] * x_drop * factor, v[u + 2] * x_drop * factor, v[u + 3] * x_drop * factor)
                                       : make_float4(0.f, 0.f, 0.f, 0.f);
-                store4<32>(to, row, u, t, lift(et));
+                store4<32>(to, row, u, t, up_t);
             }
         }
     }
@@ -252,8 +268,8 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     tc_fence_after();
     if (warp == 0) {
         if (gave_up) {                                   // what is still on its way must land before the block ends
-            mbar_wait(down, s.chunks - 1 & 1, c.limit);
-            mbar_wait(used, s.chunks - 1 & 1, c.limit);
+            mbar_wait(down, s.chunks - 1 & 1, kDefaultWaitIters);
+            mbar_wait(used, s.chunks - 1 & 1, kDefaultWaitIters);
         }
         tmem_dealloc(tmem, columns);
     }
@@ -359,7 +375,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         if (!ok) {
             if (elect_one()) mma_commit(smem_u32(&drained));
             __syncwarp();
-            mbar_wait(smem_u32(&drained), 0, c.limit);
+            mbar_wait(smem_u32(&drained), 0, kDefaultWaitIters);
         }
     } else {
         const int lane = threadIdx.x & 31, half = warp >> 2;
@@ -368,7 +384,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         int buffer = 0, phase = 0;
         for (int i = blockIdx.x; i < work; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
-            const float x_drop = drop(exponents(c)[4 + np]);
+            const float x_drop = drop(exponents(c)[4 + (size_t)np * kTile + (warp & 3) * 32 + lane]);
             const float grown = w_drop * (1.0f + kCutOff * (float)((kX3 ? 3 : 1) * (s.chunks * (kChunk / 16) + (ranks_of(np) ? (s.R + 15) / 16 : 0))));
             if (!mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit)) break;
             tc_fence_after();
@@ -413,7 +429,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     __syncthreads();
     tc_fence_after();
     if (gave_up && warp == 8)                            // what is still on its way must land before the block ends
-        for (int x = max(0, issued - kStages); x < issued; ++x) mbar_wait(full + x % kStages * 8, (x / kStages) & 1, c.limit);
+        for (int x = max(0, issued - kStages); x < issued; ++x) mbar_wait(full + x % kStages * 8, (x / kStages) & 1, kDefaultWaitIters);
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 

@@ -141,6 +141,7 @@ __global__ void __launch_bounds__(kThreads, R * DP >= 512 ? 1 : 2) attention_few
             }
         }
     }
+    copy_wait<0>();
     // the warp's four groups, then the block's warps, then the cluster's blocks
 #pragma unroll
     for (int r = 0; r < R; ++r) {

@@ -280,7 +280,6 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
         }
         __syncwarp();
         grid_dep_sync();
-        grid_dep_trigger();
         while (issued < min(2 * tiles, c.ring)) load(issued);
     }
     if (wg < nq) {                                       // eight lanes a row
@@ -334,6 +333,8 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
     auto s_at = [&](int buffer) { return tmem + buffer * kTile; };
     auto o_at = [&](int tile) { return tmem + 3 * kTile + tile * DP; };
 
+    // Not before this block has its tensor memory: a block of the next kernel could take it, and wait for this kernel's end with it.
+    if (warp == loader) grid_dep_trigger();
     if (warp == loader) {
         for (int slot = 0, phase = 0; issued < 2 * tiles;) {
             if (!mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit)) break;
@@ -402,14 +403,14 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
         if (!ok) {
             if (elect_one()) mma_commit(smem_u32(&sh.drained));
             __syncwarp();
-            mbar_wait(smem_u32(&sh.drained), 0, c.limit);
+            mbar_wait(smem_u32(&sh.drained), 0, kDefaultWaitIters);
         }
     } else if (wg < nq) {
         grid_dep_sync();
         const float *undo = undo_scaling(a, c.tiles, kBytes) + ((size_t)n * a.kv_heads + hk) * c.tiles * 2;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;               // this warp's 32 lanes of tensor memory
         const float q_drop = sh.q_drop[wg][row], cap2 = a.cap * kLog2e, over_cap = a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
-        const float *at_table = (c.table_floats ? table : bias) + qoff;
+        const float *at_copy = table + qoff;             // (a pointer of its own: one that could be either place is read the slow way)
         uint64_t o[kOut / 2];
         float l = 0.0f, m = INFINITY;                    // m: 14 less the running maximum, in powers of two
         float2 drops = tiles ? *reinterpret_cast<const float2 *>(undo) : make_float2(0.f, 0.f), next = drops;
@@ -460,17 +461,17 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
 #pragma unroll
                             for (int u = 0; u < 32; u += kRun) {
                                 if (run[u / kRun] >= 0) {            // one row of the plane: neighbours in the table
-                                    const float *b = at_table - run[u / kRun];
+                                    const float *b = at_copy - run[u / kRun];
 #pragma unroll
                                     for (int w = 0; w < kRun; ++w) v[u + w] = fmaf(v[u + w], f1, b[kRun - 1 - w]);
                                 } else {
 #pragma unroll
-                                    for (int w = 0; w < kRun; ++w) v[u + w] = fmaf(v[u + w], f1, at_table[-place[u + w]]);
+                                    for (int w = 0; w < kRun; ++w) v[u + w] = fmaf(v[u + w], f1, at_copy[-place[u + w]]);
                                 }
                             }
                         } else {
 #pragma unroll
-                            for (int u = 0; u < 32; ++u) v[u] = fmaf(v[u], f1, powers_of_two(at_table[-place[u]]));
+                            for (int u = 0; u < 32; ++u) v[u] = fmaf(v[u], f1, powers_of_two(bias[qoff - place[u]]));
                         }
                     }
                 }
@@ -627,8 +628,8 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
     __syncthreads();
     tc_fence_after();
     if (sh.gave_up && warp == loader) {                  // what is still on its way must land before the block ends
-        for (int x = max(0, issued - c.ring); x < issued; ++x) mbar_wait(full + x % c.ring * 8, (x / c.ring) & 1, c.limit);
-        for (int t = max(0, (issued + 1) / 2 - kPlaces); kGeneral && t < (issued + 1) / 2; ++t) mbar_wait(placed + t % kPlaces * 8, t / kPlaces & 1, c.limit);
+        for (int x = max(0, issued - c.ring); x < issued; ++x) mbar_wait(full + x % c.ring * 8, (x / c.ring) & 1, kDefaultWaitIters);
+        for (int t = max(0, (issued + 1) / 2 - kPlaces); kGeneral && t < (issued + 1) / 2; ++t) mbar_wait(placed + t % kPlaces * 8, t / kPlaces & 1, kDefaultWaitIters);
     }
     if (warp == issuer) tmem_dealloc(tmem, 512);
 }

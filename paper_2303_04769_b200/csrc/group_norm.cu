@@ -279,6 +279,7 @@ int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return 
 // one is cut until three share one (56 x 56, 400 KB, batch 128, 256 channels: 181 us in eighths or in parts of 70 KB, 208 in quarters).
 constexpr size_t kBlockBytes = 104u << 10, kSplitBytes = 70u << 10;
 constexpr size_t kMostBytes = 220u << 10;         // at all
+constexpr size_t kMostShared = (227u << 10) - 2048;         // what a block can have, less the kernels' static shared memory
 
 size_t block_bytes(const NormPlan &p, int HW) {   // the tile, the sums of channels, their means, scales and shifts
     return (size_t)p.unit_blocks * 128 * ((HW + p.splits - 1) / p.splits + p.warps_per_block + 3);
@@ -311,7 +312,7 @@ NormPlan plan_norm(int N, int C, int HW, int groups) {
 template <unsigned kAct>
 int launch_norm(small_ctx *ctx, const NormArgs &a, const NormPlan &p, int N, cudaStream_t st) {
     static std::atomic<unsigned long long> whole{0}, part{0};
-    const size_t most = ctx->max_smem_optin - 2048;
+    const size_t most = kMostShared;
     const dim3 grid((unsigned)(N * p.splits), (unsigned)p.units), block(kThreads);
     if (p.on_chip) {
         if (int s = allow_shared_memory(ctx, group_norm_kernel<true, kAct>, whole, most)) return s;
@@ -351,6 +352,7 @@ SMALL_API int small_group_norm(small_ctx *ctx, const float *in, const float *gam
     if (int s = check_pointers({in, out}, {gamma, beta, workspace})) return s;
     if (!norm_shape_ok(N, C, H, W, groups)) return SMALL_ERR_SHAPE;
     const NormPlan p = plan_norm(N, C, H * W, groups);
+    if (p.smem > kMostShared) return SMALL_ERR_UNSUPPORTED;
     const long long blocks = (long long)N * p.units * p.splits;
     if (blocks > 0x7fffffffLL || p.units > 65535) return SMALL_ERR_SHAPE;
     const size_t bytes = sizeof(float) * packed_elems(N, C, H, W), ws = small_group_norm_workspace_bytes(N, C, H, W, groups);
@@ -369,6 +371,5 @@ SMALL_API int small_group_norm(small_ctx *ctx, const float *in, const float *gam
     const NormArgs a{in, gamma, beta, out, static_cast<float *>(workspace), C, blocks_of(C), cpg, H * W, p.unit_blocks, p.units, p.splits, part, p.warps_per_block,
                      cpg <= 32 && (cpg & (cpg - 1)) == 0 ? __builtin_ctz(cpg) : -1, eps, (float)(1.0 / ((double)cpg * H * W))};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (p.smem > ctx->max_smem_optin - 2048) return SMALL_ERR_UNSUPPORTED;           // the kernels have static shared memory too
     return flags == SMALL_RELU ? launch_norm<SMALL_RELU>(ctx, a, p, N, st) : flags == SMALL_SILU ? launch_norm<SMALL_SILU>(ctx, a, p, N, st) : launch_norm<0>(ctx, a, p, N, st);
 }

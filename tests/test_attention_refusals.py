@@ -45,6 +45,7 @@ def test_group_norm():
         assert norm(**bad) == SHAPE
         full = dict(N=2, C=64, H=8, W=8, groups=8) | bad
         assert B.small_group_norm_workspace_bytes(full["N"], full["C"], full["H"], full["W"], full["groups"]) == 0
+    assert norm(N=1, C=65536, H=2, W=2, groups=1) == 6                   # a group that no block's shared memory holds the sums of
     assert norm(out=at(0) + 1024) == OVERLAP and norm(gamma=at(3) + 16) == OVERLAP and norm(beta=at(3)) == OVERLAP
     big = dict(H=512, W=512)
     assert B.small_group_norm_workspace_bytes(2, 64, 512, 512, 8) > 0 and B.small_group_norm_workspace_bytes(2, 64, 8, 8, 8) == 0

@@ -50,7 +50,8 @@ class Layer:
 SHAPES = [  # N, C, K, H, W, rank, adapters
     (1, 1, 1, 1, 1, 1, 1), (8, 512, 512, 1, 1, 8, 16), (3, 64, 64, 1, 1, 128, 2), (33, 96, 40, 1, 1, 4, 5), (130, 64, 128, 1, 1, 16, 7), (4, 96, 130, 13, 14, 5, 7),
     (2, 128, 128, 28, 28, 16, 3), (5, 40, 200, 7, 7, 33, 4), (2, 31, 33, 5, 9, 3, 2), (1, 256, 768, 14, 14, 64, 2), (3, 64, 96, 31, 29, 20, 9), (6, 320, 64, 3, 3, 8, 3),
-    (1, 100, 300, 56, 56, 16, 1), (2, 32, 32, 1, 300, 100, 2), (9, 200, 1000, 1, 1, 16, 4)]
+    (1, 100, 300, 56, 56, 16, 1), (2, 32, 32, 1, 300, 100, 2), (9, 200, 1000, 1, 1, 16, 4),
+    (40, 70, 300, 12, 11, 17, 6), (90, 33, 45, 8, 9, 128, 3), (75, 160, 64, 16, 16, 48, 80)]
 
 
 @pytest.mark.parametrize("mode", MODES)
@@ -94,6 +95,23 @@ def test_images_do_not_reach_one_another(mode):
         assert np.isnan(got[2]).all() and np.isnan(got[4, :, 0, 0]).all()
         got[2], got[4, :, 0, 0] = ref[2], ref[4, :, 0, 0]
         assert rel_err(got, ref) <= TOL[mode]
+
+
+@pytest.mark.parametrize("mode", ["fp32", "3xtf32"])
+@pytest.mark.parametrize("R_", [4, 40])
+def test_pixels_and_adapters_of_very_different_size(R_, mode):
+    """One pixel far larger than its neighbours, and adapters far larger and smaller than the filters: each pixel keeps its own accuracy."""
+    rng = np.random.default_rng(25)
+    layer, x = Layer(rng, 96, 160, R_, 3), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    x[:, :, 4, 5] *= 1e12
+    x[:, :, 7, 1] *= 1e-12
+    layer.b[:] = 0
+    layer.up[1] *= 1e6
+    layer.down[2] *= 1e-6
+    ids = (np.arange(80) % 4 - 1).astype(np.int32)
+    got, ref = layer.run(x, ids, mode), layer.ref(x, ids)
+    size = np.sqrt((ref ** 2).mean(1, keepdims=True))
+    assert rel_err(got / size, ref / size) <= TOL[mode]
 
 
 @pytest.mark.parametrize("plane", [(1, 1), (14, 13)])

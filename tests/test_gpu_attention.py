@@ -152,6 +152,16 @@ def test_scales_of_the_operands(qp, qs, ks, vs, mode):
     close(run(q, k, v, 2, 2, mode, scale=scale) / vs, R.attention(q, k, v, 2, 2, scale) / vs, mode)
 
 
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("qp", [(1, 1), (13, 12)])
+@pytest.mark.parametrize("scale", [0.0, -0.15])
+def test_scales_that_are_not_positive(qp, scale, mode):
+    rng = np.random.default_rng(19)
+    q, k, v = make(rng, 2, 2, 1, 40, qp, (13, 12))
+    for args in (dict(), dict(bias=table(rng, 2, qp, (13, 12))), dict(cap=2.0)):
+        close(run(q, k, v, 2, 1, mode, scale=scale, **args), R.attention(q, k, v, 2, 1, scale, **args), mode)
+
+
 @pytest.mark.parametrize("mode", ["fp32", "3xtf32"])
 def test_large_scores(mode):
     """Scores of some hundreds: nearly all weight on one key; the largest score may come last or first."""
@@ -210,6 +220,23 @@ def test_repeatable_on_streams_and_in_a_graph(shape, mode):
     for _ in range(3):
         graph.replay()
     assert np.array_equal(from_blk(out, N, heads * D, *qp), first)
+
+
+def test_between_kernels_that_hold_tensor_memory():
+    """Attention whose blocks take turns on an SM's tensor memory, with convolutions right behind it that want some too, over and over."""
+    rng = np.random.default_rng(20)
+    N, heads, D, plane = 24, 8, 32, (11, 11)
+    q, k, v = make(rng, N, heads, heads, D, plane, plane)
+    qb, kb, vb, out = to_blk(q), to_blk(k), to_blk(v), new_blk(N, heads * D, *plane)
+    ws = workspace(N, heads, heads, D, plane, plane, "3xtf32")
+    w = dev((rng.standard_normal((256, 256, 3, 3)) / 48).astype(np.float32))
+    wb, y = torch.empty(B.small_conv_weight_elems(256, 256, 3, 3, B.MATH_3XTF32), device="cuda"), new_blk(N, 256, *plane)
+    B.small_pack_conv_weights(ctx(), w, wb, 256, 256, 3, 3, B.MATH_3XTF32)
+    for _ in range(40):
+        B.small_attention(ctx(), qb, kb, vb, out, ws, ws.numel(), N, heads, heads, D, plane, plane, flags=B.MATH_3XTF32)
+        B.small_conv2d(ctx(), out, wb, None, y, N, 256, 256, *plane, 3, 3, 1, (1, 1, 1, 1), B.MATH_3XTF32)
+    close(from_blk(out, N, heads * D, *plane), R.attention(q, k, v, heads, heads, D ** -0.5), "3xtf32")
+    assert np.isfinite(from_blk(y, N, 256, *plane)).all() and B.small_device_status(ctx()) == B.OK
 
 
 @pytest.mark.parametrize("mode", MODES)
