@@ -147,6 +147,8 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
         if (some) {
             tmem_alloc(smem_u32(&tmem_s), columns);
             load_down(0);
+        } else {                                         // a block that could still ask for tensor memory keeps the next one off its SM
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
     }
     // the largest value of each pixel: eight lanes take a pixel's 128 bytes, a thread four pixels

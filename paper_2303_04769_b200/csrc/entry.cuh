@@ -40,7 +40,8 @@ template <typename K>
 static inline int allow_shared_memory(small_ctx *ctx, K *kern, std::atomic<unsigned long long> &done, size_t bytes) {
     const unsigned long long bit = 1ull << (ctx->device & 63);
     if (done.load(std::memory_order_relaxed) & bit) return SMALL_OK;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, 100);       // several blocks a SM where they fit
     if (e != cudaSuccess) { ctx->last_cuda = (int)e; return SMALL_ERR_CUDA; }
     done.fetch_or(bit, std::memory_order_relaxed);
     return SMALL_OK;
