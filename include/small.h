@@ -373,7 +373,8 @@ int small_fc_uses_tensor_cores(int N, int J, int K, unsigned math);
  * workspace: device, 16-byte aligned, small_group_norm_workspace_bytes bytes; may be NULL where that is 0 - planes whose group fits
  * a cluster's shared memory, which are read once.  Calls that may run at the same time need workspaces of their own.  The mean is
  * taken first and the deviations are summed after it, all sums in FP32.  A value that is not finite makes its image's group NaN.
- * Errors: INVALID_ARG, SHAPE, ALIGN, OVERLAP, WORKSPACE (needed and NULL). */
+ * Errors: INVALID_ARG, SHAPE, ALIGN, OVERLAP, WORKSPACE (needed and NULL), UNSUPPORTED (a run of whole groups and whole channel blocks of
+ * more than some 10,000 channels). */
 size_t small_group_norm_workspace_bytes(int N, int C, int H, int W, int groups);
 int small_group_norm(small_ctx *ctx, const float *in, const float *gamma, const float *beta, float *out, void *workspace,
                      int N, int C, int H, int W, int groups, float eps, unsigned flags, void *stream);
@@ -390,14 +391,16 @@ int small_group_norm(small_ctx *ctx, const float *in, const float *gamma, const 
  * channel blocks of one stacked tensor (a stride below the run's own size is SMALL_ERR_SHAPE, one not a multiple of 4 floats
  * SMALL_ERR_ALIGN).
  * bias: float[heads][QH + KH - 1][QW + KW - 1], a value for each displacement, or NULL.  -inf keeps a pair apart; any finite value,
- * the type's lowest too, is a number to be added.
+ * the type's lowest too, is a number to be added (from 2.3e38 on, in magnitude, they may count as equal).
  * q_extents, k_extents: int32[N][2], the rows and columns of image n's plane that hold its pixels (clamped to the plane), or
  * NULL for whole planes.  Key pixels outside are not read as keys: whatever they hold, NaN too, has no part in the result.  Query
  * pixels outside, and queries that no key is left for, get 0.
  * scale, cap: finite, cap >= 0 (0: no cap).  D at most 128, any number; heads, kv_heads at least 1.
  * flags: one SMALL_MATH_*.  FP32: FP32 multiply-adds.  TF32, 3XTF32: both products on the tensor cores where the shape has the
- * queries for it, operands of 11 significant bits, or two such terms each (three products: FP32 accuracy); scores, their
- * maxima and sums and the accumulation over keys in FP32.
+ * queries for it (more than 16), operands of 11 significant bits, or two such terms each (three products: FP32 accuracy); scores,
+ * their maxima and sums and the accumulation over keys in FP32.  The terms are halves, scaled by a query's and by 128 keys' largest value:
+ * keys and values 2^23 below the largest of their 128 begin to lose accuracy.  A value that is not finite makes what it
+ * takes part in not finite (NaN where FP32 arithmetic has an infinity, possibly).
  * workspace: device, 16-byte aligned, small_attention_workspace_bytes bytes (keys and values as the tensor cores read them; 0 and
  * NULL where they are read as they lie).  Calls that may run at the same time, and graphs that may be replayed at the same
  * time, need workspaces of their own.
@@ -411,7 +414,7 @@ int small_attention(small_ctx *ctx, const float *q, const float *k, const float 
 /* 1 x 1 convolution (a full reduction where H = W = 1) whose images bring low-rank adapters of their own beside the filters
  * that all of them share:
  *     out = act(W in + bias + scale[a] * Up[a] (Down[a] in))        a = adapter[n], the adapter of image n
- * An index outside 0 .. adapters - 1 (-1, say) means none.  Down: [R][C], Up: [K][R], R at most 128.
+ * An index outside 0 .. adapters - 1 (-1, say) means none; indexes are read when the work runs.  Down: [R][C], Up: [K][R], R at most 128.
  * small_pack_adapters lays out all adapters once: down: device float[adapters][R][C], up: device float[adapters][K][R],
  * packed: device, small_adapter_elems floats. */
 size_t small_adapter_elems(int adapters, int C, int K, int R);
@@ -420,7 +423,8 @@ int small_pack_adapters(small_ctx *ctx, const float *down, const float *up, floa
 /* in: blocked [N][C][H][W]; w_blk: from small_pack_conv_weights(C, K, 1, 1, math); bias: K floats or NULL; adapter: device
  * int32[N]; scale: device float[adapters] or NULL (1); out: blocked [N][K][H][W].  flags: SMALL_RELU, SMALL_ACCUMULATE (out_previous is
  * added in front of the activation) and one SMALL_MATH_* for both parts.  workspace: device, 16-byte aligned,
- * small_adapted_conv2d_workspace_bytes bytes (the products with Down); calls that may run at the same time need their own.
+ * small_adapted_conv2d_workspace_bytes bytes (the products with Down, and where the layer runs as one product on the tensor cores its
+ * operands as halves, scaled by pixel); calls that may run at the same time need their own.
  * Errors as small_conv2d, and WORKSPACE (NULL). */
 size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R);
 int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,

@@ -135,8 +135,14 @@ bool attention_shape_ok(int N, int heads, int kv_heads, int D, int QH, int QW, i
     return N <= 65535 && heads <= 65535 && ((long long)QH + KH) * ((long long)QW + KW) <= (1ll << 30);
 }
 
-// Tiles of 128 queries: worth it where at least some of a tile is real.
-bool on_tensor_cores(int QP, unsigned math) { return math != SMALL_MATH_FP32 && QP >= 32; }
+// Which kernel.  Few queries: theirs, in every math mode (8 heads of 64, 28 x 28 keys, batch 8: 16 queries 27.6 us, on the tensor cores some 28;
+// one query 10).  In the tensor-core modes the tensor cores from there on (17 queries 28 us, in FP32 123), but where all of an image is one tile of
+// the FP32 kernel and those tiles are more than the SMs (7 x 7, 8 heads, us, FP32 / tensor cores: 64 channels batch 4 16.2 / 11.4, 16 16.5 / 15.9, 32
+// 25.3 / 25.9, 128 60.5 / 89.3; 32 channels batch 16 11.6 / 12.1, 32 14.4 / 21.6, 128 35.1 / 65.7).
+bool on_tensor_cores(int N, int heads, int QP, int KP, unsigned math) {
+    if (math == SMALL_MATH_FP32 || QP <= kFewQueries) return false;
+    return QP > kRows || KP > kKeys || (long long)N * heads <= kSmCount;
+}
 
 }  // namespace
 
@@ -150,7 +156,7 @@ using namespace small;
 
 SMALL_API size_t small_attention_workspace_bytes(int N, int heads, int kv_heads, int D, int QH, int QW, int KH, int KW, unsigned math) {
     if (!attention_shape_ok(N, heads, kv_heads, D, QH, QW, KH, KW) || (math & ~SMALL_MATH_MASK) || !one_math_mode(math)) return 0;
-    return on_tensor_cores(QH * QW, math) ? attention_tc_workspace(N, kv_heads, D, KH * KW) : 0;
+    return on_tensor_cores(N, heads, QH * QW, KH * KW, math) ? attention_tc_workspace(N, kv_heads, D, KH * KW) : 0;
 }
 
 SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, const float *v, const float *bias, const int32_t *q_extents,
@@ -187,6 +193,6 @@ SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, co
     const AttnArgs a{q, k, v, bias, q_extents, k_extents, out, workspace, N, heads, kv_heads, D, QH, QW, KH, KW, QP, KP, blocks_of(heads * D),
                      q_stride, k_stride, v_stride, scale, cap, QW + KW - 1};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (on_tensor_cores(QP, flags)) return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
+    if (on_tensor_cores(N, heads, QP, KP, flags)) return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
     return QP <= kFewQueries ? launch_attention_few(ctx, a, st) : launch_attention_fp32(ctx, a, st);
 }

@@ -52,7 +52,8 @@ SHAPES = [  # N, heads, kv heads, D, query plane, key plane
     (1, 4, 2, 40, (25, 13), (25, 13)), (1, 2, 2, 64, (28, 28), (28, 28)), (2, 2, 1, 128, (12, 11), (12, 11)), (1, 3, 1, 96, (9, 16), (9, 16)), (1, 1, 1, 5, (11, 12), (11, 12)),
     (1, 2, 2, 33, (13, 13), (13, 13)), (1, 1, 1, 64, (16, 16), (8, 16)), (1, 1, 1, 64, (1, 128), (1, 129)), (1, 1, 1, 32, (127, 1), (128, 1)), (1, 2, 1, 64, (16, 17), (3, 1)),
     (2, 8, 8, 64, (1, 1), (7, 7)), (3, 8, 2, 64, (1, 1), (31, 33)), (1, 6, 2, 48, (1, 3), (20, 21)), (1, 16, 1, 32, (1, 1), (40, 41)), (1, 1, 1, 128, (2, 1), (96, 96)),
-    (1, 1, 1, 64, (3, 1), (1, 1)), (1, 5, 5, 20, (1, 1), (9, 9)), (1, 1, 1, 7, (1, 1), (33, 3)), (1, 2, 2, 64, (50, 41), (50, 41)), (1, 1, 1, 128, (1, 300), (2, 150))]
+    (1, 1, 1, 64, (3, 1), (1, 1)), (1, 5, 5, 20, (1, 1), (9, 9)), (1, 1, 1, 7, (1, 1), (33, 3)), (1, 2, 2, 64, (50, 41), (50, 41)), (1, 1, 1, 128, (1, 300), (2, 150)),
+    (25, 8, 4, 48, (7, 7), (7, 7)), (2, 2, 2, 64, (1, 16), (12, 12)), (2, 2, 2, 64, (1, 17), (12, 12)), (1, 4, 1, 128, (4, 4), (8, 8)), (1, 40, 8, 32, (2, 3), (10, 10))]
 
 
 @pytest.mark.parametrize("mode", MODES)
