@@ -1,11 +1,11 @@
 // 1 x 1 convolution with a low-rank adapter for each image, out = act(W x + b + s_a Up_a (Down_a x)): entry points, and the form for few
-// pixels and for FP32 arithmetic - small_conv2d for the shared product, and two kernels for what the adapters add to it.
+// pixels and for FP32 arithmetic - small_conv2d for the shared product, and a kernel for what the adapters add to it.
 #include "adapter.cuh"
 
 namespace small {
 namespace {
 
-constexpr int kMaxRank = 128, kThreads = 256;
+constexpr int kMaxRank = 128, kThreads = 256, kWarps = kThreads / 32;
 
 bool adapter_shape_ok(int adapters, int C, int K, int R) {
     return adapters >= 1 && C >= 1 && K >= 1 && R >= 1 && R <= kMaxRank && C <= (1 << 20) && K <= (1 << 20) && adapters <= (1 << 20);
@@ -28,87 +28,92 @@ __global__ void __launch_bounds__(kThreads) pack_adapters_kernel(const float *__
     }
 }
 
-__device__ __forceinline__ bool adapter_of(const AdaptArgs &a, int n, int &id) {
-    id = a.adapter[n];
-    return id >= 0 && id < a.adapters;
-}
+// out = act(out + scale Up (Down x)) behind the convolution that has written `out`: a block takes up to 32 pixels of an image (kPoint: one) and a
+// run of filter blocks.  The products with Down, t, come first, from what is older than the convolution: they are taken while it runs.
+// For them a warp takes four pixels and eight ranks, a lane a channel of each block, so that every load is a whole line and serves four or
+// eight products; one pixel's channel blocks are dealt out to the warps.  Then a warp takes a filter block, a lane a filter.
+constexpr int kRun = 32;                 // pixels of a block
 
-// t[n][pixel][rank] = scale Down x.  A warp takes kPixels pixels of an image and eight ranks, a lane a channel of each block: every load is a
-// whole line, and each serves kPixels or eight products.  The sums are dealt out over the lanes while they are added up.
-template <int kPixels>
-__global__ void __launch_bounds__(kThreads) adapter_down_kernel(const AdaptArgs a, const AdapterShape s) {
-    grid_dep_sync();
-    grid_dep_trigger();
-    const int lane = threadIdx.x & 31, rows = s.RP / 8, runs = (a.HW + kPixels - 1) / kPixels;
-    const long long tasks = (long long)a.N * runs * rows, stride = (long long)gridDim.x * (kThreads / 32);
-    for (long long i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i < tasks; i += stride) {
-        const int rg = (int)(i % rows), p0 = (int)(i / rows % runs) * kPixels, n = (int)(i / rows / runs);
-        int id;
-        if (!adapter_of(a, n, id)) continue;
-        const float *x = a.in + (size_t)n * s.CB * a.HW * 32 + lane, *w = a.packed + id * s.down + rg * 256 + lane;
-        float acc[kPixels * 8];
-#pragma unroll
-        for (int u = 0; u < kPixels * 8; ++u) acc[u] = 0.0f;
-#pragma unroll 4
-        for (int cb = 0; cb < s.CB; ++cb) {
-            float v[kPixels];
-#pragma unroll
-            for (int q = 0; q < kPixels; ++q) v[q] = p0 + q < a.HW && cb * 32 + lane < s.C ? x[((size_t)cb * a.HW + p0 + q) * 32] : 0.0f;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const float u = w[(cb * s.RP + r) * 32];
-#pragma unroll
-                for (int q = 0; q < kPixels; ++q) acc[q * 8 + r] = fmaf(v[q], u, acc[q * 8 + r]);
-            }
-        }
-        // halves of the sums go to halves of the lanes, until a lane has kPixels / 4 of them left (or several lanes the same one)
-        int have = kPixels * 8;
-#pragma unroll
-        for (int bit = 16; bit; bit /= 2) {
-            const bool upper = lane & bit;
-            if (have > 1) {
-#pragma unroll
-                for (int u = 0; u < kPixels * 4; ++u)
-                    if (u < have / 2) {
-                        const float give = upper ? acc[u] : acc[u + have / 2], keep = upper ? acc[u + have / 2] : acc[u];
-                        acc[u] = keep + __shfl_xor_sync(~0u, give, bit);
-                    }
-                have /= 2;
-            } else {
-                acc[0] += __shfl_xor_sync(~0u, acc[0], bit);
-            }
-        }
+template <bool kPoint>
+__global__ void __launch_bounds__(kThreads) adapter_add_kernel(const AdaptArgs a, const AdapterShape s, int runs, int filter_blocks) {
+    extern __shared__ float t_s[];                       // [pixels][RP], kPoint: [warps][RP]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockIdx.x / runs, p0 = blockIdx.x % runs * (kPoint ? 1 : kRun);
+    const int pixels = kPoint ? 1 : min(kRun, a.HW - p0), id = a.adapter[n];
+    const bool some = id >= 0 && id < a.adapters;
+    if (some) {
+        const float *x = a.in + ((size_t)n * s.CB * a.HW + p0) * 32 + lane, *w = a.packed + id * s.down + lane;
         const float factor = a.scale ? a.scale[id] : 1.0f;
-        const int e = kPixels == 4 ? lane : lane >> 2, p = p0 + e / 8;               // one pixel: four lanes have each rank's sum
-        if ((kPixels == 4 || (lane & 3) == 0) && p < a.HW) static_cast<float *>(a.ws)[((size_t)n * a.HW + p) * s.RP + rg * 8 + e % 8] = factor * acc[0];
+        constexpr int kPixels = kPoint ? 1 : 4, kSums = kPixels * 8;
+        for (int i = kPoint ? 0 : warp; i < (kPoint ? 1 : (pixels + 3) / 4) * (s.RP / 8); i += kPoint ? 1 : kWarps) {
+            const int rg = i % (s.RP / 8), q0 = i / (s.RP / 8) * 4;
+            float acc[kSums];
+#pragma unroll
+            for (int u = 0; u < kSums; ++u) acc[u] = 0.0f;
+#pragma unroll 4
+            for (int cb = kPoint ? warp : 0; cb < s.CB; cb += kPoint ? kWarps : 1) {
+                float v[kPixels];
+#pragma unroll
+                for (int q = 0; q < kPixels; ++q) v[q] = q0 + q < pixels && cb * 32 + lane < s.C ? x[((size_t)cb * a.HW + q0 + q) * 32] : 0.0f;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float u = w[(cb * s.RP + rg * 8 + r) * 32];
+#pragma unroll
+                    for (int q = 0; q < kPixels; ++q) acc[q * 8 + r] = fmaf(v[q], u, acc[q * 8 + r]);
+                }
+            }
+            // halves of the sums go to halves of the lanes, until each lane has one (one pixel: four lanes the same one)
+            int have = kSums;
+#pragma unroll
+            for (int bit = 16; bit; bit /= 2) {
+                const bool upper = lane & bit;
+                if (have > 1) {
+#pragma unroll
+                    for (int u = 0; u < kSums / 2; ++u)
+                        if (u < have / 2) {
+                            const float give = upper ? acc[u] : acc[u + have / 2], keep = upper ? acc[u + have / 2] : acc[u];
+                            acc[u] = keep + __shfl_xor_sync(~0u, give, bit);
+                        }
+                    have /= 2;
+                } else {
+                    acc[0] += __shfl_xor_sync(~0u, acc[0], bit);
+                }
+            }
+            if (kPoint) {
+                if ((lane & 3) == 0) t_s[warp * s.RP + rg * 8 + lane / 4] = factor * acc[0];
+            } else if (q0 + lane / 8 < pixels) {
+                t_s[(q0 + lane / 8) * s.RP + rg * 8 + lane % 8] = factor * acc[0];
+            }
+        }
+        __syncthreads();
+        if (kPoint) {
+            float sum = 0.0f;
+            if (threadIdx.x < s.RP)
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) sum += t_s[i * s.RP + threadIdx.x];
+            __syncthreads();
+            if (threadIdx.x < s.RP) t_s[threadIdx.x] = sum;
+            __syncthreads();
+        }
     }
-}
-
-// out = act(out + Up t).  A warp takes kPixels pixels and a block of filters, a lane a filter.
-template <int kPixels>
-__global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdaptArgs a, const AdapterShape s) {
-    grid_dep_sync();
+    grid_dep_sync();                                     // the convolution
     grid_dep_trigger();
-    const int lane = threadIdx.x & 31, runs = (a.HW + kPixels - 1) / kPixels;
-    const long long tasks = (long long)a.N * s.KB * runs, stride = (long long)gridDim.x * (kThreads / 32);
-    for (long long i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); i < tasks; i += stride) {
-        const int p0 = (int)(i % runs) * kPixels, kb = (int)(i / runs % s.KB), n = (int)(i / runs / s.KB);
-        int id;
-        const bool some = adapter_of(a, n, id);
-        if (!some && !a.relu) continue;
-        float *out = a.out + (((size_t)n * s.KB + kb) * a.HW + p0) * 32 + lane;
+    if (!some && !a.relu) return;
+    constexpr int kPixels = kPoint ? 1 : 8;
+    const int kb0 = blockIdx.y * filter_blocks, count = min(filter_blocks, s.KB - kb0), groups = kPoint ? 1 : (pixels + 7) / 8;
+    for (int i = warp; i < count * groups; i += kWarps) {
+        const int kb = kb0 + i / groups, q0 = i % groups * 8;
+        float *out = a.out + (((size_t)n * s.KB + kb) * a.HW + p0 + q0) * 32 + lane;
         float acc[kPixels];
 #pragma unroll
-        for (int q = 0; q < kPixels; ++q) acc[q] = p0 + q < a.HW ? out[q * 32] : 0.0f;
+        for (int q = 0; q < kPixels; ++q) acc[q] = q0 + q < pixels ? out[q * 32] : 0.0f;
         if (some) {
             const float *w = a.packed + s.down * a.adapters + id * s.up + (size_t)kb * s.RP * 32 + lane;
-            const float4 *t = reinterpret_cast<const float4 *>(static_cast<const float *>(a.ws) + ((size_t)n * a.HW + p0) * s.RP);
 #pragma unroll 2
             for (int r = 0; r < s.RP; r += 4) {
                 const float w0 = w[r * 32], w1 = w[r * 32 + 32], w2 = w[r * 32 + 64], w3 = w[r * 32 + 96];
 #pragma unroll
                 for (int q = 0; q < kPixels; ++q) {
-                    const float4 v = p0 + q < a.HW ? t[(q * s.RP + r) / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float4 v = q0 + q < pixels ? *reinterpret_cast<const float4 *>(t_s + (q0 + q) * s.RP + r) : make_float4(0.f, 0.f, 0.f, 0.f);
                     acc[q] = fmaf(v.x, w0, fmaf(v.y, w1, fmaf(v.z, w2, fmaf(v.w, w3, acc[q]))));
                 }
             }
@@ -116,7 +121,7 @@ __global__ void __launch_bounds__(kThreads) adapter_up_kernel(const AdaptArgs a,
         if (kb * 32 + lane >= s.K) continue;             // pad lanes stay what the convolution has written
 #pragma unroll
         for (int q = 0; q < kPixels; ++q)
-            if (p0 + q < a.HW) out[q * 32] = a.relu && !(acc[q] > 0.0f) ? 0.0f : acc[q];
+            if (q0 + q < pixels) out[q * 32] = a.relu && !(acc[q] > 0.0f) ? 0.0f : acc[q];
     }
 }
 
@@ -153,9 +158,7 @@ SMALL_API int small_pack_adapters(small_ctx *ctx, const float *down, const float
 
 SMALL_API size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R) {
     if (N < 1 || H < 1 || W < 1 || (long long)H * W > (1ll << 24) || !adapter_shape_ok(1, C, K, R)) return 0;
-    const size_t products = sizeof(float) * (size_t)N * H * W * AdapterShape(1, C, K, R).RP;
-    const size_t whole = adapted_tc_preferred(N, C, K, H * W, R, kSmCount) ? adapted_tc_workspace(N, C, K, H * W, R) : 0;
-    return whole > products ? whole : products;
+    return adapted_tc_preferred(N, C, K, H * W, R, kSmCount) ? adapted_tc_workspace(N, C, K, H * W, R) : 0;
 }
 
 SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,
@@ -169,15 +172,15 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     if (!adapter_shape_ok(adapters, C, K, R)) return SMALL_ERR_SHAPE;
     if (int s = make_geom(g, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0)) return s;
     const size_t ws = small_adapted_conv2d_workspace_bytes(N, C, K, H, W, R);
-    if (!workspace) return SMALL_ERR_WORKSPACE;
+    if (ws && !workspace) return SMALL_ERR_WORKSPACE;
     const unsigned math = flags & SMALL_MATH_MASK;
     const size_t in_b = sizeof(float) * packed_elems(N, C, H, W), out_b = sizeof(float) * packed_elems(N, K, H, W);
     const struct { const void *p; size_t n; } read[] = {
         {in, in_b}, {w_blk, sizeof(float) * small_conv_weight_elems(C, K, 1, 1, math)}, {bias, sizeof(float) * K},
         {packed, sizeof(float) * small_adapter_elems(adapters, C, K, R)}, {adapter, sizeof(int32_t) * N}, {scale, sizeof(float) * adapters}};
     for (const auto &r : read)
-        if (r.p && (ranges_overlap(r.p, r.n, out, out_b) || ranges_overlap(r.p, r.n, workspace, ws))) return SMALL_ERR_OVERLAP;
-    if (ranges_overlap(out, out_b, workspace, ws)) return SMALL_ERR_OVERLAP;
+        if (r.p && (ranges_overlap(r.p, r.n, out, out_b) || (ws && ranges_overlap(r.p, r.n, workspace, ws)))) return SMALL_ERR_OVERLAP;
+    if (ws && ranges_overlap(out, out_b, workspace, ws)) return SMALL_ERR_OVERLAP;
     const OnDevice on(ctx);
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -186,12 +189,15 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, C, K, H * W, R, kSmCount))
         return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
     if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
-    const bool runs = H * W >= 4;                        // several pixels a warp where an image has them
-    const long long rows = (long long)N * (s.RP / 8), blocks = (long long)N * s.KB;
-    if (runs) launch_kernel(ctx, adapter_down_kernel<4>, dim3(task_blocks(ctx, rows * ceil_div(H * W, 4))), dim3(kThreads), 0, st, a, s);
-    else launch_kernel(ctx, adapter_down_kernel<1>, dim3(task_blocks(ctx, rows * H * W)), dim3(kThreads), 0, st, a, s);
-    if (int e = check_launch(ctx)) return e;
-    if (runs) launch_kernel(ctx, adapter_up_kernel<8>, dim3(task_blocks(ctx, blocks * ceil_div(H * W, 8))), dim3(kThreads), 0, st, a, s);
-    else launch_kernel(ctx, adapter_up_kernel<1>, dim3(task_blocks(ctx, blocks * H * W)), dim3(kThreads), 0, st, a, s);
+    const bool point = H * W < 4;
+    const int runs = point ? H * W : ceil_div(H * W, kRun);
+    if ((long long)N * runs > 0x7fffffff) return SMALL_ERR_SHAPE;
+    // blocks for about two a SM; each takes the products with Down anew, so no more than eight filter blocks' worth apart
+    const int most = ceil_div(s.KB, 8), wanted = (int)((2ll * ctx->sm_count + (long long)N * runs - 1) / ((long long)N * runs));
+    const int filter_blocks = ceil_div(s.KB, wanted < most ? wanted : most);
+    const dim3 grid((unsigned)(N * runs), (unsigned)ceil_div(s.KB, filter_blocks));
+    const size_t t = sizeof(float) * s.RP * (point ? kWarps : kRun);
+    if (point) launch_kernel(ctx, adapter_add_kernel<true>, grid, dim3(kThreads), t, st, a, s, runs, filter_blocks);
+    else launch_kernel(ctx, adapter_add_kernel<false>, grid, dim3(kThreads), t, st, a, s, runs, filter_blocks);
     return check_launch(ctx);
 }

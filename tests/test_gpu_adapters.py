@@ -31,7 +31,7 @@ class Layer:
 
     def workspace(self, N, H, W):
         need = B.small_adapted_conv2d_workspace_bytes(N, self.C, self.K, H, W, self.R)
-        return torch.full((need // 4,), float("nan"), device="cuda")
+        return torch.full((max(4, need // 4),), float("nan"), device="cuda")
 
     def run(self, x, ids, mode, relu=False, before=None):
         N, _, H, W = x.shape
