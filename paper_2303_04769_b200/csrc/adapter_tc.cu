@@ -482,10 +482,14 @@ __global__ void __launch_bounds__(kThreads) pack_halves_kernel(const float *__re
 
 }  // namespace
 
-bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms) {
-    (void)C; (void)R;
+// The other form writes the result twice and takes the adapter's products in FP32, which costs the more the larger the rank; this one lays the
+// pixels out first.  us, here / there, batch 64 unless said, rank 8 and 32: 256 -> 768 on 28 x 28 126 / 222 and 128 / 376; 256 -> 256 87 / 103 and 87 /
+// 213; 128 -> 128 43 / 42 and 44 / 92; 64 -> 64 29 / 26 and 29 / 55; 256 -> 256 on 14 x 14 35 / 30 and 36 / 56; 512 -> 128 63 / 41 and 74 / 82; batch
+// 128, 512 -> 512 125 / 148 and 139 / 249, on 8 x 8 71 / 58 and 76 / 127; batch 4, 320 -> 960 on 32 x 32 45 / 37 and 46 / 69.
+bool adapted_tc_preferred(int N, int K, int HW, int R, int sms) {
     const long long tiles = (long long)N * ceil_div(HW, kTile) * ceil_div(blocks_of(K), kFilterTile);
-    return HW >= 64 && tiles >= sms / 2 && tiles < (1 << 28);
+    if (HW < 64 || tiles >= (1 << 28)) return false;
+    return R > 8 ? tiles >= sms / 2 : K > 128 && tiles >= 2 * sms;
 }
 
 size_t adapted_tc_workspace(int N, int C, int K, int HW, int R) { return Layout(N, C, K, HW, R).bytes; }

@@ -88,7 +88,7 @@ def test_attention():
             assert attend(**{name: at(4)}, **large) == OVERLAP
 
 
-def adapt(ctx=CTX, x=at(0), w=at(1), b=at(2), packed=at(3), ids=at(4), scale=at(5), out=at(6), ws=at(7), N=80, C=64, K=96, H=8, W=8, R=8, A=4,
+def adapt(ctx=CTX, x=at(0), w=at(1), b=at(2), packed=at(3), ids=at(4), scale=at(5), out=at(6), ws=at(7), N=80, C=64, K=96, H=8, W=8, R=9, A=4,
           flags=B.MATH_3XTF32 if B else 0):
     return status(B.small_adapted_conv2d, ctx, x, w, b, packed, ids, scale, out, ws, N, C, K, H, W, R, A, flags, STREAM)
 
@@ -99,8 +99,8 @@ def test_adapters():
         assert adapt(**{name: None}) == INVALID and adapt(**{name: at(9) + 4}) == ALIGN
     for name in ("b", "scale", "ws"):
         assert adapt(**{name: at(9) + 4}) == ALIGN
-    assert adapt(ws=None) == WORKSPACE and B.small_adapted_conv2d_workspace_bytes(80, 64, 96, 8, 8, 8) > 0
-    assert B.small_adapted_conv2d_workspace_bytes(2, 64, 96, 8, 8, 8) == 0 and adapt(ws=None, N=2) not in (WORKSPACE, INVALID)        # not needed: gets as far as the device
+    assert adapt(ws=None) == WORKSPACE and B.small_adapted_conv2d_workspace_bytes(80, 64, 96, 8, 8, 9) > 0
+    assert B.small_adapted_conv2d_workspace_bytes(2, 64, 96, 8, 8, 9) == 0 and adapt(ws=None, N=2) not in (WORKSPACE, INVALID)        # not needed: gets as far as the device
     assert adapt(flags=B.SILU) == INVALID and adapt(flags=B.RELU_MID) == INVALID and adapt(flags=3 << 4) == INVALID
     for bad in (dict(N=0), dict(C=0), dict(K=0), dict(H=0), dict(W=0), dict(R=0), dict(R=129), dict(A=0), dict(H=1 << 13, W=1 << 12)):
         assert adapt(**bad) == SHAPE

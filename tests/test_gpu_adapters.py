@@ -51,7 +51,7 @@ SHAPES = [  # N, C, K, H, W, rank, adapters
     (1, 1, 1, 1, 1, 1, 1), (8, 512, 512, 1, 1, 8, 16), (3, 64, 64, 1, 1, 128, 2), (33, 96, 40, 1, 1, 4, 5), (130, 64, 128, 1, 1, 16, 7), (4, 96, 130, 13, 14, 5, 7),
     (2, 128, 128, 28, 28, 16, 3), (5, 40, 200, 7, 7, 33, 4), (2, 31, 33, 5, 9, 3, 2), (1, 256, 768, 14, 14, 64, 2), (3, 64, 96, 31, 29, 20, 9), (6, 320, 64, 3, 3, 8, 3),
     (1, 100, 300, 56, 56, 16, 1), (2, 32, 32, 1, 300, 100, 2), (9, 200, 1000, 1, 1, 16, 4),
-    (40, 70, 300, 12, 11, 17, 6), (90, 33, 45, 8, 9, 128, 3), (75, 160, 64, 16, 16, 48, 80)]
+    (40, 70, 300, 12, 11, 17, 6), (90, 33, 45, 8, 9, 128, 3), (75, 160, 64, 16, 16, 48, 80), (150, 64, 200, 10, 13, 5, 9)]
 
 
 @pytest.mark.parametrize("mode", MODES)
