@@ -3,8 +3,9 @@
 // The rows that share a key head - its query heads times the queries, R of them a block - are held in registers, and so are their sums.  Eight
 // lanes take a key's channels, 128 bytes a load; a warp's four such groups and a block's eight warps walk the keys side by side, each
 // group with a running maximum of its own.  Loads go through shared memory, where each thread copies what it will read itself: two of three
-// stages of 128 bytes a thread are under way while it works on the third, 128 KB for the two blocks of an SM, without a register or a
-// barrier for them (with as many loads held in registers, one block fitting an SM: 57 us against the figure below).  A cluster of up to 16 blocks shares out the keys; what groups, warps and blocks have found is joined by their maxima.
+// stages of 128 bytes a thread are under way while it works on the third, without a register or a barrier for them, in two blocks an SM (six
+// stages in one block: 30 us for the 75 MB below, loads held in registers 57).  A cluster of up to 16 blocks shares out the keys; what groups, warps
+// and blocks have found is joined by their maxima.  Batch 4, 4 key heads of 64 for 8 heads, 96 x 96: 75 MB in 23 us, 3.3 TB/s; 16 of 56 x 56: 4.5 TB/s.
 #include "attention.cuh"
 
 namespace small {
@@ -234,9 +235,12 @@ int launch(small_ctx *ctx, FewArgs f, cudaStream_t st) {
     if (int s = allow_shared_memory(ctx, attention_few_kernel<DP, R, kGeneral>, roomy, kRing)) return s;
     f.groups = ceil_div(f.rows, R);
     if ((long long)f.a.kv_heads * f.groups > 65535) return launch_attention_fp32(ctx, f.a, st);          // a grid's limit
-    // blocks for about two a SM, each with work for its groups
+    // up to eight blocks a cluster while they are fewer than the SMs and have some rounds each, sixteen where even so most SMs would be idle: those
+    // start together only where an eighth of the GPU is free (us, 8 / 16: batch 2, 8 heads of 64, 56 x 56 12.6 / 16.3, batch 4, 4 heads, 96 x 96 23.0 / 24.7,
+    // one image and head 15.2 / 10.4)
     f.splits = 1;
-    while (f.splits < kMostSplits && (long long)f.a.N * f.a.kv_heads * f.groups * f.splits <= kSmCount && f.a.KP >= f.splits * 2 * 64) f.splits *= 2;
+    auto blocks = [&] { return (long long)f.a.N * f.a.kv_heads * f.groups * f.splits; };
+    while (f.splits < kMostSplits && blocks() <= (f.splits < 8 ? kSmCount : kSmCount / 4) && f.a.KP >= f.splits * 2 * 64) f.splits *= 2;
     launch_clusters(ctx, attention_few_kernel<DP, R, kGeneral>, dim3((unsigned)f.splits, (unsigned)(f.a.kv_heads * f.groups), (unsigned)f.a.N), dim3(kThreads), f.splits, kRing, st, f);
     return check_launch(ctx);
 }
