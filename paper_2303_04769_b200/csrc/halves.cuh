@@ -29,19 +29,17 @@ __device__ __forceinline__ uint32_t pack_halves(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// Two floats -> their leading halves and what these leave.
-__device__ __forceinline__ void split(float a, float b, uint32_t &hi, uint32_t &lo) {
-    const float ah = __uint_as_float(__float_as_uint(a) & 0xffffe000u), bh = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
+// Two operands -> the nearest halves (off by at most 2^-12 of the value) and what these leave.  What is left of a value that is not finite
+// is 0, or it would turn infinities into NaN in every product.
+__device__ __forceinline__ float nearest_half(float x) { return __uint_as_float((__float_as_uint(x) + 0x1000u) & 0xffffe000u); }        // |x| < 65488
+__device__ __forceinline__ void split_finite(float a, float b, uint32_t &hi, uint32_t &lo) {
+    const float ah = nearest_half(a), bh = nearest_half(b);
     hi = pack_halves(ah, bh);
     lo = pack_halves(a - ah, b - bh);
-}
-// The same for operands: what is left of a value that is not finite is 0, or it would turn infinities into NaN in every product.
-__device__ __forceinline__ void split_finite(float a, float b, uint32_t &hi, uint32_t &lo) {
-    split(a, b, hi, lo);
-    if (!(fabsf(a) <= 65504.0f) || !(fabsf(b) <= 65504.0f)) {
-        const float ah = __uint_as_float(__float_as_uint(a) & 0xffffe000u), bh = __uint_as_float(__float_as_uint(b) & 0xffffe000u);
-        hi = pack_halves(fabsf(a) <= 65504.0f ? ah : a, fabsf(b) <= 65504.0f ? bh : b);
-        lo = pack_halves(fabsf(a) <= 65504.0f ? a - ah : 0.0f, fabsf(b) <= 65504.0f ? b - bh : 0.0f);
+    const bool a_in = fabsf(a) < 65488.0f, b_in = fabsf(b) < 65488.0f;
+    if (!a_in || !b_in) {
+        hi = pack_halves(a_in ? ah : a, b_in ? bh : b);
+        lo = pack_halves(a_in ? a - ah : 0.0f, b_in ? b - bh : 0.0f);
     }
 }
 
