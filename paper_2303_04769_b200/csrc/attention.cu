@@ -135,13 +135,22 @@ bool attention_shape_ok(int N, int heads, int kv_heads, int D, int QH, int QW, i
     return N <= 65535 && heads <= 65535 && ((long long)QH + KH) * ((long long)QW + KW) <= (1ll << 30);
 }
 
-// Which kernel.  Few queries: theirs, in every math mode (8 heads of 64, 28 x 28 keys, batch 8: 16 queries 27.6 us, on the tensor cores some 28;
-// one query 10).  In the tensor-core modes the tensor cores from there on (17 queries 28 us, in FP32 123), but where all of an image is one tile of
-// the FP32 kernel and those tiles are more than the SMs (7 x 7, 8 heads, us, FP32 / tensor cores: 64 channels batch 4 16.2 / 11.4, 16 16.5 / 15.9, 32
-// 25.3 / 25.9, 128 60.5 / 89.3; 32 channels batch 16 11.6 / 12.1, 32 14.4 / 21.6, 128 35.1 / 65.7).
-bool on_tensor_cores(int N, int heads, int QP, int KP, unsigned math) {
-    if (math == SMALL_MATH_FP32 || QP <= kFewQueries) return false;
-    return QP > kRows || KP > kKeys || (long long)N * heads <= kSmCount;
+// Which kernel (us, 4 heads unless said, with a bias).
+//   Few queries (8 heads of 64): where a row's keys are long, the kernel that streams them (196 keys, batch 2, 4 rows a key head 7.3, in shared memory
+//   8.7; batch 32 11.9 and 16.9; 7 heads of 96, 88 keys, one row, batch 8 7.3 and 11.2), with more rows or few keys shared memory (8 rows 9.8 and 8.9, 16 rows batch 32 44.7 and 17.9; one row of 100 keys 7.5 and 6.4).
+//   More queries, FP32: shared memory wherever it holds the keys (144 keys of 128 channels, batch 128 708 and 312; of 64, batch 2 36 and 12).
+//   In the tensor-core modes those kernels' two launches cost 10 at least.  Where queries and keys fit one of their tiles, half empty then, shared memory at
+//   any batch (49 pixels, 64 channels: batch 2 11.0 and 6.2, 128 40.8 and 25.4); else up to some 48 M multiply-adds of whole tiles (72 pixels, 64
+//   channels: batch 16, 38 M, 12.5 and 11.7, 32 16.7 and 16.8; 196 pixels: 64 channels batch 4, 51 M, 16.4 and 14.6, 32 channels batch 8, 51 M, 13.1 and 14.5).
+enum class Kernel { few, small, tensor_cores, fp32 };
+
+Kernel kernel_of(int N, int heads, int kv_heads, int D, int QP, int KP, unsigned math) {
+    const bool holds = attention_small_bytes(D, KP) <= kSmallShared;
+    const int lanes = D <= 32 ? 32 : D <= 64 ? 64 : 128;             // channels as the kernels hold them
+    if (QP <= kFewQueries) return holds && ((KP <= 128 && KP * lanes <= 8192) || QP * (heads / kv_heads) > 4) ? Kernel::small : Kernel::few;
+    const double work = (double)N * heads * QP * (ceil_div(KP, 64) * 64.0) * lanes;
+    if (holds && (math == SMALL_MATH_FP32 || (QP <= 64 && KP <= 64) || work <= 48e6)) return Kernel::small;
+    return math == SMALL_MATH_FP32 ? Kernel::fp32 : Kernel::tensor_cores;
 }
 
 }  // namespace
@@ -156,7 +165,7 @@ using namespace small;
 
 SMALL_API size_t small_attention_workspace_bytes(int N, int heads, int kv_heads, int D, int QH, int QW, int KH, int KW, unsigned math) {
     if (!attention_shape_ok(N, heads, kv_heads, D, QH, QW, KH, KW) || (math & ~SMALL_MATH_MASK) || !one_math_mode(math)) return 0;
-    return on_tensor_cores(N, heads, QH * QW, KH * KW, math) ? attention_tc_workspace(N, kv_heads, D, KH * KW) : 0;
+    return kernel_of(N, heads, kv_heads, D, QH * QW, KH * KW, math) == Kernel::tensor_cores ? attention_tc_workspace(N, kv_heads, D, KH * KW) : 0;
 }
 
 SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, const float *v, const float *bias, const int32_t *q_extents,
@@ -193,6 +202,10 @@ SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, co
     const AttnArgs a{q, k, v, bias, q_extents, k_extents, out, workspace, N, heads, kv_heads, D, QH, QW, KH, KW, QP, KP, blocks_of(heads * D),
                      q_stride, k_stride, v_stride, scale, cap, QW + KW - 1};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (on_tensor_cores(N, heads, QP, KP, flags)) return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
-    return QP <= kFewQueries ? launch_attention_few(ctx, a, st) : launch_attention_fp32(ctx, a, st);
+    switch (kernel_of(N, heads, kv_heads, D, QP, KP, flags)) {
+    case Kernel::tensor_cores: return launch_attention_tc(ctx, a, (flags & SMALL_MATH_MASK) == SMALL_MATH_3XTF32, st);
+    case Kernel::few: return launch_attention_few(ctx, a, st);
+    case Kernel::small: return launch_attention_small(ctx, a, st);
+    default: return launch_attention_fp32(ctx, a, st);
+    }
 }

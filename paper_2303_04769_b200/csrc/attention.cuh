@@ -55,6 +55,10 @@ __device__ __forceinline__ float4 load4(const float *x, int first, int c, int D,
     return v;
 }
 
+__device__ __forceinline__ void copy16_or_clear(uint32_t to, const float *from, bool some) {        // 16 bytes to shared memory, zeros where there are none
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(some ? 16 : 0) : "memory");
+}
+
 // cap * tanh(x / cap).  Below 1/2 by Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + x^2 / (7 + x^2 / 9)))), whose
 // relative error there is some x^10 / 1e7, 1e-10; above as (e - 1) / (e + 1), e = exp(2 x), where neither is a small difference.
 __device__ __forceinline__ float capped(float x, float cap, float over_cap) {
@@ -70,6 +74,10 @@ int launch_attention_fp32(small_ctx *, const AttnArgs &, cudaStream_t);
 // attention_few.cu: few queries; a row is a query of a head that shares its keys
 constexpr int kFewQueries = 16;
 int launch_attention_few(small_ctx *, const AttnArgs &, cudaStream_t);
+// attention_small.cu: a head's keys and values in a block's shared memory, and how much of it that takes
+constexpr size_t kSmallShared = 220 * 1024;
+size_t attention_small_bytes(int D, int KP);
+int launch_attention_small(small_ctx *, const AttnArgs &, cudaStream_t);
 // attention_tc.cu: the tensor-core form, and the workspace it takes
 size_t attention_tc_workspace(int N, int kv_heads, int D, int KP);
 int launch_attention_tc(small_ctx *, const AttnArgs &, bool x3, cudaStream_t);

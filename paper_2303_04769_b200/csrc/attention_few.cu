@@ -17,10 +17,6 @@ constexpr int kStages = 3;
 constexpr int kMostSplits = 16;
 constexpr size_t kRing = (size_t)kWarps * kStages * 8 * 32 * sizeof(float4);
 
-__device__ __forceinline__ void copy_or_clear(uint32_t to, const float *from, bool some) {          // zeros where there are none
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(some ? 16 : 0) : "memory");
-}
-
 struct FewArgs {
     AttnArgs a;
     int rows, groups, splits;                            // rows of a key head, groups of R of them, blocks of a cluster
@@ -84,8 +80,8 @@ __global__ void __launch_bounds__(kThreads, R * DP >= 512 ? 1 : 2) attention_few
 #pragma unroll
             for (int c = 0; c < kVec; ++c) {
                 const bool some = in && c * 32 + c0 < a.D;
-                copy_or_clear(mine_s + ((stage * 2 + 0) * 4 + u * kVec + c) * 512, kc[c] + (size_t)p * 32, some);
-                copy_or_clear(mine_s + ((stage * 2 + 1) * 4 + u * kVec + c) * 512, vc[c] + (size_t)p * 32, some);
+                copy16_or_clear(mine_s + ((stage * 2 + 0) * 4 + u * kVec + c) * 512, kc[c] + (size_t)p * 32, some);
+                copy16_or_clear(mine_s + ((stage * 2 + 1) * 4 + u * kVec + c) * 512, vc[c] + (size_t)p * 32, some);
             }
         }
         copy_commit();
