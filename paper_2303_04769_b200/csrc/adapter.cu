@@ -28,17 +28,17 @@ __global__ void __launch_bounds__(kThreads) pack_adapters_kernel(const float *__
     }
 }
 
-// out = act(out + scale Up (Down x)) behind the convolution that has written `out`: a block takes up to 32 pixels of an image (kPoint: one) and a
+// out = act(out + scale Up (Down x)) behind the convolution that has written `out`: a block takes a run of up to 32 pixels of an image (kPoint: one) and a
 // run of filter blocks.  The products with Down, t, come first, from what is older than the convolution: they are taken while it runs.
 // For them a warp takes four pixels and eight ranks, a lane a channel of each block, so that every load is a whole line and serves four or
 // eight products; one pixel's channel blocks are dealt out to the warps.  Then a warp takes a filter block, a lane a filter.
-constexpr int kRun = 32;                 // pixels of a block
+constexpr int kMostRun = 32;             // pixels of a block
 
 template <bool kPoint>
-__global__ void __launch_bounds__(kThreads) adapter_add_kernel(const AdaptArgs a, const AdapterShape s, int runs, int filter_blocks) {
+__global__ void __launch_bounds__(kThreads) adapter_add_kernel(const AdaptArgs a, const AdapterShape s, int run, int runs, int filter_blocks) {
     extern __shared__ float t_s[];                       // [pixels][RP], kPoint: [warps][RP]
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockIdx.x / runs, p0 = blockIdx.x % runs * (kPoint ? 1 : kRun);
-    const int pixels = kPoint ? 1 : min(kRun, a.HW - p0), id = a.adapter[n];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockIdx.x / runs, p0 = blockIdx.x % runs * run;
+    const int pixels = kPoint ? 1 : min(run, a.HW - p0), id = a.adapter[n];
     const bool some = id >= 0 && id < a.adapters;
     if (some) {
         const float *x = a.in + ((size_t)n * s.CB * a.HW + p0) * 32 + lane, *w = a.packed + id * s.down + lane;
@@ -188,16 +188,19 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     const AdaptArgs a{in, w_blk, bias, packed, scale, adapter, out, workspace, N, H * W, adapters, (flags & SMALL_RELU) != 0, (flags & SMALL_ACCUMULATE) != 0};
     if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, K, H * W, R, kSmCount))
         return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
-    if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
     const bool point = H * W < 4;
-    const int runs = point ? H * W : ceil_div(H * W, kRun);
-    if ((long long)N * runs > 0x7fffffff) return SMALL_ERR_SHAPE;
-    // blocks for about two a SM; each takes the products with Down anew, so no more than eight filter blocks' worth apart
-    const int most = ceil_div(s.KB, 8), wanted = (int)((2ll * ctx->sm_count + (long long)N * runs - 1) / ((long long)N * runs));
-    const int filter_blocks = ceil_div(s.KB, wanted < most ? wanted : most);
+    if ((long long)N * ceil_div(H * W, point ? 1 : 8) > 0x7fffffff) return SMALL_ERR_SHAPE;
+    if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
+    // Blocks for the SMs: shorter runs while they are few, then, up to two a SM, fewer filter blocks each, at least eight apart, as each takes the products
+    // with Down anew.  us, runs of 32 / 16 / 8: 93 -> 280, rank 43, 6 x 46, batch 6 32.1 / 20.6 / 14.5; 256 -> 256, rank 64, 14 x 14, batch 1 39.8 /
+    // 22.8 / 14.4; 183 -> 237, rank 2, 5 x 5, batch 64 12.9 / 11.9 / 14.1.
+    int run = point ? 1 : kMostRun;
+    while (run > 8 && (long long)N * ceil_div(H * W, run) < ctx->sm_count * 3 / 4) run /= 2;
+    const int runs = ceil_div(H * W, run), most = ceil_div(s.KB, 8), more = (int)std::max(1ll, 2ll * ctx->sm_count / ((long long)N * runs));
+    const int filter_blocks = ceil_div(s.KB, more < most ? more : most);
     const dim3 grid((unsigned)(N * runs), (unsigned)ceil_div(s.KB, filter_blocks));
-    const size_t t = sizeof(float) * s.RP * (point ? kWarps : kRun);
-    if (point) launch_kernel(ctx, adapter_add_kernel<true>, grid, dim3(kThreads), t, st, a, s, runs, filter_blocks);
-    else launch_kernel(ctx, adapter_add_kernel<false>, grid, dim3(kThreads), t, st, a, s, runs, filter_blocks);
+    const size_t t = sizeof(float) * s.RP * (point ? kWarps : run);
+    if (point) launch_kernel(ctx, adapter_add_kernel<true>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
+    else launch_kernel(ctx, adapter_add_kernel<false>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
     return check_launch(ctx);
 }
