@@ -11,6 +11,9 @@
 // adapter_product_kernel: a block walks tiles of 128 pixels x 256 filters; warps for loading (plain bulk copies, two stages of 96 KB), MMAs
 //   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
+//
+// Batch 64, 256 -> 768, 28 x 28, rank 16: 136 us.  Pixels 47 (the filters, 13, beside them): waits for loads, twice over 51 MB.  Product 80: MMAs 53 % of the
+// time, the rest a stage waits for its load.  Floor 33 for the bytes, 37 for three products.
 #include "adapter.cuh"
 #include "halves.cuh"
 

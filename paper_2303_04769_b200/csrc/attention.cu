@@ -136,12 +136,14 @@ bool attention_shape_ok(int N, int heads, int kv_heads, int D, int QH, int QW, i
 }
 
 // Which kernel (us, 4 heads unless said, with a bias).
-//   Few queries (8 heads of 64): where a row's keys are long, the kernel that streams them (196 keys, batch 2, 4 rows a key head 7.3, in shared memory
-//   8.7; batch 32 11.9 and 16.9; 7 heads of 96, 88 keys, one row, batch 8 7.3 and 11.2), with more rows or few keys shared memory (8 rows 9.8 and 8.9, 16 rows batch 32 44.7 and 17.9; one row of 100 keys 7.5 and 6.4).
+//   Few queries (8 heads of 64): where a row's keys are long, the kernel that streams them (196 keys, batch 2, 4 rows a key head 7.3, in shared
+//   memory 8.7; batch 32 11.9 and 16.9; 7 heads of 96, 88 keys, one row, batch 8 7.3 and 11.2), with more rows or few keys shared memory (8 rows
+//   9.8 and 8.9, 16 rows batch 32 44.7 and 17.9; one row of 100 keys 7.5 and 6.4).
 //   More queries, FP32: shared memory wherever it holds the keys (144 keys of 128 channels, batch 128 708 and 312; of 64, batch 2 36 and 12).
-//   In the tensor-core modes those kernels' two launches cost 10 at least.  Where queries and keys fit one of their tiles, half empty then, shared memory at
-//   any batch (49 pixels, 64 channels: batch 2 11.0 and 6.2, 128 40.8 and 25.4); else up to some 48 M multiply-adds of whole tiles (72 pixels, 64
-//   channels: batch 16, 38 M, 12.5 and 11.7, 32 16.7 and 16.8; 196 pixels: 64 channels batch 4, 51 M, 16.4 and 14.6, 32 channels batch 8, 51 M, 13.1 and 14.5).
+//   In the tensor-core modes those kernels' two launches cost 10 at least.  Where queries and keys fit one of their tiles, half empty then, shared
+//   memory at any batch (49 pixels, 64 channels: batch 2 11.0 and 6.2, 128 40.8 and 25.4); else up to some 48 M multiply-adds of whole tiles (72
+//   pixels, 64 channels: batch 16, 38 M, 12.5 and 11.7, 32 16.7 and 16.8; 196 pixels: 64 channels batch 4, 51 M, 16.4 and 14.6, 32 channels
+//   batch 8, 51 M, 13.1 and 14.5).
 enum class Kernel { few, small, tensor_cores, fp32 };
 
 Kernel kernel_of(int N, int heads, int kv_heads, int D, int QP, int KP, unsigned math) {

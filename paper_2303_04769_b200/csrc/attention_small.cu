@@ -4,7 +4,8 @@
 // A block holds the keys and values of one key head and takes a share of its rows (queries of the heads that read them).  A warp takes four
 // rows at a time: two keys a lane for the scores, which go through shared memory; then eight keys of each row for the bias, the cap, the
 // maximum and the weights, every score being known; then eight lanes a key's channels for the sums, four keys at a time.  Few instructions matter
-// more than any of this: what a block runs once it fetches from L2 first (with all four rows unrolled 14 us where this takes 10).
+// more than any of this: what a block runs once it fetches from L2 first (2 x 3 planes: four rows' cap and
+// bias unrolled 10 us, now 4.6).  8 heads of 64, 7 x 7 with a bias: batch 8 6.7 us, 64 25.6.
 #include "attention.cuh"
 
 namespace small {

@@ -9,11 +9,14 @@
 // block instead would repeat it that many times beside the softmax, which is what bounds the main kernel.
 //
 // attention_tc_kernel: a block takes one or two tiles of 128 queries of a head.  One warp loads tiles, one issues MMAs, four (eight)
-// do the softmax of each query tile.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128
-// columns); a thread takes a row (two share it where the result has 128 channels) and writes the weights as halves over the scores, where
-// they are the second product's A operand.  While one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values starts from zero and is
-// added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
+// do the softmax of each query tile.  Scores lie in three rotating buffers of tensor memory (128 lanes x 128 columns); a thread takes a
+// row (two share it where the result has 128 channels) and writes the weights as halves over the scores, where they are the second
+// product's A operand.  While one tile's softmax runs, the tensor cores work on the other's.  Each key tile's product with the values
+// starts from zero and is added to the thread's own FP32 sums: the tensor core's accumulator is cut off, not rounded, at each step, which over
 // thousands of keys would add up (5e-8 a step), and no rescaling of tensor memory is needed when the maximum grows.
+//
+// Bound by the softmax: a table entry, an exponential, the split into halves and two crossings of tensor memory a score.  Batch 4, 8 heads of 64,
+// 56 x 56 with a bias: 362 us (tiles 19 of them), 223 TFLOP/s of the formula's operations; the three products alone would take 148.
 #include <type_traits>
 
 #include "attention.cuh"
