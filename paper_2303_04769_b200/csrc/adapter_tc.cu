@@ -289,7 +289,8 @@ constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, k
 template <bool kX3>
 __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(const TcArgs c) {
     extern __shared__ char raw[];
-    __shared__ uint64_t full_s[kStages], empty_s[kStages], done_s[2], free_s[2], drained;
+    __shared__ uint64_t full_s[kStages * 2], empty_s[kStages],        // a stage: what the first term takes, the rest
+                         done_s[2], free_s[2], drained;
     __shared__ uint32_t tmem_s;
     __shared__ int gave_up;
     const AdaptArgs &a = c.a;
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     if (warp == 9) tmem_alloc(smem_u32(&tmem_s), 512);
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (int i = 0; i < kStages; ++i) { mbar_init(full + i * 8, 1); mbar_init(empty + i * 8, 1); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(full + i * 16, 1); mbar_init(full + i * 16 + 8, 1); mbar_init(empty + i * 8, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(done + i * 8, 1); mbar_init(free + i * 8, 256); }
         mbar_init(smem_u32(&drained), 1);
         mbar_fence_init();
@@ -330,14 +331,28 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
             for (int k = 0; k < c.s.chunks + ranks; ++k) {
                 if (issued >= kStages && !(ok = mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit))) break;
                 const int rb = k - c.s.chunks;
-                // high parts lie in front: without the low ones half of a chunk is enough (32 ranks have both in a row)
-                const uint32_t nx = rb >= 0 ? kRankBytes : kX3 ? kPixelBytes : kPixelBytes / 2, nw = rb >= 0 ? rows * 128 : kX3 ? rows * 256 : rows * 128;
                 if (elect_one()) {
-                    const uint32_t to = smem_u32(stages + slot * kStageBytes);
-                    mbar_expect_tx(full + slot * 8, nx + nw);
-                    const char *fx = rb >= 0 ? t + (size_t)rb * kRankBytes : x + (size_t)k * kPixelBytes, *fw = rb >= 0 ? u + (size_t)rb * rows * 128 : w + (size_t)k * rows * 256;
-                    for (uint32_t e = 0; e < nx; e += 8192) bulk_load(to + e, fx + e, min(8192u, nx - e), full + slot * 8);
-                    for (uint32_t e = 0; e < nw; e += 8192) bulk_load(to + kPixelBytes + e, fw + e, min(8192u, nw - e), full + slot * 8);
+                    const uint32_t to = smem_u32(stages + slot * kStageBytes), bar = full + slot * 16;
+                    auto load = [&](uint32_t at, const char *from, uint32_t bytes, uint32_t b) {
+                        for (uint32_t e = 0; e < bytes; e += 8192) bulk_load(to + at + e, from + e, min(8192u, bytes - e), b);
+                    };
+                    if (rb >= 0) {                       // 32 ranks have both parts in a row
+                        mbar_expect_tx(bar, kRankBytes + rows * 128);
+                        load(0, t + (size_t)rb * kRankBytes, kRankBytes, bar);
+                        load(kPixelBytes, u + (size_t)rb * rows * 128, rows * 128, bar);
+                        if (kX3) mbar_arrive(bar + 8);
+                    } else {                             // high parts lie in front; the terms begin with low pixels and high filters
+                        const char *fx = x + (size_t)k * kPixelBytes, *fw = w + (size_t)k * rows * 256;
+                        const uint32_t half = kPixelBytes / 2;
+                        mbar_expect_tx(bar, half + rows * 128);
+                        load(kX3 ? half : 0, kX3 ? fx + half : fx, half, bar);
+                        load(kPixelBytes, fw, rows * 128, bar);
+                        if (kX3) {
+                            mbar_expect_tx(bar + 8, half + rows * 128);
+                            load(0, fx, half, bar + 8);
+                            load(kPixelBytes + rows * 128, fw + rows * 128, rows * 128, bar + 8);
+                        }
+                    }
                 }
                 __syncwarp();
                 ++issued;
@@ -353,16 +368,24 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
             const uint32_t desc = f16_desc(rows), d = tmem + buffer * 256;
             if (turn >= 2 && !(ok = mbar_wait_uniform(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
             for (int k = 0; k < c.s.chunks + ranks; ++k) {
-                if (!(ok = mbar_wait_uniform(full + slot * 8, phase, stop, c.status, c.limit))) break;
+                const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
+                if (!(ok = mbar_wait_uniform(full + slot * 16, phase, stop, c.status, c.limit))) break;
                 tc_fence_after();
+                if (kX3) {                               // small terms first: low pixels and high filters while the rest is on its way
+                    if (k < c.s.chunks && elect_one())
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mma_f16(d, x + e * 2 + kPixelBytes / 32, w + e * 2, desc, k > 0 || e > 0);
+                    __syncwarp();
+                    if (!(ok = mbar_wait_uniform(full + slot * 16 + 8, phase, stop, c.status, c.limit))) break;
+                    tc_fence_after();
+                }
                 if (elect_one()) {
-                    const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
                     if (k < c.s.chunks) {
 #pragma unroll
-                        for (int term = kX3 ? 0 : 2; term < 3; ++term)           // small terms first
+                        for (int term = kX3 ? 1 : 2; term < 3; ++term)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                mma_f16(d, x + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), w + e * 2 + (term == 1 ? rows * 8 : 0), desc, k > 0 || e > 0 || term > (kX3 ? 0 : 2));
+                                mma_f16(d, x + e * 2, w + e * 2 + (term == 1 ? rows * 8 : 0), desc, kX3 || k > 0 || e > 0);
                     } else {
                         const int steps = (min(s.R - (k - c.s.chunks) * 32, 32) + 15) / 16;
 #pragma unroll
@@ -434,7 +457,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     __syncthreads();
     tc_fence_after();
     if (gave_up && warp == 8)                            // what is still on its way must land before the block ends
-        for (int x = max(0, issued - kStages); x < issued; ++x) mbar_wait(full + x % kStages * 8, (x / kStages) & 1, kDefaultWaitIters);
+        for (int x = max(0, issued - kStages); x < issued; ++x)
+            for (int y = 0; y < (kX3 ? 2 : 1); ++y) mbar_wait(full + x % kStages * 16 + y * 8, (x / kStages) & 1, kDefaultWaitIters);
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 

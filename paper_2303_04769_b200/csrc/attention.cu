@@ -147,7 +147,7 @@ bool attention_shape_ok(int N, int heads, int kv_heads, int D, int QH, int QW, i
 enum class Kernel { few, small, tensor_cores, fp32 };
 
 Kernel kernel_of(int N, int heads, int kv_heads, int D, int QP, int KP, unsigned math) {
-    const bool holds = attention_small_bytes(D, KP) <= kSmallShared;
+    const bool holds = attention_small_bytes(D, KP) <= kSmallShared && (long long)QP * (heads / kv_heads) <= 1 << 30;      // rows are ints there
     const int lanes = D <= 32 ? 32 : D <= 64 ? 64 : 128;             // channels as the kernels hold them
     if (QP <= kFewQueries) return holds && ((KP <= 128 && KP * lanes <= 8192) || QP * (heads / kv_heads) > 4) ? Kernel::small : Kernel::few;
     const double work = (double)N * heads * QP * (ceil_div(KP, 64) * 64.0) * lanes;
