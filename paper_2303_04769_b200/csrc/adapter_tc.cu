@@ -12,8 +12,9 @@
 //   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
 //
-// Batch 64, 256 -> 768, 28 x 28, rank 16: 136 us.  Pixels 47 (the filters, 13, beside them): waits for loads, twice over 51 MB.  Product 80: MMAs 53 % of the
-// time, the rest a stage waits for its load.  Floor 33 for the bytes, 37 for three products.
+// Batch 64, 256 -> 768, 28 x 28, rank 16: 128 us.  Pixels 48 (the filters, 13, beside them): 20 for the largest values,
+// while memory still takes the result before, then four chunks that wait for their loads.  Product 72: MMAs 58 % of the time, the rest a stage waits
+// for its load.  Floor 33 for the bytes, 37 for three products.
 #include "adapter.cuh"
 #include "halves.cuh"
 
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                     }
                     if (a.relu) y = make_float4(fmaxf(y.x, 0.0f), fmaxf(y.y, 0.0f), fmaxf(y.z, 0.0f), fmaxf(y.w, 0.0f));
                     if (k0 + 4 > s.K) y = make_float4(k0 < s.K ? y.x : 0.0f, k0 + 1 < s.K ? y.y : 0.0f, k0 + 2 < s.K ? y.z : 0.0f, 0.0f);       // +0 in pad lanes
-                    out[u * 32] = y;
+                    __stcs(out + u * 32, y);             // operands are read again, results here not: they leave L2 first (131 -> 128 us)
                 }
                 __syncwarp();
             }
