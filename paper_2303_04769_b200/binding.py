@@ -483,7 +483,7 @@ def small_attention(ctx, q, k, v, out, workspace, workspace_bytes, N, heads, kv_
     """q_plane, k_plane: (rows, columns).  scale: 1 / sqrt(D) where None.  strides: floats between the images of q, k and v (0: a
     tensor of its own).  extents: int32[N][2] tensors of valid rows and columns."""
     _n.small_attention(ctx, q, k, v, bias, q_extents, k_extents, out, workspace, workspace_bytes, N, heads, kv_heads, D, q_plane[0], q_plane[1],
-                       k_plane[0], k_plane[1], strides[0], strides[1], strides[2], D ** -0.5 if scale is None else scale, cap, flags, stream)
+                       k_plane[0], k_plane[1], strides[0], strides[1], strides[2], (D ** -0.5 if D > 0 else 1.0) if scale is None else scale, cap, flags, stream)
 
 
 def small_adapter_elems(adapters, C, K, R):

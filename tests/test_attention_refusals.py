@@ -113,3 +113,8 @@ def test_adapters():
     pack = lambda ctx=CTX, down=at(0), up=at(1), packed=at(2), A=4, C=64, K=96, R=8: status(B.small_pack_adapters, ctx, down, up, packed, A, C, K, R, STREAM)  # noqa: E731
     assert pack(ctx=0) == NOT_INIT and pack(down=None) == INVALID and pack(up=at(1) + 4) == ALIGN and pack(R=0) == SHAPE and pack(A=0) == SHAPE
     assert pack(down=at(2)) == OVERLAP and pack(up=at(2) + 64) == OVERLAP
+
+
+def test_attention_without_channels_and_a_scale():
+    for D in (0, -1):
+        assert attend(D=D, scale=None) == SHAPE
