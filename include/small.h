@@ -422,7 +422,7 @@ int small_pack_adapters(small_ctx *ctx, const float *down, const float *up, floa
                         void *stream);
 /* in: blocked [N][C][H][W]; w_blk: from small_pack_conv_weights(C, K, 1, 1, math); bias: K floats or NULL; adapter: device
  * int32[N]; scale: device float[adapters] or NULL (1); out: blocked [N][K][H][W].  flags: SMALL_RELU, SMALL_ACCUMULATE (out_previous is
- * added in front of the activation) and one SMALL_MATH_* for both parts.  workspace: device, 16-byte aligned,
+ * added in front of the activation) and one SMALL_MATH_* for both parts (few pixels of few channels: FP32 multiply-adds in each).  workspace: device, 16-byte aligned,
  * small_adapted_conv2d_workspace_bytes bytes (operands as halves, scaled by pixel, where the layer runs as one product on the tensor
  * cores; 0 and NULL where it does not in any math mode); calls that may run at the same time need their own.
  * Errors as small_conv2d, and WORKSPACE (needed and NULL). */

@@ -125,6 +125,113 @@ __global__ void __launch_bounds__(kThreads) adapter_add_kernel(const AdaptArgs a
     }
 }
 
+// The whole layer for few pixels, in FP32 whatever the mode: a block takes 32 filters and eight pixels.  The warps share out the filters' channel
+// blocks, a lane a filter, each load serving eight products; before that each warp takes one pixel's t, a lane a channel of each block, and what
+// Up makes of it, a lane a filter.  Bound by the launch and two trips to L2; two dependent launches cost half as much again.
+constexpr int kFew = 8;                  // pixels of a block
+
+__global__ void __launch_bounds__(kThreads) adapted_few_kernel(const AdaptArgs a, const AdapterShape s) {
+    extern __shared__ float4 few_s[];
+    float *x_s = reinterpret_cast<float *>(few_s), *part_s = x_s + s.CB * 32 * kFew, *t_s = part_s + kWarps * kFew * 32;      // [channel][pixel], [warp][pixel][filter], [pixel][RP]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kb = blockIdx.x, m0 = blockIdx.y * kFew, M = a.N * a.HW;
+    grid_dep_sync();
+    grid_dep_trigger();
+    const float *w = a.w + (size_t)kb * s.CB * 1024 + lane;
+    float w_now[32];
+    auto fetch = [&](int cb) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) w_now[c] = cb < s.CB ? w[(size_t)cb * 1024 + c * 32] : 0.0f;
+    };
+    fetch(warp);
+    for (int i = threadIdx.x; i < s.CB * 8 * kFew; i += kThreads) {
+        const int q = i % kFew, c = i / kFew * 4, m = m0 + q;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (m < M) v = *reinterpret_cast<const float4 *>(a.in + (((size_t)(m / a.HW) * s.CB + (c >> 5)) * a.HW + m % a.HW) * 32 + (c & 31));
+        x_s[(c + 0) * kFew + q] = c + 0 < s.C ? v.x : 0.0f; x_s[(c + 1) * kFew + q] = c + 1 < s.C ? v.y : 0.0f;
+        x_s[(c + 2) * kFew + q] = c + 2 < s.C ? v.z : 0.0f; x_s[(c + 3) * kFew + q] = c + 3 < s.C ? v.w : 0.0f;
+    }
+    // this warp's pixel: what its adapter adds to filter `lane`
+    const int m = m0 + warp, n = m / a.HW, id = m < M ? a.adapter[n] : -1;
+    float sum = 0.0f;
+    if (id >= 0 && id < a.adapters) {
+        const float *x = a.in + ((size_t)n * s.CB * a.HW + m % a.HW) * 32 + lane, *down = a.packed + id * s.down + lane;
+        const float *up = a.packed + s.down * a.adapters + id * s.up + (size_t)kb * s.RP * 32 + lane;
+        const float factor = a.scale ? a.scale[id] : 1.0f;
+        float *t = t_s + warp * s.RP;
+        constexpr int kAhead = 8;
+        for (int rg = 0; rg < s.RP; rg += 8) {
+            float acc[8] = {};
+#pragma unroll 1
+            for (int cb = 0; cb < s.CB; cb += kAhead) {  // all of these loads on their way at once (left to the compiler they were not: 14.4 us for 6.9)
+                float v[kAhead], d[kAhead][8];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const bool in = cb + u < s.CB;
+                    v[u] = in && (cb + u) * 32 + lane < s.C ? __ldg(x + (size_t)(cb + u) * a.HW * 32) : 0.0f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) d[u][r] = in ? __ldg(down + ((cb + u) * s.RP + rg + r) * 32) : 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) acc[r] = fmaf(v[u], d[u][r], acc[r]);
+            }
+            // halves of the sums go to halves of the lanes; four lanes end with the same one
+#pragma unroll
+            for (int bit = 16, have = 8; bit; bit /= 2, have /= 2) {
+                const bool upper = lane & bit;
+                if (have > 1) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (u < have / 2) {
+                            const float give = upper ? acc[u] : acc[u + have / 2], keep = upper ? acc[u + have / 2] : acc[u];
+                            acc[u] = keep + __shfl_xor_sync(~0u, give, bit);
+                        }
+                } else {
+                    acc[0] += __shfl_xor_sync(~0u, acc[0], bit);
+                }
+            }
+            if ((lane & 3) == 0) t[rg + lane / 4] = factor * acc[0];
+        }
+        __syncwarp();
+#pragma unroll 8
+        for (int r = 0; r < s.RP; ++r) sum = fmaf(t[r], up[r * 32], sum);
+    }
+    __syncthreads();
+    float acc[kFew] = {};
+    for (int cb = warp; cb < s.CB; cb += kWarps) {
+        float now[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) now[c] = w_now[c];
+        fetch(cb + kWarps);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            const float4 lo = *reinterpret_cast<const float4 *>(x_s + (cb * 32 + c) * kFew), hi = *reinterpret_cast<const float4 *>(x_s + (cb * 32 + c) * kFew + 4);
+            acc[0] = fmaf(now[c], lo.x, acc[0]); acc[1] = fmaf(now[c], lo.y, acc[1]); acc[2] = fmaf(now[c], lo.z, acc[2]); acc[3] = fmaf(now[c], lo.w, acc[3]);
+            acc[4] = fmaf(now[c], hi.x, acc[4]); acc[5] = fmaf(now[c], hi.y, acc[5]); acc[6] = fmaf(now[c], hi.z, acc[6]); acc[7] = fmaf(now[c], hi.w, acc[7]);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < kFew; ++q) part_s[(warp * kFew + q) * 32 + lane] = acc[q];
+    __syncthreads();
+    if (m >= M) return;
+    float *out = a.out + (((size_t)n * s.KB + kb) * a.HW + m % a.HW) * 32 + lane;
+    const int k = kb * 32 + lane;
+    if (k >= s.K) { *out = 0.0f; return; }
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) sum += part_s[(i * kFew + warp) * 32 + lane];
+    if (a.bias) sum += a.bias[k];
+    if (a.accumulate) sum += *out;
+    *out = a.relu && !(sum > 0.0f) ? 0.0f : sum;
+}
+// While its blocks are no more than the SMs, and t is not taken from many rank groups one after the other (us, here / the layer in two launches: one
+// vector or 7 x 7 of four images, 64 -> 64, rank 8 4.4 / 6.4; 128 vectors 256 -> 256, rank 8 5.3 / 6.5, 512 17.6 / 6.8; eight of 512 -> 512, rank 8
+// 7.6 / 6.6, as a plane of 5 x 5 7.7 / 12.1, where the shared product takes longer; 64 -> 512, rank 32 7.0 / 6.5).
+bool few_preferred(int N, int HW, const AdapterShape &s, int sms) {
+    return s.RP <= 24 && s.CB * s.RP <= (HW < 4 ? 64 : 128) && ((long long)N * HW + kFew - 1) / kFew * s.KB <= sms;
+}
+size_t few_bytes(const AdapterShape &s) { return sizeof(float) * (size_t)(s.CB * 32 * kFew + kWarps * kFew * 32 + kFew * s.RP); }       // 26 KB at most
+
 unsigned task_blocks(const small_ctx *ctx, long long tasks) {
     const long long blocks = (tasks + kThreads / 32 - 1) / (kThreads / 32), most = (long long)ctx->sm_count * 16;
     return (unsigned)(blocks < most ? blocks : most);
@@ -188,6 +295,10 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     const AdaptArgs a{in, w_blk, bias, packed, scale, adapter, out, workspace, N, H * W, adapters, (flags & SMALL_RELU) != 0, (flags & SMALL_ACCUMULATE) != 0};
     if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, K, H * W, R, kSmCount))
         return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
+    if (few_preferred(N, H * W, s, ctx->sm_count)) {
+        launch_kernel(ctx, adapted_few_kernel, dim3((unsigned)s.KB, (unsigned)ceil_div(N * H * W, kFew)), dim3(kThreads), few_bytes(s), st, a, s);
+        return check_launch(ctx);
+    }
     const bool point = H * W < 4;
     if ((long long)N * ceil_div(H * W, point ? 1 : 8) > 0x7fffffff) return SMALL_ERR_SHAPE;
     if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
