@@ -34,7 +34,9 @@ __global__ void __launch_bounds__(kThreads) pack_adapters_kernel(const float *__
 // eight products; one pixel's channel blocks are dealt out to the warps.  Then a warp takes a filter block, a lane a filter.
 constexpr int kMostRun = 32;             // pixels of a block
 
-template <bool kPoint>
+// kAhead: channel blocks whose loads are on their way at once (left to the compiler they were not: 16.5 us for 11.9, four images 512 -> 512 on 7 x 7);
+// two cost a block of three an SM, so one where blocks are many (64 images 64 -> 64 on 28 x 28: 24.3 for 26.6).
+template <bool kPoint, int kAhead>
 __global__ void __launch_bounds__(kThreads) adapter_add_kernel(const AdaptArgs a, const AdapterShape s, int run, int runs, int filter_blocks) {
     extern __shared__ float t_s[];                       // [pixels][RP], kPoint: [warps][RP]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockIdx.x / runs, p0 = blockIdx.x % runs * run;
@@ -49,17 +51,24 @@ __global__ void __launch_bounds__(kThreads) adapter_add_kernel(const AdaptArgs a
             float acc[kSums];
 #pragma unroll
             for (int u = 0; u < kSums; ++u) acc[u] = 0.0f;
-#pragma unroll 4
-            for (int cb = kPoint ? warp : 0; cb < s.CB; cb += kPoint ? kWarps : 1) {
-                float v[kPixels];
+            constexpr int kStep = kPoint ? kWarps : 1;
+#pragma unroll 1
+            for (int cb = kPoint ? warp : 0; cb < s.CB; cb += kAhead * kStep) {
+                float v[kAhead][kPixels], u[kAhead][8];
 #pragma unroll
-                for (int q = 0; q < kPixels; ++q) v[q] = q0 + q < pixels && cb * 32 + lane < s.C ? x[((size_t)cb * a.HW + q0 + q) * 32] : 0.0f;
+                for (int h = 0; h < kAhead; ++h) {
+                    const int b = cb + h * kStep;
 #pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const float u = w[(cb * s.RP + rg * 8 + r) * 32];
+                    for (int q = 0; q < kPixels; ++q) v[h][q] = q0 + q < pixels && b * 32 + lane < s.C ? __ldg(x + ((size_t)b * a.HW + q0 + q) * 32) : 0.0f;
 #pragma unroll
-                    for (int q = 0; q < kPixels; ++q) acc[q * 8 + r] = fmaf(v[q], u, acc[q * 8 + r]);
+                    for (int r = 0; r < 8; ++r) u[h][r] = b < s.CB ? __ldg(w + (b * s.RP + rg * 8 + r) * 32) : 0.0f;
                 }
+#pragma unroll
+                for (int h = 0; h < kAhead; ++h)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+#pragma unroll
+                        for (int q = 0; q < kPixels; ++q) acc[q * 8 + r] = fmaf(v[h][q], u[h][r], acc[q * 8 + r]);
             }
             // halves of the sums go to halves of the lanes, until each lane has one (one pixel: four lanes the same one)
             int have = kSums;
@@ -303,15 +312,16 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     if ((long long)N * ceil_div(H * W, point ? 1 : 8) > 0x7fffffff) return SMALL_ERR_SHAPE;
     if (int e = small_conv2d(ctx, in, w_blk, bias, out, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0, flags & ~SMALL_RELU, stream)) return e;
     // Blocks for the SMs: shorter runs while they are few, then, up to two a SM, fewer filter blocks each, at least eight apart, as each takes the products
-    // with Down anew.  us, runs of 32 / 16 / 8: 93 -> 280, rank 43, 6 x 46, batch 6 32.1 / 20.6 / 14.5; 256 -> 256, rank 64, 14 x 14, batch 1 39.8 /
-    // 22.8 / 14.4; 183 -> 237, rank 2, 5 x 5, batch 64 12.9 / 11.9 / 14.1.
+    // with Down anew.  us, runs of 32 / 16 / 8: 93 -> 280, rank 43, 6 x 46, batch 6 26.7 / 17.9 / 15.6; 256 -> 256, rank 64, 14 x 14, batch 1 34.9 /
+    // 19.5 / 11.8; 183 -> 237, rank 2, 5 x 5, batch 64 12.7 / 11.8 / 13.0.
     int run = point ? 1 : kMostRun;
     while (run > 8 && (long long)N * ceil_div(H * W, run) < ctx->sm_count * 3 / 4) run /= 2;
     const int runs = ceil_div(H * W, run), most = ceil_div(s.KB, 8), more = (int)std::max(1ll, 2ll * ctx->sm_count / ((long long)N * runs));
     const int filter_blocks = ceil_div(s.KB, more < most ? more : most);
     const dim3 grid((unsigned)(N * runs), (unsigned)ceil_div(s.KB, filter_blocks));
     const size_t t = sizeof(float) * s.RP * (point ? kWarps : run);
-    if (point) launch_kernel(ctx, adapter_add_kernel<true>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
-    else launch_kernel(ctx, adapter_add_kernel<false>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
+    if (point) launch_kernel(ctx, adapter_add_kernel<true, 4>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
+    else if ((long long)N * runs > 4 * ctx->sm_count) launch_kernel(ctx, adapter_add_kernel<false, 1>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
+    else launch_kernel(ctx, adapter_add_kernel<false, 2>, grid, dim3(kThreads), t, st, a, s, run, runs, filter_blocks);
     return check_launch(ctx);
 }
