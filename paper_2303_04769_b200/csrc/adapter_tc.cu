@@ -158,11 +158,19 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     // the largest value of each pixel: eight lanes take a pixel's 128 bytes, a thread four pixels
     const int r0 = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
     float most[kTile / 32] = {};
-#pragma unroll 2
-    for (int cb = 0; cb < s.CB; ++cb)
+#pragma unroll 1
+    for (int cb = 0; cb < s.CB; cb += 2) {
+        float4 v[2][kTile / 32];
 #pragma unroll
-        for (int i = 0; i < kTile / 32; ++i)
-            if (r0 + i * 32 < pixels) most[i] = fmaxf(most[i], magnitude(*reinterpret_cast<const float4 *>(x + ((size_t)cb * a.HW + r0 + i * 32) * 32 + c0)));
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < kTile / 32; ++i)
+                v[g][i] = r0 + i * 32 < pixels && cb + g < s.CB ? __ldg(reinterpret_cast<const float4 *>(x + ((size_t)(cb + g) * a.HW + r0 + i * 32) * 32 + c0)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < kTile / 32; ++i) most[i] = fmaxf(most[i], magnitude(v[g][i]));
+    }
 #pragma unroll
     for (int i = 0; i < kTile / 32; ++i)
 #pragma unroll
@@ -200,21 +208,10 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
         const bool multiply = some && step < s.chunks, keep = step >= steps - s.chunks;
         float4 v2[2][kTile / 32];                        // on its way while the chunk before is written out and multiplied
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int cb = k * 2 + g, ch = cb * 32 + c0;
-            float4 (&v)[kTile / 32] = v2[g];
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int i = 0; i < kTile / 32; ++i) {
-                const int r = r0 + i * 32;
-                v[i] = r < pixels && cb < s.CB ? *reinterpret_cast<const float4 *>(x + ((size_t)cb * a.HW + r) * 32 + c0) : make_float4(0.f, 0.f, 0.f, 0.f);
-                if (ch + 4 > s.C) {                      // pad lanes, whatever lies there
-                    if (ch + 0 >= s.C) v[i].x = 0.0f;
-                    if (ch + 1 >= s.C) v[i].y = 0.0f;
-                    if (ch + 2 >= s.C) v[i].z = 0.0f;
-                    v[i].w = 0.0f;
-                }
-            }
-        }
+            for (int i = 0; i < kTile / 32; ++i)
+                v2[g][i] = r0 + i * 32 < pixels && k * 2 + g < s.CB ? __ldg(reinterpret_cast<const float4 *>(x + ((size_t)(k * 2 + g) * a.HW + r0 + i * 32) * 32 + c0)) : make_float4(0.f, 0.f, 0.f, 0.f);
         if (step) {
             if (warp == 0) {
                 bulk_store_wait<0>();
@@ -223,6 +220,17 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
             }
             __syncthreads();
         }
+        if ((k * 2 + 2) * 32 > s.C)                      // pad lanes, whatever lies there
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < kTile / 32; ++i) {
+                    const int ch = (k * 2 + g) * 32 + c0;
+                    if (ch + 0 >= s.C) v2[g][i].x = 0.0f;
+                    if (ch + 1 >= s.C) v2[g][i].y = 0.0f;
+                    if (ch + 2 >= s.C) v2[g][i].z = 0.0f;
+                    if (ch + 3 >= s.C) v2[g][i].w = 0.0f;
+                }
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
