@@ -274,7 +274,7 @@ SMALL_API int small_pack_adapters(small_ctx *ctx, const float *down, const float
 
 SMALL_API size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R) {
     if (N < 1 || H < 1 || W < 1 || (long long)H * W > (1ll << 24) || !adapter_shape_ok(1, C, K, R)) return 0;
-    return adapted_tc_preferred(N, K, H * W, R, kSmCount) ? adapted_tc_workspace(N, C, K, H * W, R) : 0;
+    return adapted_tc_preferred(N, C, K, H * W, R, kSmCount) ? adapted_tc_workspace(N, C, K, H * W, R) : 0;
 }
 
 SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,
@@ -302,7 +302,7 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const AdapterShape s(adapters, C, K, R);
     const AdaptArgs a{in, w_blk, bias, packed, scale, adapter, out, workspace, N, H * W, adapters, (flags & SMALL_RELU) != 0, (flags & SMALL_ACCUMULATE) != 0};
-    if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, K, H * W, R, kSmCount))
+    if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, C, K, H * W, R, kSmCount))
         return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
     if (few_preferred(N, H * W, s, ctx->sm_count)) {
         launch_kernel(ctx, adapted_few_kernel, dim3((unsigned)s.KB, (unsigned)ceil_div(N * H * W, kFew)), dim3(kThreads), few_bytes(s), st, a, s);

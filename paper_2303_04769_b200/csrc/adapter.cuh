@@ -40,7 +40,7 @@ struct AdaptArgs {
 };
 
 // adapter_tc.cu: the whole layer on the tensor cores, whether it pays, its workspace, and its operands
-bool adapted_tc_preferred(int N, int K, int HW, int R, int sms);
+bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms);
 size_t adapted_tc_workspace(int N, int C, int K, int HW, int R);
 int launch_adapted_tc(small_ctx *, const AdaptArgs &, const AdapterShape &, bool x3, cudaStream_t);
 int launch_pack_halves(small_ctx *, const float *down, const float *up, float *packed, int adapters, const AdapterShape &, cudaStream_t);

@@ -12,9 +12,9 @@
 //   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
 //
-// Batch 64, 256 -> 768, 28 x 28, rank 16: 128 us.  Pixels 48 (the filters, 13, beside them): 20 for the largest values,
-// while memory still takes the result before, then four chunks that wait for their loads.  Product 72: MMAs 58 % of the time, the rest a stage waits
-// for its load.  Floor 33 for the bytes, 37 for three products.
+// Batch 64, 256 -> 768, 28 x 28, rank 16: 111 to 124 us (operands from L2 or not).  Pixels 37 (the filters, 12, beside them): the largest values, while
+// memory still takes the result before, then four chunks that wait for their loads.  Product 72: MMAs 58 % of the time, the rest a stage
+// waits for its load.  Floor 33 for the bytes, 37 for three products.
 #include "adapter.cuh"
 #include "halves.cuh"
 
@@ -25,7 +25,7 @@ using namespace halves;
 constexpr int kThreads = 256;
 constexpr int kChunk = 64;               // channels
 constexpr uint32_t kPixelBytes = kTile * 256, kRankBytes = kTile * 128;          // of a chunk of channels, of 32 ranks
-constexpr int kCluster = 8, kTeams = 4;  // blocks of adapter_filters_kernel, teams of 256 threads of a block
+constexpr int kCluster = 8, kTeams = 4, kKept = 6;       // blocks of adapter_filters_kernel, teams of 256 threads of a block, items of a team in registers
 
 struct Layout {
     int tiles, filter_tiles;             // pixel tiles of an image
@@ -69,9 +69,23 @@ __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const
     grid_dep_trigger();
     const int items = c.s.KB * c.s.chunks * 2, tid = threadIdx.x % kThreads, team = blockIdx.x * kTeams + threadIdx.x / kThreads;
     const float4 *w = reinterpret_cast<const float4 *>(c.a.w);
+    auto fetch = [&](int i) {
+        const int kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2);
+        return i < items && cb < c.s.CB ? __ldg(w + ((size_t)kb * c.s.CB + cb) * 256 + tid) : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
     float most = 0.0f;
-#pragma unroll 4
-    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < (size_t)c.s.KB * c.s.CB * 256; i += kCluster * kThreads * kTeams) most = fmaxf(most, magnitude(w[i]));
+    float4 kept[kKept];                                  // the first ones stay in registers
+#pragma unroll
+    for (int e = 0; e < kKept; ++e) kept[e] = fetch(team + e * kCluster * kTeams);
+#pragma unroll
+    for (int e = 0; e < kKept; ++e) most = fmaxf(most, magnitude(kept[e]));
+    for (int i = team + kKept * kCluster * kTeams; i < items; i += 4 * kCluster * kTeams) {
+        float4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fetch(i + e * kCluster * kTeams);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = fmaxf(most, magnitude(v[e]));
+    }
     most = block_max(most, most_s);
     if (threadIdx.x == 0) top = most;
     cluster_arrive();
@@ -84,19 +98,14 @@ __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const
     if (blockIdx.x == 0 && threadIdx.x == 0) exponents(c)[0] = ex;
     char *out = ws_of(c) + c.at.filters_at;
     float (*block)[33] = blocks[threadIdx.x / kThreads];
-    auto fetch = [&](int i) {
-        const int kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2);
-        return i < items && cb < c.s.CB ? w[((size_t)kb * c.s.CB + cb) * 256 + tid] : make_float4(0.f, 0.f, 0.f, 0.f);
-    };
-    float4 v = fetch(team);
-    for (int i0 = 0; i0 < items; i0 += kCluster * kTeams) {
-        const int i = i0 + team, kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2), kt = kb / kFilterTile;
+    auto lay_out = [&](int i, const float4 &v, auto ahead) {
+        const int kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2), kt = kb / kFilterTile;
         __syncthreads();
         const int ch = tid >> 3, f0 = (tid & 7) * 4;
         block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
-        v = fetch(i + kCluster * kTeams);
+        ahead();
         __syncthreads();
-        if (i >= items) continue;
+        if (i >= items) return;
         const int f = tid >> 3, c0 = (tid & 7) * 4, rows = tile_rows(c, kt), row = kb % kFilterTile * 32 + f, col = (cb & 1) * 32 + c0;
         const bool real = kb * 32 + f < c.s.K;
         uint2 hi, lo;
@@ -105,6 +114,14 @@ __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const
         char *to = out + ((size_t)kt * c.s.chunks * kFilterTile * 32 + (size_t)(cb >> 1) * rows) * 256;
         *reinterpret_cast<uint2 *>(to + chunk_at(row, col, rows) + (col & 4) * 2) = hi;
         *reinterpret_cast<uint2 *>(to + chunk_at(row, kChunk + col, rows) + (col & 4) * 2) = lo;
+    };
+#pragma unroll
+    for (int e = 0; e < kKept; ++e)
+        if (e * kCluster * kTeams < items) lay_out(team + e * kCluster * kTeams, kept[e], [] {});
+    float4 v = fetch(team + kKept * kCluster * kTeams);
+    for (int i0 = kKept * kCluster * kTeams; i0 < items; i0 += kCluster * kTeams) {
+        const float4 now = v;
+        lay_out(i0 + team, now, [&] { v = fetch(i0 + team + kCluster * kTeams); });
     }
     cluster_wait();                                      // the others have read this block's maximum
 }
@@ -519,13 +536,18 @@ __global__ void __launch_bounds__(kThreads) pack_halves_kernel(const float *__re
 }  // namespace
 
 // The other form writes the result twice and takes the adapter's products in FP32, which costs the more the larger the rank; this one lays the
-// pixels out first.  us, here / there, batch 64 unless said, rank 8 and 32: 256 -> 768 on 28 x 28 126 / 222 and 128 / 376; 256 -> 256 87 / 103 and 87 /
-// 213; 128 -> 128 43 / 42 and 44 / 92; 64 -> 64 29 / 26 and 29 / 55; 256 -> 256 on 14 x 14 35 / 30 and 36 / 56; 512 -> 128 63 / 41 and 74 / 82; batch
-// 128, 512 -> 512 125 / 148 and 139 / 249, on 8 x 8 71 / 58 and 76 / 127; batch 4, 320 -> 960 on 32 x 32 45 / 37 and 46 / 69.
-bool adapted_tc_preferred(int N, int K, int HW, int R, int sms) {
+// pixels out first.  us, here / there, rank 8 and 32, batch 64 unless said: 256 -> 768 on 28 x 28 110 / 209 and 114 / 338; 256 -> 256 74 / 92 and 74 /
+// 173; 128 -> 128 37 / 38 and 38 / 78; 64 -> 64 27 / 24 and 27 / 47; 256 -> 256 on 14 x 14 30 / 33 and 30 / 61; 512 -> 128 on 28 x 28 119 / 104 and 119 /
+// 236; batch 128, 512 -> 512 on 14 x 14 94 / 136 and 95 / 224, on 8 x 8 56 / 46 and 57 / 82; batch 4, 320 -> 960 on 32 x 32 40 / 35 and 40 / 61.  Few
+// channels, ranks 16 and 32: batch 95, 11 -> 52 on 11 x 19 20.2 / 14.4 and 20.4 / 20.5, batch 41, 41 -> 17 on 32 x 8 15.3 / 10.2 and 15.4 / 14.1.  Few
+// tiles, many operations: batch 31, 390 -> 135, rank 31 on 11 x 20 35.4 / 58.6.
+bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms) {
     const long long tiles = (long long)N * ceil_div(HW, kTile) * ceil_div(blocks_of(K), kFilterTile);
     if (HW < 64 || tiles >= (1 << 28)) return false;
-    return R > 8 ? tiles >= sms / 2 : K > 128 && tiles >= 2 * sms;
+    if (R <= 8) return K > 128 && tiles >= 2 * sms;
+    const int blocks = blocks_of(C) + blocks_of(K);
+    const double apart = (double)N * HW * blocks * 32 * ceil_div(R, 8) * 8;          // the adapter's multiply-adds in FP32
+    return tiles >= sms / 2 ? blocks > 4 || apart >= 40e6 : tiles >= sms / 4 && apart >= 100e6;
 }
 
 size_t adapted_tc_workspace(int N, int C, int K, int HW, int R) { return Layout(N, C, K, HW, R).bytes; }

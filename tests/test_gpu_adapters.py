@@ -174,3 +174,14 @@ def test_an_attention_block(N, C, heads, plane, mode):
     # four layers behind one another: each one's error, and the first projection's once more through the scores
     assert rel_err(from_blk(out, N, C, H, W), proj.ref(z, ids, before=x)) <= 2 * TOL[mode]
     assert B.small_device_status(ctx()) == B.OK
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_more_filters_than_stay_in_registers(mode):
+    """300 and 486 blocks of 32 x 32 weights; a converting team keeps six."""
+    rng = np.random.default_rng(61)
+    for N, C, K in ((80, 320, 960), (76, 840, 570)):
+        layer, x = Layer(rng, C, K, 9, 3), rng.standard_normal((N, C, 8, 8)).astype(np.float32)
+        ids = rng.integers(-1, 3, N).astype(np.int32)
+        assert B.small_adapted_conv2d_workspace_bytes(N, C, K, 8, 8, 9) > 0
+        assert rel_err(layer.run(x, ids, mode), layer.ref(x, ids)) <= TOL[mode]
