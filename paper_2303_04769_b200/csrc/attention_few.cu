@@ -71,12 +71,23 @@ __global__ void __launch_bounds__(kThreads, R * DP >= 512 ? 1 : 2) attention_few
         vc[c] = v + e;
     }
     int next = from + warp * 4 + (lane >> 3);            // this group's first key of the round that is fetched next
+    // rows and columns of the keys to be fetched and of those to be weighed; a block's groups are kWarps * 4 keys apart
+    struct Walk {
+        int y, x;
+        __device__ void on(int dy, int dx, int width) {
+            y += dy;
+            x += dx;
+            if (x >= width) { x -= width; ++y; }
+        }
+    };
+    const int width = kGeneral ? max(ke.y, 1) : 1, dy = kWarps * 4 / width, dx = kWarps * 4 % width;
+    Walk ahead{next / width, next % width}, here = ahead;
     auto fetch = [&](int stage) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u, next += kWarps * 4) {
             const bool in = next < to;
-            int p = in ? next : 0;
-            if (kGeneral && !whole) p = p / ke.y * a.KW + p % ke.y;
+            const int p = !in ? 0 : kGeneral && !whole ? ahead.y * a.KW + ahead.x : next;
+            if (kGeneral && !whole) ahead.on(dy, dx, width);
 #pragma unroll
             for (int c = 0; c < kVec; ++c) {
                 const bool some = in && c * 32 + c0 < a.D;
@@ -94,10 +105,16 @@ __global__ void __launch_bounds__(kThreads, R * DP >= 512 ? 1 : 2) attention_few
         fetch(stage == 0 ? kStages - 1 : stage - 1);
         copy_wait<kStages - 1>();
         float4 x[kAhead][kVec], y[kAhead][kVec];
-        int place[kAhead];
+        float bias_of[R][kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (kGeneral && a.bias) place[u] = of_key(a, (j + u * kWarps * 4) / ke.y, (j + u * kWarps * 4) % ke.y);
+            if (kGeneral && a.bias) {                    // on their way while the products are taken
+                const bool in = j + u * kWarps * 4 < to;
+                const int place = of_key(a, here.y, here.x);
+                here.on(dy, dx, width);
+#pragma unroll
+                for (int r = 0; r < R; ++r) bias_of[r][u] = in ? __ldg(bias[r] - place) : 0.0f;
+            }
 #pragma unroll
             for (int c = 0; c < kVec; ++c) {
                 x[u][c] = mine[((stage * 2 + 0) * 4 + u * kVec + c) * 32];
@@ -117,7 +134,7 @@ __global__ void __launch_bounds__(kThreads, R * DP >= 512 ? 1 : 2) attention_few
                 for (int w = 1; w < 8; w *= 2) s[u] += __shfl_xor_sync(~0u, s[u], w);
                 if (kGeneral && capping) s[u] = capped(s[u], cap2, over_cap);
                 const bool in = j + u * kWarps * 4 < to;
-                if (kGeneral && a.bias && in) s[u] += powers_of_two(bias[r][-place[u]]);
+                if (kGeneral && a.bias) s[u] += powers_of_two(bias_of[r][u]);
                 if (!in) s[u] = -INFINITY;
                 top = fmaxf(top, s[u]);
             }
