@@ -144,6 +144,9 @@ bool attention_shape_ok(int N, int heads, int kv_heads, int D, int QH, int QW, i
 //   memory at any batch (49 pixels, 64 channels: batch 2 11.0 and 6.2, 128 40.8 and 25.4); else up to some 48 M multiply-adds of whole tiles (72
 //   pixels, 64 channels: batch 16, 38 M, 12.5 and 11.7, 32 16.7 and 16.8; 196 pixels: 64 channels batch 4, 51 M, 16.4 and 14.6, 32 channels
 //   batch 8, 51 M, 13.1 and 14.5).
+//   Beyond that, while the rows of all heads are few, the streaming kernel, which shares out the keys (us, FP32 kernel / tensor cores / it, 8 heads
+//   of 64: 17 queries on 96 x 96, batch 4, 544 rows 1439 / 195 / 137; 64 queries on 56 x 56, 512 rows 458 / 60 / 39, 128 61 / 60; 64 queries on 96 x
+//   96, batch 4, 2048 rows 1431 / 195 / 260, on 28 x 28, batch 11, 5632 rows 126 / 33 / 94).
 enum class Kernel { few, small, tensor_cores, fp32 };
 
 Kernel kernel_of(int N, int heads, int kv_heads, int D, int QP, int KP, unsigned math) {
@@ -152,7 +155,9 @@ Kernel kernel_of(int N, int heads, int kv_heads, int D, int QP, int KP, unsigned
     if (QP <= kFewQueries) return holds && ((KP <= 128 && KP * lanes <= 8192) || QP * (heads / kv_heads) > 4) ? Kernel::small : Kernel::few;
     const double work = (double)N * heads * QP * (ceil_div(KP, 64) * 64.0) * lanes;
     if (holds && (math == SMALL_MATH_FP32 || (QP <= 64 && KP <= 64) || work <= 48e6)) return Kernel::small;
-    return math == SMALL_MATH_FP32 ? Kernel::fp32 : Kernel::tensor_cores;
+    const long long rows = (long long)N * heads * QP;
+    if (math != SMALL_MATH_FP32) return rows <= 768 && (D & 3) == 0 ? Kernel::few : Kernel::tensor_cores;
+    return rows <= 6000 ? Kernel::few : Kernel::fp32;
 }
 
 }  // namespace

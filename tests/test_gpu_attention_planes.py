@@ -10,12 +10,23 @@ from gpu_util import B
 pytestmark = pytest.mark.gpu
 
 LONG = [  # N, heads, kv heads, D, query plane, key plane
-    (1, 1, 1, 5, (11, 12), (24, 25)), (1, 2, 2, 33, (13, 13), (20, 19)), (2, 4, 2, 40, (19, 19), (19, 19)), (1, 1, 1, 64, (17, 1), (1, 385)),
-    (1, 1, 1, 64, (1, 128), (1, 512)), (1, 1, 1, 64, (3, 7), (2, 192)), (1, 2, 1, 128, (12, 11), (13, 16)), (1, 3, 1, 96, (9, 16), (1, 257)),
-    (1, 1, 1, 32, (127, 1), (640, 1)), (1, 1, 1, 32, (129, 1), (641, 1)), (1, 1, 1, 1, (5, 5), (1, 700)), (25, 8, 4, 48, (10, 10), (10, 10)),
+    (1, 1, 1, 5, (11, 12), (24, 25)), (1, 2, 2, 33, (13, 13), (20, 19)), (2, 4, 2, 40, (19, 19), (19, 19)), (46, 1, 1, 64, (17, 1), (1, 385)),
+    (7, 1, 1, 64, (1, 128), (1, 512)), (40, 1, 1, 64, (3, 7), (2, 192)), (3, 2, 1, 128, (12, 11), (13, 16)), (2, 3, 1, 96, (9, 16), (1, 257)),
+    (7, 1, 1, 32, (127, 1), (640, 1)), (6, 1, 1, 32, (129, 1), (641, 1)), (1, 1, 1, 1, (5, 5), (1, 700)), (25, 8, 4, 48, (10, 10), (10, 10)),
     (16, 16, 16, 64, (11, 12), (8, 16)), (3, 1, 1, 7, (33, 3), (33, 17)), (40, 4, 2, 128, (9, 9), (9, 9)), (30, 8, 8, 32, (9, 8), (9, 8))]
 MANY = [(64, 8, 8, 64, (7, 7), (7, 7)), (200, 2, 2, 16, (8, 8), (8, 8)), (100, 6, 2, 20, (5, 5), (6, 6)), (90, 4, 2, 33, (8, 8), (3, 5)), (2, 1, 1, 128, (40, 40), (9, 7)),
         (1, 1, 1, 32, (17, 1), (1, 500)), (1, 1, 1, 64, (1, 21), (1, 300)), (1, 2, 1, 128, (1, 33), (4, 42)), (70, 3, 3, 3, (2, 9), (1, 2)), (160, 1, 1, 128, (1, 12), (1, 129))]
+
+SPREAD = [  # rows of all heads few, keys many: their blocks share out the keys in every mode
+    (1, 1, 1, 32, (5, 10), (60, 61)), (1, 4, 2, 64, (7, 7), (33, 31)), (2, 3, 1, 20, (1, 100), (27, 28)), (1, 1, 1, 128, (1, 700), (1, 190)), (3, 2, 2, 48, (8, 16), (2, 260))]
+
+
+@pytest.mark.parametrize("mode", A.MODES)
+@pytest.mark.parametrize("shape", SPREAD)
+def test_few_rows_over_many_keys(shape, mode):
+    assert B.small_attention_workspace_bytes(*shape, B.MATH[mode]) == 0
+    A.test_matches_the_formula(shape, mode)
+    A.test_bias_cap_and_padded_images(shape, 3.0, mode)
 
 
 @pytest.mark.parametrize("mode", A.MODES)
@@ -57,7 +68,7 @@ def test_what_lies_outside_the_extents_has_no_part(mode):
 @pytest.mark.parametrize("mode", A.MODES)
 def test_values_that_are_not_finite_are_not_hidden(mode):
     rng = np.random.default_rng(32)
-    q, k, v = A.make(rng, 3, 1, 1, 32, (9, 9), (25, 25))
+    q, k, v = A.make(rng, 3, 1, 1, 32, (19, 19), (25, 25))
     ref = R.attention(q, k, v, 1, 1, 32 ** -0.5)
     v[1, 4, 3, 3] = np.nan
     k[2, 0, 24, 24] = np.nan
@@ -71,7 +82,7 @@ def test_values_that_are_not_finite_are_not_hidden(mode):
 @pytest.mark.parametrize("qs,ks,vs", [(1e4, 1e-4, 1.0), (1e-15, 1e15, 1e20), (1.0, 1.0, 1e-20), (1e-20, 1e19, 1e-30)])
 def test_scales_of_the_operands(qs, ks, vs, mode):
     rng = np.random.default_rng(33)
-    q, k, v = A.make(rng, 2, 2, 2, 32, (13, 12), (25, 24))
+    q, k, v = A.make(rng, 2, 2, 2, 32, (25, 24), (25, 24))
     v[:, :, ::2] *= 1e-3
     q, k, v = (q * qs).astype(np.float32), (k * ks).astype(np.float32), (v * vs).astype(np.float32)
     scale = 1.0 / (32 ** 0.5 * qs * ks)
@@ -82,8 +93,8 @@ def test_scales_of_the_operands(qs, ks, vs, mode):
 @pytest.mark.parametrize("scale", [0.0, -0.15])
 def test_scales_that_are_not_positive(scale, mode):
     rng = np.random.default_rng(34)
-    q, k, v = A.make(rng, 2, 2, 1, 40, (13, 12), (19, 19))
-    for args in (dict(), dict(bias=A.table(rng, 2, (13, 12), (19, 19))), dict(cap=2.0)):
+    q, k, v = A.make(rng, 2, 2, 1, 40, (19, 19), (19, 19))
+    for args in (dict(), dict(bias=A.table(rng, 2, (19, 19), (19, 19))), dict(cap=2.0)):
         A.close(A.run(q, k, v, 2, 1, mode, scale=scale, **args), R.attention(q, k, v, 2, 1, scale, **args), mode)
 
 
