@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
             const uint32_t bytes = issued & 1 ? v_bytes : k_bytes;
             mbar_expect_tx(full + slot * 8, bytes);
             bulk_load(smem_u32(slots + slot * kBytes), from_tiles + (size_t)issued * kBytes, bytes, full + slot * 8);
-            if (kGeneral && !(issued & 1)) {
+            if (kGeneral && bias && !(issued & 1)) {           // (whoever asks waits: nothing may arrive behind a block's end)
                 const int t = issued >> 1, at = t % kPlaces;
                 mbar_expect_tx(placed + at * 8, kPlaceInts * sizeof(int));
                 bulk_load(smem_u32(sh.places[at]), from_places + t * kPlaceInts, kPlaceInts * sizeof(int), placed + at * 8);
@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
     tc_fence_after();
     if (sh.gave_up && warp == loader) {                  // what is still on its way must land before the block ends
         for (int x = max(0, issued - c.ring); x < issued; ++x) mbar_wait(full + x % c.ring * 8, (x / c.ring) & 1, kDefaultWaitIters);
-        for (int t = max(0, (issued + 1) / 2 - kPlaces); kGeneral && t < (issued + 1) / 2; ++t) mbar_wait(placed + t % kPlaces * 8, t / kPlaces & 1, kDefaultWaitIters);
+        for (int t = max(0, (issued + 1) / 2 - kPlaces); kGeneral && bias && t < (issued + 1) / 2; ++t) mbar_wait(placed + t % kPlaces * 8, t / kPlaces & 1, kDefaultWaitIters);
     }
     if (warp == issuer) tmem_dealloc(tmem, 512);
 }

@@ -102,3 +102,17 @@ def test_scales_that_are_not_positive(scale, mode):
 @pytest.mark.parametrize("shape", [(2, 4, 2, 64, (19, 18), (19, 18)), (16, 4, 4, 32, (7, 7), (7, 7))])
 def test_repeatable_on_streams_and_in_a_graph(shape, mode):
     A.test_repeatable_on_streams_and_in_a_graph(shape, mode)
+
+
+@pytest.mark.parametrize("mode", ["3xtf32", "tf32"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_a_cap_without_a_table_over_many_tiles_of_keys(D, mode):
+    """The tensor cores' general form without a table: more tiles of 128 keys than places of them are held (8), block after block on each SM."""
+    shape = (2, 4, 2, D, (40, 33), (39, 34))
+    assert B.small_attention_workspace_bytes(*shape, B.MATH[mode]) > 0
+    rng = np.random.default_rng(35)
+    q, k, v = A.make(rng, *shape)
+    ke = np.array([[39, 34], [30, 33]], np.int32)
+    ref = R.attention(q, k, v, 4, 2, D ** -0.5, cap=3.0, k_extents=ke)
+    for _ in range(3):
+        A.close(A.run(q, k, v, 4, 2, mode, cap=3.0, ke=ke), ref, mode)
