@@ -312,7 +312,7 @@ NormPlan plan_norm(int N, int C, int HW, int groups) {
 
 template <unsigned kAct>
 int launch_norm(small_ctx *ctx, const NormArgs &a, const NormPlan &p, int N, cudaStream_t st) {
-    static std::atomic<unsigned long long> whole{0}, part{0};
+    static std::atomic<unsigned long long> whole{0}, part{0}, applied{0};
     const size_t most = kMostShared;
     const dim3 grid((unsigned)(N * p.splits), (unsigned)p.units), block(kThreads);
     if (p.on_chip) {
@@ -324,7 +324,11 @@ int launch_norm(small_ctx *ctx, const NormArgs &a, const NormPlan &p, int N, cud
     if (int s = allow_shared_memory(ctx, group_norm_kernel<false, 0>, part, most)) return s;
     launch_kernel(ctx, group_norm_kernel<false, 0>, grid, block, p.smem, st, a);
     if (int s = check_launch(ctx)) return s;
-    launch_kernel(ctx, group_norm_apply_kernel<kAct>, grid, block, 3 * (size_t)p.unit_blocks * 128, st, a);
+    // means, scales and shifts of some more than 4000 channels pass the 48 KB that need not be asked for (with the kernel's static 256 bytes)
+    const size_t channels = 3 * (size_t)p.unit_blocks * 128;
+    if (channels > (47u << 10))
+        if (int s = allow_shared_memory(ctx, group_norm_apply_kernel<kAct>, applied, most)) return s;
+    launch_kernel(ctx, group_norm_apply_kernel<kAct>, grid, block, channels, st, a);
     return check_launch(ctx);
 }
 

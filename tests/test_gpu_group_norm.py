@@ -124,3 +124,14 @@ def test_repeatable_on_streams_and_in_a_graph(shape):
     for _ in range(3):
         graph.replay()
     assert np.array_equal(from_blk(out, N, C, H, W), first)
+
+
+@pytest.mark.parametrize("shape", [(1, 4096, 16, 16, 1), (1, 8192, 12, 12, 1), (2, 4128, 16, 17, 32), (1, 6144, 9, 9, 1)])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_units_of_thousands_of_channels(shape, act):
+    """The second form's second kernel: means, scales and shifts of a unit's channels take more than the 48 KB a kernel has unasked."""
+    N, C, H, W, groups = shape
+    rng = np.random.default_rng(C + H)
+    x, gamma, beta = make(rng, N, C, H, W)
+    assert B.small_group_norm_workspace_bytes(*shape) > 0
+    assert rel_err(run(x, gamma, beta, groups, act=act), R.group_norm(x, gamma, beta, groups, 1e-5, act)) <= TOL["fp32"]
