@@ -374,7 +374,7 @@ int small_fc_uses_tensor_cores(int N, int J, int K, unsigned math);
  * a cluster's shared memory, which are read once.  Calls that may run at the same time need workspaces of their own.  The mean is
  * taken first and the deviations are summed after it, all sums in FP32.  A value that is not finite makes its image's group NaN.
  * Errors: INVALID_ARG, SHAPE, ALIGN, OVERLAP, WORKSPACE (needed and NULL), UNSUPPORTED (a run of whole groups and whole channel blocks of
- * more than some 10,000 channels). */
+ * more than 11,520 channels). */
 size_t small_group_norm_workspace_bytes(int N, int C, int H, int W, int groups);
 int small_group_norm(small_ctx *ctx, const float *in, const float *gamma, const float *beta, float *out, void *workspace,
                      int N, int C, int H, int W, int groups, float eps, unsigned flags, void *stream);

@@ -305,6 +305,7 @@ NormPlan plan_norm(int N, int C, int HW, int groups) {
         p.splits = (int)((bytes + kBlockBytes / 2 - 1) / (kBlockBytes / 2));
         if (p.splits > HW) p.splits = HW;
         p.splits = ceil_div(HW, ceil_div(HW, p.splits));         // none without a pixel
+        for (int part = ceil_div(HW, p.splits); part > 1 && block_bytes(p, HW) > kMostShared;) p.splits = ceil_div(HW, --part);
     }
     p.smem = block_bytes(p, HW);
     return p;

@@ -135,3 +135,12 @@ def test_units_of_thousands_of_channels(shape, act):
     x, gamma, beta = make(rng, N, C, H, W)
     assert B.small_group_norm_workspace_bytes(*shape) > 0
     assert rel_err(run(x, gamma, beta, groups, act=act), R.group_norm(x, gamma, beta, groups, 1e-5, act)) <= TOL["fp32"]
+
+
+@pytest.mark.parametrize("shape", [(1, 9984, 10, 11, 1), (1, 11520, 7, 9, 1), (2, 10240, 3, 3, 1)])
+def test_the_largest_units(shape):
+    """Two or more pixels of these are too many for a block, one is not."""
+    N, C, H, W, groups = shape
+    rng = np.random.default_rng(C + H)
+    x, gamma, beta = make(rng, N, C, H, W)
+    assert rel_err(run(x, gamma, beta, groups), R.group_norm(x, gamma, beta, groups, 1e-5, "none")) <= TOL["fp32"]
