@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(kThreads) group_norm_apply_kernel(const NormAr
         float mean = 0.0f, dev = 0.0f, count = 0.0f;
         auto join = [&](float m, float d2, float n) {
             if (n == 0.0f) return;
+            if (count == 0.0f) { mean = m; dev = d2; count = n; return; }        // (below, 0 * the square of a far mean: of one beyond 1.8e19 NaN)
             const float d = m - mean, all = count + n, share = n / all;
             dev += d2 + d * d * (count * share) * (float)a.cpg;
             mean += d * share;

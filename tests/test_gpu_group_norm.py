@@ -144,3 +144,13 @@ def test_the_largest_units(shape):
     rng = np.random.default_rng(C + H)
     x, gamma, beta = make(rng, N, C, H, W)
     assert rel_err(run(x, gamma, beta, groups), R.group_norm(x, gamma, beta, groups, 1e-5, "none")) <= TOL["fp32"]
+
+
+@pytest.mark.parametrize("H", [10, 150])
+def test_a_group_without_spread_far_from_zero(H):
+    """2^70 everywhere in one group: its sums are exact, their squares are beyond FP32's range and have no part."""
+    rng = np.random.default_rng(11)
+    x, gamma, beta = make(rng, 2, 48, H, 120)
+    x[1, 16:32] = np.float32(2.0 ** 70)
+    got = run(x, gamma, beta, 3)
+    assert np.array_equal(got[1, 16:32], np.broadcast_to(beta[16:32, None, None], (16, H, 120)))
