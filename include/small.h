@@ -372,7 +372,8 @@ int small_fc_uses_tensor_cores(int N, int J, int K, unsigned math);
  * gamma, beta: C floats each, or NULL (1, 0).  eps: finite and >= 0.  flags: SMALL_RELU or SMALL_SILU or neither.  out may equal in.
  * workspace: device, 16-byte aligned, small_group_norm_workspace_bytes bytes; may be NULL where that is 0 - planes whose group fits
  * a cluster's shared memory, which are read once.  Calls that may run at the same time need workspaces of their own.  The mean is
- * taken first and the deviations are summed after it, all sums in FP32.  A value that is not finite makes its image's group NaN.
+ * taken first and the deviations are summed after it, all sums in FP32 (a variance beyond its range is infinite: beta is left).  A value
+ * that is not finite makes its image's group NaN (0 with SMALL_RELU, as in every layer's).
  * Errors: INVALID_ARG, SHAPE, ALIGN, OVERLAP, WORKSPACE (needed and NULL), UNSUPPORTED (a run of whole groups and whole channel blocks of
  * more than 11,520 channels). */
 size_t small_group_norm_workspace_bytes(int N, int C, int H, int W, int groups);

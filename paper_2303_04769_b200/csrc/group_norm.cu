@@ -43,10 +43,10 @@ __device__ __forceinline__ float4 clear_pad(float4 v, int c, int channels) {    
     if (c + 4 <= channels) return v;
     return make_float4(c < channels ? v.x : 0.0f, c + 1 < channels ? v.y : 0.0f, c + 2 < channels ? v.z : 0.0f, 0.0f);
 }
-// 1 / sqrt(x): the approximation and one step of Newton's.
+// 1 / sqrt(x): the approximation and one step of Newton's, which has nothing to add to the 0 of an infinite variance (inf * 0).
 __device__ __forceinline__ float over_sqrt(float x) {
     const float r = rsqrtf(x);
-    return r * fmaf(-0.5f * x * r, r, 1.5f);
+    return x < INFINITY ? r * fmaf(-0.5f * x * r, r, 1.5f) : r;
 }
 
 // The unit of this thread block and the part of its pixels that the block holds.

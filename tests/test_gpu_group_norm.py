@@ -154,3 +154,29 @@ def test_a_group_without_spread_far_from_zero(H):
     x[1, 16:32] = np.float32(2.0 ** 70)
     got = run(x, gamma, beta, 3)
     assert np.array_equal(got[1, 16:32], np.broadcast_to(beta[16:32, None, None], (16, H, 120)))
+
+
+@pytest.mark.parametrize("H", [10, 150])
+def test_a_variance_beyond_the_range(H):
+    """Values whose squares are more than FP32 holds: an infinite variance, and what the formula makes of one."""
+    rng = np.random.default_rng(9)
+    x, gamma, beta = make(rng, 2, 48, H, 120)
+    y = x.copy()
+    y[1, 16:32] *= 1e25                                         # group 1 of image 1
+    got, ref = run(y, gamma, beta, 3), R.group_norm(x, gamma, beta, 3, 1e-5, "none")
+    assert np.array_equal(got[1, 16:32], np.broadcast_to(beta[16:32, None, None], (16, H, 120)))
+    got[1, 16:32] = ref[1, 16:32]
+    assert rel_err(got, ref) <= TOL["fp32"]
+
+
+@pytest.mark.parametrize("H", [10, 150])
+def test_a_value_that_is_not_finite_before_an_activation(H):
+    rng = np.random.default_rng(10)
+    x, gamma, beta = make(rng, 1, 48, H, 120)
+    ref = {act: R.group_norm(x, gamma, beta, 3, 1e-5, act) for act in ("relu", "silu")}
+    x[0, 20, H // 2, 7] = np.nan                                # group 1
+    for act, left in (("relu", 0.0), ("silu", np.nan)):         # max(NaN, 0) is 0 in every layer of the library
+        got = run(x, gamma, beta, 3, act=act)
+        assert np.array_equal(got[0, 16:32], np.full((16, H, 120), left, np.float32), equal_nan=True)
+        got[0, 16:32] = ref[act][0, 16:32]
+        assert rel_err(got, ref[act]) <= TOL["fp32"]
