@@ -396,7 +396,7 @@ int small_group_norm(small_ctx *ctx, const float *in, const float *gamma, const 
  * q_extents, k_extents: int32[N][2], the rows and columns of image n's plane that hold its pixels (clamped to the plane), or
  * NULL for whole planes.  Key pixels outside are not read as keys: whatever they hold, NaN too, has no part in the result.  Query
  * pixels outside, and queries that no key is left for, get 0.
- * scale, cap: finite, cap >= 0 (0: no cap).  D at most 128, any number; heads, kv_heads at least 1.
+ * scale, cap: finite, cap >= 0 (0: no cap; above 2^100 as 0).  D at most 128, any number; heads, kv_heads at least 1.
  * flags: one SMALL_MATH_*.  FP32: FP32 multiply-adds.  TF32, 3XTF32: the same for few queries and small planes, else both
  * products on the tensor cores, operands rounded to 11 significant bits, or two such terms each (three products: FP32 accuracy); scores,
  * their maxima and sums and the accumulation over keys in FP32.  The terms are halves, scaled by a query's and by 128 keys' largest value:

@@ -3,6 +3,8 @@
 // attention_fp32_kernel: a block takes 64 queries of one head and walks the keys 64 at a time.  Scores, maxima and sums of a row stay
 // in the 16 lanes that share it; the exponentials cross shared memory once to become the second product's operand.  Bound by FP32
 // multiply-adds: 4 x 4 scores a thread, then 4 rows x D / 16 columns of the result.
+#include <algorithm>
+
 #include "attention.cuh"
 
 namespace small {
@@ -206,6 +208,10 @@ SMALL_API int small_attention(small_ctx *ctx, const float *q, const float *k, co
     if (ws && ranges_overlap(out, out_bytes, workspace, ws)) return SMALL_ERR_OVERLAP;
     const OnDevice on(ctx);
     if (on.error != cudaSuccess) { ctx->last_cuda = (int)on.error; return SMALL_ERR_CUDA; }
+    // The kernels take cap * log2(e) and 1 / cap: both stay ordinary numbers.  Scores below 2^80 lose less than 2^-41 of themselves to a cap above 2^100;
+    // capped at 2^-60 or below, all scores weigh 1 to FP32's last bit.
+    if (cap > 0x1p100f) cap = 0.0f;
+    else if (cap > 0.0f) cap = std::max(cap, 0x1p-60f);
     const AttnArgs a{q, k, v, bias, q_extents, k_extents, out, workspace, N, heads, kv_heads, D, QH, QW, KH, KW, QP, KP, blocks_of(heads * D),
                      q_stride, k_stride, v_stride, scale, cap, QW + KW - 1};
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -253,3 +253,21 @@ def test_random_shapes(mode):
         ke = np.stack([rng.integers(0, kp[0] + 1, N), rng.integers(0, kp[1] + 1, N)], 1).astype(np.int32) if rng.random() < 0.4 else None
         cap = float(rng.choice([0.0, 2.0]))
         close(run(q, k, v, heads, kv, mode, cap=cap, bias=bias, ke=ke), R.attention(q, k, v, heads, kv, D ** -0.5, cap=cap, bias=bias, k_extents=ke), mode)
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("shape", [(2, 2, 1, 32, (1, 1), (20, 21)), (2, 2, 2, 40, (5, 6), (5, 6)), (2, 4, 2, 64, (19, 19), (19, 19))])
+def test_caps_at_both_ends_of_the_range(shape, mode):
+    """Far above every score a cap has no part; next to nothing it leaves all keys alike, a score of exactly 0 (a query of zeros) among them."""
+    N, heads, kv, D, qp, kp = shape
+    rng = np.random.default_rng(21)
+    q, k, v = make(rng, N, heads, kv, D, qp, kp)
+    bias = table(rng, heads, qp, kp)
+    q[:, :, 0, 0] = 0
+    for b in (None, bias):
+        free = R.attention(q, k, v, heads, kv, D ** -0.5, bias=b)
+        for cap in (3.4e38, 2.4e38, 1e33):
+            close(run(q, k, v, heads, kv, mode, cap=cap, bias=b), free, mode)
+        alike = R.attention(q * 0, k, v, heads, kv, D ** -0.5, bias=b)
+        for cap in (1e-39, 1e-38, 1e-30):
+            close(run(q, k, v, heads, kv, mode, cap=cap, bias=b), alike, mode)
