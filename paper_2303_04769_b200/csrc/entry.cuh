@@ -20,13 +20,14 @@ static inline int check_pointers(std::initializer_list<const void *> required, s
 
 static inline bool one_math_mode(unsigned flags) { return (flags & SMALL_MATH_MASK) != SMALL_MATH_MASK; }
 
-// The call runs on the context's device, whichever is current: its tensors live there.
+// The call runs on the context's device, whichever is current: its tensors live there.  A context that small_init has not filled has none: the rules
+// that plan a launch divide by its SMs.
 struct OnDevice {
     int before = -1;
     cudaError_t error;
     explicit OnDevice(const small_ctx *ctx) {
         int now = 0;
-        error = cudaGetDevice(&now);
+        error = ctx->sm_count > 0 ? cudaGetDevice(&now) : cudaErrorInvalidDevice;
         if (error == cudaSuccess && now != ctx->device) {
             before = now;
             error = cudaSetDevice(ctx->device);

@@ -8,7 +8,7 @@ B = pytest.importorskip("paper_2303_04769_b200.binding")
 
 CTX = ctypes.c_void_p()
 _room = (ctypes.c_char * 8192)()
-INVALID, SHAPE, ALIGN, OVERLAP, WORKSPACE, NOT_INIT = 1, 2, 3, 4, 5, 9
+INVALID, SHAPE, ALIGN, OVERLAP, WORKSPACE, CUDA, NOT_INIT = 1, 2, 3, 4, 5, 7, 9
 STREAM = 0
 
 
@@ -118,3 +118,10 @@ def test_adapters():
 def test_attention_without_channels_and_a_scale():
     for D in (0, -1):
         assert attend(D=D, scale=None) == SHAPE
+
+
+def test_a_context_without_a_device_goes_no_further():
+    """Calls with nothing else wrong: a zeroed context has no SMs to plan for, with a GPU in the machine or without one."""
+    for refused in (norm(), attend(), attend(qp=(1, 1)), attend(flags=B.MATH_FP32), adapt(), adapt(N=2, ws=None), adapt(N=2, H=1, W=1), adapt(flags=B.MATH_FP32),
+                    status(B.small_pack_adapters, CTX, at(0), at(1), at(2), 4, 64, 96, 8, STREAM)):
+        assert refused == CUDA
