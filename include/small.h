@@ -425,7 +425,7 @@ int small_pack_adapters(small_ctx *ctx, const float *down, const float *up, floa
  * int32[N]; scale: device float[adapters] or NULL (1); out: blocked [N][K][H][W].  flags: SMALL_RELU, SMALL_ACCUMULATE (out_previous is
  * added in front of the activation) and one SMALL_MATH_* for both parts (few pixels of few channels: FP32 multiply-adds in each).  workspace: device, 16-byte aligned,
  * small_adapted_conv2d_workspace_bytes bytes (operands as halves, scaled by pixel, where the layer runs as one product on the tensor
- * cores; 0 and NULL where it does not in any math mode); calls that may run at the same time need their own.
+ * cores; 0 and NULL where it does not, and NULL in FP32 anywhere); calls that may run at the same time need their own.
  * Errors as small_conv2d, and WORKSPACE (needed and NULL). */
 size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R);
 int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,

@@ -287,9 +287,9 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     Geom g;
     if (!adapter_shape_ok(adapters, C, K, R)) return SMALL_ERR_SHAPE;
     if (int s = make_geom(g, N, C, K, H, W, 1, 1, 1, 0, 0, 0, 0)) return s;
-    const size_t ws = small_adapted_conv2d_workspace_bytes(N, C, K, H, W, R);
-    if (ws && !workspace) return SMALL_ERR_WORKSPACE;
     const unsigned math = flags & SMALL_MATH_MASK;
+    const size_t ws = math == SMALL_MATH_FP32 ? 0 : small_adapted_conv2d_workspace_bytes(N, C, K, H, W, R);
+    if (ws && !workspace) return SMALL_ERR_WORKSPACE;
     const size_t in_b = sizeof(float) * packed_elems(N, C, H, W), out_b = sizeof(float) * packed_elems(N, K, H, W);
     const struct { const void *p; size_t n; } read[] = {
         {in, in_b}, {w_blk, sizeof(float) * small_conv_weight_elems(C, K, 1, 1, math)}, {bias, sizeof(float) * K},
@@ -302,7 +302,7 @@ SMALL_API int small_adapted_conv2d(small_ctx *ctx, const float *in, const float 
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const AdapterShape s(adapters, C, K, R);
     const AdaptArgs a{in, w_blk, bias, packed, scale, adapter, out, workspace, N, H * W, adapters, (flags & SMALL_RELU) != 0, (flags & SMALL_ACCUMULATE) != 0};
-    if (math != SMALL_MATH_FP32 && adapted_tc_preferred(N, C, K, H * W, R, kSmCount))
+    if (ws)
         return launch_adapted_tc(ctx, a, s, math == SMALL_MATH_3XTF32, st);
     if (few_preferred(N, H * W, s, ctx->sm_count)) {
         launch_kernel(ctx, adapted_few_kernel, dim3((unsigned)s.KB, (unsigned)ceil_div(N * H * W, kFew)), dim3(kThreads), few_bytes(s), st, a, s);

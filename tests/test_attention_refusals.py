@@ -125,3 +125,12 @@ def test_a_context_without_a_device_goes_no_further():
     for refused in (norm(), attend(), attend(qp=(1, 1)), attend(flags=B.MATH_FP32), adapt(), adapt(N=2, ws=None), adapt(N=2, H=1, W=1), adapt(flags=B.MATH_FP32),
                     status(B.small_pack_adapters, CTX, at(0), at(1), at(2), 4, 64, 96, 8, STREAM)):
         assert refused == CUDA
+
+
+def test_fp32_needs_no_workspace():
+    """The products of halves are the other modes': FP32 gets as far as the device without their room, and does not look at what is given."""
+    assert B.small_adapted_conv2d_workspace_bytes(80, 64, 96, 8, 8, 9) > 0
+    for ws in (None, at(6), at(0)):
+        assert adapt(ws=ws, flags=B.MATH_FP32) == CUDA
+    for flags in (B.MATH_TF32, B.MATH_3XTF32):
+        assert adapt(ws=None, flags=flags) == WORKSPACE and adapt(ws=at(6), flags=flags) == OVERLAP
