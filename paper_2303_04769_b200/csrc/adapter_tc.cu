@@ -433,13 +433,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         }
     } else {
         const int lane = threadIdx.x & 31, half = warp >> 2;
-        const float w_drop = drop(exponents(c)[0]);
+        const int w_exponent = exponents(c)[0];
         float4 *rows = reinterpret_cast<float4 *>(stages + kStages * kStageBytes) + warp * 256;
         int buffer = 0, phase = 0;
         for (int i = blockIdx.x; i < work; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
-            const float x_drop = drop(exponents(c)[4 + (size_t)np * kTile + (warp & 3) * 32 + lane]);
-            const float grown = w_drop * (1.0f + kCutOff * (float)((kX3 ? 3 : 1) * (s.chunks * (kChunk / 16) + (ranks_of(np) ? (s.R + 15) / 16 : 0))));
+            // undoes both operands' scaling: the pixel's and the filters' parts may each pass FP32's range where the result does not
+            const TwoFactors back(exponents(c)[4 + (size_t)np * kTile + (warp & 3) * 32 + lane] + w_exponent - 2 * 141);
+            const float grown = (1.0f + kCutOff * (float)((kX3 ? 3 : 1) * (s.chunks * (kChunk / 16) + (ranks_of(np) ? (s.R + 15) / 16 : 0))));
             if (!mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit)) break;
             tc_fence_after();
             const int blocks = tile_rows(c, kt) / 32;
@@ -449,7 +450,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                 // through shared memory, so that a store is whole lines: eight lanes a pixel
 #pragma unroll
                 for (int u = 0; u < 8; ++u)
-                    rows[lane * 8 + (u ^ (lane & 7))] = make_float4(v[u * 4] * x_drop, v[u * 4 + 1] * x_drop, v[u * 4 + 2] * x_drop, v[u * 4 + 3] * x_drop);
+                    rows[lane * 8 + (u ^ (lane & 7))] = make_float4(v[u * 4] * back.a * back.b, v[u * 4 + 1] * back.a * back.b, v[u * 4 + 2] * back.a * back.b,
+                                                                    v[u * 4 + 3] * back.a * back.b);
                 __syncwarp();
                 const int k0 = (kt * kFilterTile + b) * 32 + (lane & 7) * 4;
                 float4 add = make_float4(0.f, 0.f, 0.f, 0.f);

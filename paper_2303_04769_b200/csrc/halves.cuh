@@ -21,6 +21,16 @@ __device__ __forceinline__ int top_exponent(float most) { return min(max((int)(_
 __device__ __forceinline__ float lift(int e) { return __uint_as_float((uint32_t)(268 - e) << 23); }
 __device__ __forceinline__ float drop(int e) { return __uint_as_float((uint32_t)(e - 14) << 23); }
 
+// 2^e for e from -252 to 254 as two factors: x * a * b leaves FP32's range only where x * 2^e does.
+struct TwoFactors {
+    float a, b;
+    __device__ explicit TwoFactors(int e) {
+        const int first = min(max(e, -126), 127);
+        a = __uint_as_float((uint32_t)(first + 127) << 23);
+        b = __uint_as_float((uint32_t)(e - first + 127) << 23);
+    }
+};
+
 // |x|; what is not finite does not count: it stays what it is at any scale, and must not take its tile's other values with it.
 __device__ __forceinline__ float magnitude(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
 

@@ -1,0 +1,36 @@
+"""Adapted 1 x 1 convolutions on the tensor cores over the range of what they are given: filters that are zero or tiny beside their adapters,
+filters and adapters' rows of very different size, long reductions, sums that lose nothing.  Formula as in test_gpu_adapters; the tolerances are the
+math modes' own (gpu_util.TOL) where nothing else is said, taken for each output channel by itself where channels differ in size."""
+import numpy as np
+import pytest
+
+import test_gpu_adapters as A
+from gpu_util import B, TOL, ctx, dev, from_blk, new_blk, rel_err, to_blk
+
+pytestmark = pytest.mark.gpu
+
+
+def on_tensor_cores(layer, N, H, W):
+    assert B.small_adapted_conv2d_workspace_bytes(N, layer.C, layer.K, H, W, layer.R) > 0
+
+
+def by_channel(got, ref):
+    """The largest of the channels' errors: each output channel (N, pixels) measured against its own size."""
+    return max(rel_err(got[:, k], ref[:, k]) for k in range(ref.shape[1]))
+
+
+@pytest.mark.parametrize("mode", A.MODES)
+@pytest.mark.parametrize("exponent", [None, -115, -100])
+def test_adapters_beside_filters_of_next_to_nothing(exponent, mode):
+    """A projection that starts at zero, or far below its adapters: their part, some hundreds here, is the result."""
+    rng = np.random.default_rng(71)
+    layer, x = A.Layer(rng, 96, 160, 16, 3), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    layer.w *= np.float32(0 if exponent is None else 2.0 ** exponent)
+    layer.up *= 100
+    on_tensor_cores(layer, 80, 9, 10)
+    ids = (np.arange(80) % 4 - 1).astype(np.int32)
+    got, ref = layer.run(x, ids, mode), layer.ref(x, ids)
+    assert np.isfinite(got).all() and rel_err(got, ref) <= TOL[mode]
+    none = np.full(80, -1, np.int32)
+    layer.b[:] = 0
+    assert rel_err(layer.run(x, none, mode) * 2.0 ** 100, layer.ref(x, none) * 2.0 ** 100) <= TOL[mode]
