@@ -132,6 +132,10 @@ __device__ __forceinline__ void bulk_store(void *to, uint32_t from, uint32_t byt
 template <int kLeft>
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
 
+__device__ __forceinline__ float4 clear_from(float4 v, int n) {          // the values from the n-th on: 0
+    return make_float4(n > 0 ? v.x : 0.0f, n > 1 ? v.y : 0.0f, n > 2 ? v.z : 0.0f, n > 3 ? v.w : 0.0f);
+}
+
 __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArgs c) {
     extern __shared__ char raw[];                        // a chunk of pixels and one of Down: four blocks a SM hide what each waits for
     __shared__ int ex_s[kTile], full_s[kTile];           // the pixels' exponents, and what they would be without t
@@ -183,6 +187,11 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
 #pragma unroll
             for (int i = 0; i < kTile / 32; ++i)
                 v[g][i] = r0 + i * 32 < pixels && cb + g < s.CB ? __ldg(reinterpret_cast<const float4 *>(x + ((size_t)(cb + g) * a.HW + r0 + i * 32) * 32 + c0)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if ((cb + 2) * 32 > s.C)                         // pad lanes, whatever lies there, here and below
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < kTile / 32; ++i) v[g][i] = clear_from(v[g][i], s.C - (cb + g) * 32 - c0);
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -237,17 +246,11 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
             }
             __syncthreads();
         }
-        if ((k * 2 + 2) * 32 > s.C)                      // pad lanes, whatever lies there
+        if ((k * 2 + 2) * 32 > s.C)
 #pragma unroll
             for (int g = 0; g < 2; ++g)
 #pragma unroll
-                for (int i = 0; i < kTile / 32; ++i) {
-                    const int ch = (k * 2 + g) * 32 + c0;
-                    if (ch + 0 >= s.C) v2[g][i].x = 0.0f;
-                    if (ch + 1 >= s.C) v2[g][i].y = 0.0f;
-                    if (ch + 2 >= s.C) v2[g][i].z = 0.0f;
-                    if (ch + 3 >= s.C) v2[g][i].w = 0.0f;
-                }
+                for (int i = 0; i < kTile / 32; ++i) v2[g][i] = clear_from(v2[g][i], s.C - (k * 2 + g) * 32 - c0);
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll

@@ -34,3 +34,17 @@ def test_adapters_beside_filters_of_next_to_nothing(exponent, mode):
     none = np.full(80, -1, np.int32)
     layer.b[:] = 0
     assert rel_err(layer.run(x, none, mode) * 2.0 ** 100, layer.ref(x, none) * 2.0 ** 100) <= TOL[mode]
+
+
+@pytest.mark.parametrize("fill", [1e20, float("inf"), float("nan")])
+def test_pad_lanes_that_hold_anything_have_no_part(fill):
+    rng = np.random.default_rng(76)
+    layer, x = A.Layer(rng, 72, 160, 16, 3), rng.standard_normal((80, 72, 9, 10)).astype(np.float32)
+    on_tensor_cores(layer, 80, 9, 10)
+    ids = (np.arange(80) % 4 - 1).astype(np.int32)
+    layer.pack("3xtf32")
+    blk, out = to_blk(x), new_blk(80, 160, 9, 10)
+    blk.view(80, 3, 90, 32)[:, 2, :, 8:] = fill
+    layer.call(blk, dev(ids), out, layer.workspace(80, 9, 10), 80, 9, 10, B.MATH_3XTF32)
+    assert rel_err(from_blk(out, 80, 160, 9, 10), layer.ref(x, ids)) <= TOL["3xtf32"]
+    assert B.small_device_status(ctx()) == B.OK
