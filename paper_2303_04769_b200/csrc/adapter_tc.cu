@@ -24,6 +24,7 @@ using namespace halves;
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 64;               // channels
+constexpr int kDownRun = 4;              // chunks whose products with Down one accumulator takes (see kRun)
 constexpr uint32_t kPixelBytes = kTile * 256, kRankBytes = kTile * 128;          // of a chunk of channels, of 32 ranks
 constexpr int kCluster = 8, kTeams = 4, kKept = 6;       // blocks of adapter_filters_kernel, teams of 256 threads of a block, items of a team in registers
 
@@ -147,6 +148,7 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     const int n = blockIdx.x / c.at.tiles, pt = blockIdx.x % c.at.tiles, p0 = pt * kTile, pixels = min(kTile, a.HW - p0);
     const int warp = warp_index(), lane = threadIdx.x & 31;
     char *chunk = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u), *down_chunk = chunk + kPixelBytes;
+    float *t_sums = reinterpret_cast<float *>(down_chunk + s.RQ * 256);          // [rank][row], of runs of chunks, where there are several
     const uint32_t down_bytes = s.RQ * 256, down = smem_u32(&down_s), used = smem_u32(&used_s);
     const uint32_t columns = s.RQ <= 32 ? 32 : s.RQ <= 64 ? 64 : 128;
     // What is read here is older than the kernel in front of this one, which has waited for all before itself; its result comes after the wait.
@@ -232,6 +234,20 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     const uint32_t tmem = tmem_s, desc = f16_desc(s.RQ);
     for (int step = 0, k = 0; step < steps; ++step, k = k == s.chunks - 1 ? 0 : k + 1) {
         const bool multiply = some && step < s.chunks, keep = step >= steps - s.chunks;
+        if (multiply && step && step % kDownRun == 0) {  // a run's products join the sums, as in adapter_product_kernel
+            if (warp == 0) mbar_wait_uniform(used, step - 1 & 1, &gave_up, c.status, c.limit);
+            __syncthreads();
+            tc_fence_after();
+            for (int rb = warp >> 2; rb < s.RB; rb += 2) {
+                float v[32];
+                tmem_ld32(tmem + rb * 32 + ((uint32_t)(warp & 3) << 21), v);
+                float *t = t_sums + rb * 32 * kTile + (warp & 3) * 32 + lane;
+#pragma unroll
+                for (int u = 0; u < 32; ++u)
+                    if (rb * 32 + u < s.RQ) t[u * kTile] = step == kDownRun ? v[u] : t[u * kTile] + v[u];
+            }
+            tc_fence_before();
+        }
         float4 v2[2][kTile / 32];                        // on its way while the chunk before is written out and multiplied
 #pragma unroll
         for (int g = 0; g < 2; ++g)
@@ -267,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
                     for (int term = 0; term < 3; ++term)             // small terms first
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            mma_f16(tmem, xa + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), wa + e * 2 + (term == 1 ? s.RQ * 8 : 0), desc, k > 0 || e > 0 || term > 0);
+                            mma_f16(tmem, xa + e * 2 + (term == 0 ? kPixelBytes / 32 : 0), wa + e * 2 + (term == 1 ? s.RQ * 8 : 0), desc, k % kDownRun > 0 || e > 0 || term > 0);
                     mma_commit(used);
                 }
             }
@@ -285,6 +301,10 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
             char *to = ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes;
             float v[32];
             tmem_ld32(tmem + rb * 32 + ((uint32_t)(warp & 3) << 21), v);
+            if (s.chunks > kDownRun)
+#pragma unroll
+                for (int u = 0; u < 32; ++u)
+                    if (rb * 32 + u < s.RQ) v[u] += t_sums[(rb * 32 + u) * kTile + row];
 #pragma unroll
             for (int u = 0; u < 32; u += 4) {
                 // columns behind RQ have no product in them
@@ -309,9 +329,10 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     }
 }
 
-// The tensor core cuts its accumulator off at 24 bits at each step: on the average by 0.36 * 2^-23 of what stands there, which is half the
-// result over the steps of a sum.  That much is given back; what is left of 1.1e-6 (256 channels, 51 steps, relative to the result) is its scatter, 6e-7.
-constexpr float kCutOff = 0.5f * 0.36f / (1 << 23);
+// The tensor core cuts its accumulator off at 24 bits at each step, on the average by 0.36 * 2^-23 of what stands there: what a result loses that way
+// grows with the steps of a sum and is lost on one side.  So an accumulator takes a run of chunks, and the epilogue adds the runs' products in FP32
+// registers, where sums are rounded; sums that lose nothing stay exact.
+template <bool kX3> constexpr int kRun = kX3 ? 2 : 8;        // chunks
 
 constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, kProductThreads = 320;
 
@@ -390,31 +411,34 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         }
     } else if (warp == 9) {
         const uint32_t first = smem_desc_lo(smem_u32(stages));
-        int slot = 0, phase = 0, buffer = 0, buffer_phase = 1;
+        int slot = 0, phase = 0, buffer = 0, buffer_phase = 1, turn = 0;
         bool ok = true;
-        for (int i = blockIdx.x, turn = 0; i < work && ok; i += gridDim.x, ++turn) {
+        for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, rows = tile_rows(c, i % c.at.filter_tiles), ranks = ranks_of(np);
-            const uint32_t desc = f16_desc(rows), d = tmem + buffer * 256;
-            if (turn >= 2 && !(ok = mbar_wait_uniform(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
-            for (int k = 0; k < c.s.chunks + ranks; ++k) {
+            const uint32_t desc = f16_desc(rows);
+            for (int k = 0, in_run = 0; k < c.s.chunks + ranks; ++k) {
+                if (in_run == 0 && turn >= 2 && !(ok = mbar_wait_uniform(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
+                const uint32_t d = tmem + buffer * 256;
                 const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
                 if (!(ok = mbar_wait_uniform(full + slot * 16, phase, stop, c.status, c.limit))) break;
                 tc_fence_after();
                 if (kX3) {                               // small terms first: low pixels and high filters while the rest is on its way
                     if (k < c.s.chunks && elect_one())
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) mma_f16(d, x + e * 2 + kPixelBytes / 32, w + e * 2, desc, k > 0 || e > 0);
+                        for (int e = 0; e < 4; ++e) mma_f16(d, x + e * 2 + kPixelBytes / 32, w + e * 2, desc, in_run > 0 || e > 0);
                     __syncwarp();
                     if (!(ok = mbar_wait_uniform(full + slot * 16 + 8, phase, stop, c.status, c.limit))) break;
                     tc_fence_after();
                 }
+                // the ranks' steps belong to the last run of channels
+                const bool last = k == c.s.chunks + ranks - 1 || (in_run == kRun<kX3> - 1 && k < c.s.chunks - 1);
                 if (elect_one()) {
                     if (k < c.s.chunks) {
 #pragma unroll
                         for (int term = kX3 ? 1 : 2; term < 3; ++term)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                mma_f16(d, x + e * 2, w + e * 2 + (term == 1 ? rows * 8 : 0), desc, kX3 || k > 0 || e > 0);
+                                mma_f16(d, x + e * 2, w + e * 2 + (term == 1 ? rows * 8 : 0), desc, kX3 || in_run > 0 || e > 0);
                     } else {
                         const int steps = (min(s.R - (k - c.s.chunks) * 32, 32) + 15) / 16;
 #pragma unroll
@@ -422,12 +446,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                             for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, 1);
                     }
                     mma_commit(empty + slot * 8);
-                    if (k == c.s.chunks + ranks - 1) mma_commit(done + buffer * 8);
+                    if (last) mma_commit(done + buffer * 8);
                 }
                 __syncwarp();
                 if (++slot == kStages) { slot = 0; phase ^= 1; }
+                ++in_run;
+                if (last) {
+                    in_run = 0;
+                    ++turn;
+                    if (++buffer == 2) { buffer = 0; buffer_phase ^= 1; }
+                }
             }
-            if (++buffer == 2) { buffer = 0; buffer_phase ^= 1; }
         }
         if (!ok) {
             if (elect_one()) mma_commit(smem_u32(&drained));
@@ -443,13 +472,34 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
             // undoes both operands' scaling: the pixel's and the filters' parts may each pass FP32's range where the result does not
             const TwoFactors back(exponents(c)[4 + (size_t)np * kTile + (warp & 3) * 32 + lane] + w_exponent - 2 * 141);
-            const float grown = (1.0f + kCutOff * (float)((kX3 ? 3 : 1) * (s.chunks * (kChunk / 16) + (ranks_of(np) ? (s.R + 15) / 16 : 0))));
-            if (!mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit)) break;
-            tc_fence_after();
             const int blocks = tile_rows(c, kt) / 32;
-            for (int b = half; b < blocks; b += 2) {
-                float v[32];
-                tmem_ld32(tmem + buffer * 256 + b * 32 + ((uint32_t)(warp & 3) << 21), v);
+            float sum[kFilterTile / 2][32] = {};         // of this warp's blocks of filters
+            bool given_up = false;
+#pragma unroll 1
+            for (int k = 0; k < c.s.chunks; k += kRun<kX3>) {
+                if ((given_up = !mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int e = 0; e < kFilterTile / 2; ++e) {
+                    if (half + e * 2 >= blocks) continue;
+#pragma unroll
+                    for (int g = 0; g < 32; g += 16) {
+                        float v[16];
+                        tmem_ld16(tmem + buffer * 256 + (half + e * 2) * 32 + g + ((uint32_t)(warp & 3) << 21), v);
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) sum[e][g + u] += v[u];
+                    }
+                }
+                tc_fence_before();
+                mbar_arrive(free + buffer * 8);
+                if (++buffer == 2) { buffer = 0; phase ^= 1; }
+            }
+            if (given_up) break;
+#pragma unroll
+            for (int e = 0; e < kFilterTile / 2; ++e) {
+                const int b = half + e * 2;
+                if (b >= blocks) continue;
+                const float (&v)[32] = sum[e];
                 // through shared memory, so that a store is whole lines: eight lanes a pixel
 #pragma unroll
                 for (int u = 0; u < 8; ++u)
@@ -467,7 +517,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                 for (int u = 0; u < 8; ++u) {
                     const int r = u * 4 + (lane >> 3);
                     float4 y = rows[r * 8 + ((lane & 7) ^ (r & 7))];
-                    y.x = fmaf(y.x, grown, add.x); y.y = fmaf(y.y, grown, add.y); y.z = fmaf(y.z, grown, add.z); y.w = fmaf(y.w, grown, add.w);
+                    y.x += add.x; y.y += add.y; y.z += add.z; y.w += add.w;
                     if (p0 + r >= a.HW) continue;
                     if (a.accumulate) {
                         const float4 before = out[u * 32];
@@ -479,9 +529,6 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                 }
                 __syncwarp();
             }
-            tc_fence_before();
-            mbar_arrive(free + buffer * 8);
-            if (++buffer == 2) { buffer = 0; phase ^= 1; }
         }
     }
     tc_fence_before();
@@ -567,8 +614,8 @@ int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s,
     launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads * kTeams), kCluster, 0, st, c);
     if (int e = check_launch(ctx)) return e;
     static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
-    const size_t passing = 1024 + (size_t)kPixelBytes + (size_t)s.RQ * 256, stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;
-    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + kPixelBytes + 128 * 256)) return e;
+    const size_t passing = 1024 + (size_t)kPixelBytes + (size_t)s.RQ * (256 + (s.chunks > kDownRun ? kTile * sizeof(float) : 0)), stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;
+    if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + kPixelBytes + 128 * (256 + kTile * sizeof(float)))) return e;
     launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), passing, st, c);
     if (int e = check_launch(ctx)) return e;
     const int work = a.N * c.at.tiles * c.at.filter_tiles;
