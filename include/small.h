@@ -424,8 +424,10 @@ int small_pack_adapters(small_ctx *ctx, const float *down, const float *up, floa
 /* in: blocked [N][C][H][W]; w_blk: from small_pack_conv_weights(C, K, 1, 1, math); bias: K floats or NULL; adapter: device
  * int32[N]; scale: device float[adapters] or NULL (1); out: blocked [N][K][H][W].  flags: SMALL_RELU, SMALL_ACCUMULATE (out_previous is
  * added in front of the activation) and one SMALL_MATH_* for both parts (few pixels of few channels: FP32 multiply-adds in each).  workspace: device, 16-byte aligned,
- * small_adapted_conv2d_workspace_bytes bytes (operands as halves, scaled by pixel, where the layer runs as one product on the tensor
+ * small_adapted_conv2d_workspace_bytes bytes (operands as halves, scaled by pixel and by filter, where the layer runs as one product on the tensor
  * cores; 0 and NULL where it does not, and NULL in FP32 anywhere); calls that may run at the same time need their own.
+ * There channels 2^17 below the largest of their pixel, and weights 2^17 below the largest of their filter (of Up: of their row, with Down's rows brought
+ * to one size), begin to lose accuracy.
  * Errors as small_conv2d, and WORKSPACE (needed and NULL). */
 size_t small_adapted_conv2d_workspace_bytes(int N, int C, int K, int H, int W, int R);
 int small_adapted_conv2d(small_ctx *ctx, const float *in, const float *w_blk, const float *bias, const float *packed,

@@ -10,12 +10,12 @@ namespace small {
 //   Up     float[adapters][KB][RP][32 filters]
 //   Up     [adapters][filter tiles][RB]{filters of the tile: 128 bytes, 32 high halves and 32 low ones of 32 ranks, swizzled}
 //   Down   [adapters][chunks of 64 channels]{RQ rows of 128 bytes of high halves, the same of low ones, swizzled}     RQ = R rounded up to 16
-//   [adapters]{int, int: the exponents that Up's and Down's halves were scaled by; float: the largest sum of a Down row's magnitudes; unused}
+//   [adapters]{int: Down's exponent; 3 unused; KB * 32 floats: what undoes the scaling of each row of Up}
 // Filter tiles have eight channel blocks, the last one what is left.
 struct AdapterShape {
     int C, K, R, CB, KB, RP, RB, RQ, chunks;
     size_t down, up, up_halves, down_halves;             // floats of one adapter
-    size_t up_halves_at, down_halves_at, info_at, floats;
+    size_t up_halves_at, down_halves_at, info_at, info, floats;
     AdapterShape(int adapters, int C, int K, int R) : C(C), K(K), R(R), CB(blocks_of(C)), KB(blocks_of(K)), RP((R + 7) / 8 * 8), RB(blocks_of(R)),
           RQ((R + 15) / 16 * 16), chunks((C + 63) / 64) {
         down = (size_t)CB * RP * 32;
@@ -25,7 +25,8 @@ struct AdapterShape {
         up_halves_at = (down + up) * adapters;
         down_halves_at = up_halves_at + up_halves * adapters;
         info_at = down_halves_at + down_halves * adapters;
-        floats = info_at + 4 * (size_t)adapters;
+        info = 4 + (size_t)KB * 32;
+        floats = info_at + info * adapters;
     }
 };
 constexpr int kFilterTile = 8;           // channel blocks of filters

@@ -2,19 +2,17 @@
 // behind an image's channels, and s_a Up_a behind the filters, so that the adapter costs some more steps of the reduction and the result is
 // written once.  Operands are pairs of halves (halves.cuh).
 //
-// adapter_filters_kernel: the filters as halves, 64 channels a chunk, one exponent for the layer (a cluster finds it).
+// adapter_filters_kernel: the filters as halves, 64 channels a chunk, each filter brought to the same size by a power of two.
 // adapter_pixels_kernel: 128 pixels of an image a block: each one's largest value in one pass over them (from memory), halves in a second (from
-//   L2), which pass through shared memory, where the product with Down is taken from them.  t shares the pixels' accumulator later, so its
-//   exponent follows from theirs, the filters' and the adapter's; where t could pass half precision's range - it is at most the largest value
-//   times the largest sum of a Down row's magnitudes - the pixel takes a smaller scale, 2 to 5 powers of two as a rule, of 17 that halves of both
-//   kinds have to spare.
+//   L2), which pass through shared memory, where the product with Down is taken from them.  t becomes halves by pixel, too.
 // adapter_product_kernel: a block walks tiles of 128 pixels x 256 filters; warps for loading (plain bulk copies, two stages of 96 KB), MMAs
-//   and the epilogue (bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a tile runs beside the next.
+//   and the epilogue (scales, sums, bias, previous output, ReLU), two accumulators in tensor memory so that the epilogue of a run runs beside the
+//   next.  t times Up is a run of its own, because rows of Up are brought to one size whatever the filters' is.
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
 //
-// Batch 64, 256 -> 768, 28 x 28, rank 16: 111 to 124 us (operands from L2 or not).  Pixels 37 (the filters, 12, beside them): the largest values, while
-// memory still takes the result before, then four chunks that wait for their loads.  Product 72: MMAs 58 % of the time, the rest a stage
-// waits for its load.  Floor 33 for the bytes, 37 for three products.
+// Batch 64, 256 -> 768, 28 x 28, rank 16: 164 us.  Pixels 37 (the filters, 5, beside them): the largest values, while memory still takes the result
+// before, then four chunks that wait for their loads.  Product 105: the epilogue, two thirds of it in its stores and waits for scales.  Floor 33 for
+// the bytes, 37 for three products.
 #include "adapter.cuh"
 #include "halves.cuh"
 
@@ -26,7 +24,7 @@ constexpr int kThreads = 256;
 constexpr int kChunk = 64;               // channels
 constexpr int kDownRun = 4;              // chunks whose products with Down one accumulator takes (see kRun)
 constexpr uint32_t kPixelBytes = kTile * 256, kRankBytes = kTile * 128;          // of a chunk of channels, of 32 ranks
-constexpr int kCluster = 8, kTeams = 4, kKept = 6;       // blocks of adapter_filters_kernel, teams of 256 threads of a block, items of a team in registers
+constexpr int kTeams = 4, kKept = 4;     // teams of 256 threads of adapter_filters_kernel, channel blocks of a team in registers
 
 struct Layout {
     int tiles, filter_tiles;             // pixel tiles of an image
@@ -37,7 +35,7 @@ struct Layout {
         ranks_at = (size_t)N * tiles * chunks * kPixelBytes;
         filters_at = ranks_at + (size_t)N * tiles * blocks_of(R) * kRankBytes;
         scales_at = filters_at + (size_t)chunks * blocks_of(K) * 32 * 256;
-        bytes = scales_at + sizeof(int) * ((size_t)N * tiles * kTile + 4);       // exponents: the filters', three words unused, each pixel's
+        bytes = scales_at + sizeof(float) * (size_t)blocks_of(K) * 32 + sizeof(int2) * (size_t)N * tiles * kTile;
     }
 };
 
@@ -50,81 +48,83 @@ struct TcArgs {
 };
 
 __device__ __forceinline__ char *ws_of(const TcArgs &c) { return static_cast<char *>(c.a.ws); }
-__device__ __forceinline__ int *exponents(const TcArgs &c) { return reinterpret_cast<int *>(ws_of(c) + c.at.scales_at); }
+// What undoes the scaling: each filter's factor; the exponents of each pixel's x (+ 141) and t.
+__device__ __forceinline__ float *filter_factors(const TcArgs &c) { return reinterpret_cast<float *>(ws_of(c) + c.at.scales_at); }
+__device__ __forceinline__ int2 *pixel_exponents(const TcArgs &c) { return reinterpret_cast<int2 *>(filter_factors(c) + c.s.KB * 32); }
+// Of an adapter's packed scales: the first word, Down's exponent; Up's factors from the fifth on.
+template <typename T> __device__ __forceinline__ T *info_of(T *packed, const AdapterShape &s, int id) { return packed + s.info_at + id * s.info; }
 __device__ __forceinline__ int tile_rows(const TcArgs &c, int kt) { return min(kFilterTile, c.s.KB - kt * kFilterTile) * 32; }
-__device__ __forceinline__ float block_max(float v, float *s) {
-#pragma unroll
-    for (int o = 16; o; o /= 2) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = s[0];
-#pragma unroll
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) v = fmaxf(v, s[i]);
-    return v;
-}
-
-// The FP32 section of the packed filters, [KB][CB][32 channels][32 filters], as halves [filter tile][chunk]{high: rows x 128 bytes, low: the same}.
+// The FP32 section of the packed filters, [KB][CB][32 channels][32 filters], as halves [filter tile][chunk]{high: rows x 128 bytes, low: the same}, a
+// block 32 filters: each one's largest value, then its halves.
 __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const TcArgs c) {
-    __shared__ float most_s[kThreads * kTeams / 32], top, blocks[kTeams][32][33];
+    __shared__ float most_s[kThreads * kTeams / 32][32], blocks[kTeams][32][33];
+    __shared__ int ex_s[32];
     grid_dep_sync();
     grid_dep_trigger();
-    const int items = c.s.KB * c.s.chunks * 2, tid = threadIdx.x % kThreads, team = blockIdx.x * kTeams + threadIdx.x / kThreads;
-    const float4 *w = reinterpret_cast<const float4 *>(c.a.w);
-    auto fetch = [&](int i) {
-        const int kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2);
-        return i < items && cb < c.s.CB ? __ldg(w + ((size_t)kb * c.s.CB + cb) * 256 + tid) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const int items = c.s.chunks * 2, tid = threadIdx.x % kThreads, team = threadIdx.x / kThreads, lane = threadIdx.x & 31, kb = blockIdx.x, kt = kb / kFilterTile;
+    const int rows = tile_rows(c, kt);
+    const float4 *w = reinterpret_cast<const float4 *>(c.a.w) + (size_t)kb * c.s.CB * 256 + tid;
+    auto fetch = [&](int cb) { return cb < c.s.CB ? __ldg(w + (size_t)cb * 256) : make_float4(0.f, 0.f, 0.f, 0.f); };
+    float4 most = make_float4(0.f, 0.f, 0.f, 0.f);       // of filters (tid & 7) * 4 and the next three
+    auto count = [&](const float4 &v) {
+        most = make_float4(fmaxf(most.x, magnitude(v.x)), fmaxf(most.y, magnitude(v.y)), fmaxf(most.z, magnitude(v.z)), fmaxf(most.w, magnitude(v.w)));
     };
-    float most = 0.0f;
     float4 kept[kKept];                                  // the first ones stay in registers
 #pragma unroll
-    for (int e = 0; e < kKept; ++e) kept[e] = fetch(team + e * kCluster * kTeams);
+    for (int e = 0; e < kKept; ++e) kept[e] = fetch(team + e * kTeams);
 #pragma unroll
-    for (int e = 0; e < kKept; ++e) most = fmaxf(most, magnitude(kept[e]));
-    for (int i = team + kKept * kCluster * kTeams; i < items; i += 4 * kCluster * kTeams) {
+    for (int e = 0; e < kKept; ++e) count(kept[e]);
+    for (int i = team + kKept * kTeams; i < items; i += 4 * kTeams) {
         float4 v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fetch(i + e * kCluster * kTeams);
+        for (int e = 0; e < 4; ++e) v[e] = fetch(i + e * kTeams);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) most = fmaxf(most, magnitude(v[e]));
+        for (int e = 0; e < 4; ++e) count(v[e]);
     }
-    most = block_max(most, most_s);
-    if (threadIdx.x == 0) top = most;
-    cluster_arrive();
-    cluster_wait();
 #pragma unroll
-    for (int b = 0; b < kCluster; ++b) most = fmaxf(most, cluster_read(&top, b));
-    cluster_arrive();
-    const int ex = top_exponent(most);
-    const float up = lift(ex);
-    if (blockIdx.x == 0 && threadIdx.x == 0) exponents(c)[0] = ex;
-    char *out = ws_of(c) + c.at.filters_at;
-    float (*block)[33] = blocks[threadIdx.x / kThreads];
-    auto lay_out = [&](int i, const float4 &v, auto ahead) {
-        const int kb = i / (c.s.chunks * 2), cb = i % (c.s.chunks * 2), kt = kb / kFilterTile;
+    for (int o = 8; o < 32; o *= 2) {
+        most.x = fmaxf(most.x, __shfl_xor_sync(~0u, most.x, o)); most.y = fmaxf(most.y, __shfl_xor_sync(~0u, most.y, o));
+        most.z = fmaxf(most.z, __shfl_xor_sync(~0u, most.z, o)); most.w = fmaxf(most.w, __shfl_xor_sync(~0u, most.w, o));
+    }
+    if (lane < 8) *reinterpret_cast<float4 *>(&most_s[threadIdx.x >> 5][lane * 4]) = most;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kThreads * kTeams / 32; ++i) m = fmaxf(m, most_s[i][lane]);
+        ex_s[lane] = top_exponent(m);
+        filter_factors(c)[kb * 32 + lane] = drop(ex_s[lane]);
+    }
+    __syncthreads();
+    // a thread's four channels of filter f
+    const int f = tid >> 3, c0 = (tid & 7) * 4, row = kb % kFilterTile * 32 + f;
+    const float up = lift(ex_s[f]);
+    const bool real = kb * 32 + f < c.s.K;
+    char *out = ws_of(c) + c.at.filters_at + (size_t)kt * c.s.chunks * kFilterTile * 32 * 256;
+    float (*block)[33] = blocks[team];
+    auto lay_out = [&](int cb, const float4 &v, auto ahead) {
         __syncthreads();
         const int ch = tid >> 3, f0 = (tid & 7) * 4;
         block[f0][ch] = v.x; block[f0 + 1][ch] = v.y; block[f0 + 2][ch] = v.z; block[f0 + 3][ch] = v.w;
         ahead();
         __syncthreads();
-        if (i >= items) return;
-        const int f = tid >> 3, c0 = (tid & 7) * 4, rows = tile_rows(c, kt), row = kb % kFilterTile * 32 + f, col = (cb & 1) * 32 + c0;
-        const bool real = kb * 32 + f < c.s.K;
+        if (cb >= items) return;
+        const int col = (cb & 1) * 32 + c0;
         uint2 hi, lo;
         split_finite(real ? block[f][c0] * up : 0.0f, real ? block[f][c0 + 1] * up : 0.0f, hi.x, lo.x);
         split_finite(real ? block[f][c0 + 2] * up : 0.0f, real ? block[f][c0 + 3] * up : 0.0f, hi.y, lo.y);
-        char *to = out + ((size_t)kt * c.s.chunks * kFilterTile * 32 + (size_t)(cb >> 1) * rows) * 256;
+        char *to = out + (size_t)(cb >> 1) * rows * 256;
         *reinterpret_cast<uint2 *>(to + chunk_at(row, col, rows) + (col & 4) * 2) = hi;
         *reinterpret_cast<uint2 *>(to + chunk_at(row, kChunk + col, rows) + (col & 4) * 2) = lo;
     };
 #pragma unroll
     for (int e = 0; e < kKept; ++e)
-        if (e * kCluster * kTeams < items) lay_out(team + e * kCluster * kTeams, kept[e], [] {});
-    float4 v = fetch(team + kKept * kCluster * kTeams);
-    for (int i0 = kKept * kCluster * kTeams; i0 < items; i0 += kCluster * kTeams) {
+        if (e * kTeams < items) lay_out(team + e * kTeams, kept[e], [] {});
+    float4 v = fetch(team + kKept * kTeams);
+    for (int i0 = kKept * kTeams; i0 < items; i0 += kTeams) {
         const float4 now = v;
-        lay_out(i0 + team, now, [&] { v = fetch(i0 + team + kCluster * kTeams); });
+        lay_out(i0 + team, now, [&] { v = fetch(i0 + team + kTeams); });
     }
-    cluster_wait();                                      // the others have read this block's maximum
 }
 
 __device__ __forceinline__ void bulk_store(void *to, uint32_t from, uint32_t bytes) {
@@ -139,7 +139,8 @@ __device__ __forceinline__ float4 clear_from(float4 v, int n) {          // the 
 
 __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArgs c) {
     extern __shared__ char raw[];                        // a chunk of pixels and one of Down: four blocks a SM hide what each waits for
-    __shared__ int ex_s[kTile], full_s[kTile];           // the pixels' exponents, and what they would be without t
+    __shared__ int ex_s[kTile];                          // the pixels' exponents
+    __shared__ float t_most_s[2][kTile];
     __shared__ uint64_t down_s, used_s;
     __shared__ uint32_t tmem_s;
     __shared__ int gave_up;
@@ -204,38 +205,23 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
 #pragma unroll
         for (int o = 1; o < 8; o *= 2) most[i] = fmaxf(most[i], __shfl_xor_sync(~0u, most[i], o));
     __syncthreads();                                     // (tensor memory is allocated)
-    grid_dep_sync();                                     // the filters' exponent
+    grid_dep_sync();                                     // what follows is written where an earlier call may still read
     grid_dep_trigger();
-    const float *info = a.packed + s.info_at + 4 * (size_t)(some ? id : 0);
-    const float by = some && a.scale ? a.scale[id] : 1.0f, sums = info[2] * magnitude(by);
-    const int ew = exponents(c)[0], eu = __float_as_int(info[0]), ed = __float_as_int(info[1]);
     float up[kTile / 32];
-    int shrunk = 0;                                      // by how much a pixel's scale is smaller for t's sake
 #pragma unroll
     for (int i = 0; i < kTile / 32; ++i) {
-        int ex = top_exponent(most[i]);
-        if (some) {
-            const int room = min(max(ex, top_exponent(most[i] * sums) + eu - ew), 254);
-            shrunk = max(shrunk, room - ex);
-            ex = room;
-        }
+        const int ex = top_exponent(most[i]);
         up[i] = lift(ex);
         if (c0 == 0) {
             ex_s[r0 + i * 32] = ex;
-            full_s[r0 + i * 32] = top_exponent(most[i]);
-            exponents(c)[4 + (size_t)blockIdx.x * kTile + r0 + i * 32] = ex;
+            pixel_exponents(c)[(size_t)blockIdx.x * kTile + r0 + i * 32].x = ex;
         }
     }
-    // t is taken from the halves that are written - unless so little is left of them (an adapter far larger than the filters) that t would suffer:
-    // then from halves of their own, at the pixels' full scale, in a pass in front.
-    const bool apart = __syncthreads_or(shrunk > 8);
-    const int steps = apart ? 2 * s.chunks : s.chunks;
     char *out = ws_of(c) + (size_t)blockIdx.x * s.chunks * kPixelBytes;
     const uint32_t tmem = tmem_s, desc = f16_desc(s.RQ);
-    for (int step = 0, k = 0; step < steps; ++step, k = k == s.chunks - 1 ? 0 : k + 1) {
-        const bool multiply = some && step < s.chunks, keep = step >= steps - s.chunks;
-        if (multiply && step && step % kDownRun == 0) {  // a run's products join the sums, as in adapter_product_kernel
-            if (warp == 0) mbar_wait_uniform(used, step - 1 & 1, &gave_up, c.status, c.limit);
+    for (int k = 0; k < s.chunks; ++k) {
+        if (some && k && k % kDownRun == 0) {            // a run's products join the sums, as in adapter_product_kernel
+            if (warp == 0) mbar_wait_uniform(used, k - 1 & 1, &gave_up, c.status, c.limit);
             __syncthreads();
             tc_fence_after();
             for (int rb = warp >> 2; rb < s.RB; rb += 2) {
@@ -244,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
                 float *t = t_sums + rb * 32 * kTile + (warp & 3) * 32 + lane;
 #pragma unroll
                 for (int u = 0; u < 32; ++u)
-                    if (rb * 32 + u < s.RQ) t[u * kTile] = step == kDownRun ? v[u] : t[u * kTile] + v[u];
+                    if (rb * 32 + u < s.RQ) t[u * kTile] = k == kDownRun ? v[u] : t[u * kTile] + v[u];
             }
             tc_fence_before();
         }
@@ -254,11 +240,13 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
 #pragma unroll
             for (int i = 0; i < kTile / 32; ++i)
                 v2[g][i] = r0 + i * 32 < pixels && k * 2 + g < s.CB ? __ldg(reinterpret_cast<const float4 *>(x + ((size_t)(k * 2 + g) * a.HW + r0 + i * 32) * 32 + c0)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        if (step) {
+        if (k) {
             if (warp == 0) {
                 bulk_store_wait<0>();
-                if (some && step <= s.chunks) mbar_wait_uniform(used, step - 1 & 1, &gave_up, c.status, c.limit);
-                if (multiply) load_down(k);
+                if (some) {
+                    mbar_wait_uniform(used, k - 1 & 1, &gave_up, c.status, c.limit);
+                    load_down(k);
+                }
             }
             __syncthreads();
         }
@@ -270,15 +258,15 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v2[g][i], keep ? up[i] : lift(top_exponent(most[i])));
+            for (int i = 0; i < kTile / 32; ++i) store4<kChunk>(chunk, r0 + i * 32, g * 32 + c0, v2[g][i], up[i]);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
         if (warp == 0) {
-            if (multiply) mbar_wait_uniform(down, k & 1, &gave_up, c.status, c.limit);
+            if (some) mbar_wait_uniform(down, k & 1, &gave_up, c.status, c.limit);
             tc_fence_after();
             if (elect_one()) {
-                if (keep) bulk_store(out + (size_t)k * kPixelBytes, smem_u32(chunk), kPixelBytes);
-                if (multiply) {
+                bulk_store(out + (size_t)k * kPixelBytes, smem_u32(chunk), kPixelBytes);
+                if (some) {
                     const uint32_t xa = smem_desc_lo(smem_u32(chunk)), wa = smem_desc_lo(smem_u32(down_chunk));
                     for (int term = 0; term < 3; ++term)             // small terms first
 #pragma unroll
@@ -293,26 +281,40 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
     if (some) {
         mbar_wait_uniform(used, s.chunks - 1 & 1, &gave_up, c.status, c.limit);
         tc_fence_after();
-        const int row = (warp & 3) * 32 + lane, ex = ex_s[row];
-        const int et = ex + ew - eu;                     // t * lift(et) beside halves of Up meets the pixel's scale beside halves of the filters
-        const float x_drop = drop(apart ? full_s[row] : ex);
-        const float factor = et <= 254 ? by * drop(ed) : 0.0f, up_t = lift(min(max(et, 15), 254));       // (beyond: 2^-100 of the sum and less, nothing)
-        for (int rb = warp >> 2; rb < s.RB; rb += 2) {   // a thread a pixel and 32 ranks
-            char *to = ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes;
-            float v[32];
-            tmem_ld32(tmem + rb * 32 + ((uint32_t)(warp & 3) << 21), v);
-            if (s.chunks > kDownRun)
+        // a thread a pixel and 16 of each 32 ranks: the pixel's largest t, then halves of them
+        const int row = (warp & 3) * 32 + lane, half = warp >> 2;
+        float by = a.scale ? a.scale[id] : 1.0f;
+        int far = 0;                                     // exponent of a scale that is taken in parts
+        if (fabsf(by) < 0x1p-60f) { by *= 0x1p100f; far = -100; }
+        if (fabsf(by) > 0x1p60f && fabsf(by) < INFINITY) { by *= 0x1p-100f; far = 100; }
+        auto ranks = [&](int rb, float (&t)[16]) {
+            tmem_ld16(tmem + rb * 32 + half * 16 + ((uint32_t)(warp & 3) << 21), t);
 #pragma unroll
-                for (int u = 0; u < 32; ++u)
-                    if (rb * 32 + u < s.RQ) v[u] += t_sums[(rb * 32 + u) * kTile + row];
-#pragma unroll
-            for (int u = 0; u < 32; u += 4) {
-                // columns behind RQ have no product in them
-                const bool real = rb * 32 + u < s.RQ && row < pixels;
-                const float4 t = real ? make_float4(v[u] * x_drop * factor, v[u + 1] * x_drop * factor, v[u + 2] * x_drop * factor, v[u + 3] * x_drop * factor)
-                                      : make_float4(0.f, 0.f, 0.f, 0.f);
-                store4<32>(to, row, u, t, up_t);
+            for (int u = 0; u < 16; ++u) {
+                const int r = rb * 32 + half * 16 + u;
+                if (s.chunks > kDownRun && r < s.RQ) t[u] += t_sums[r * kTile + row];
+                t[u] = r < s.RQ && row < pixels ? t[u] * by : 0.0f;              // (columns behind RQ have no product in them)
             }
+        };
+        float most_t = 0.0f;
+        for (int rb = 0; rb < s.RB; ++rb) {
+            float t[16];
+            ranks(rb, t);
+#pragma unroll
+            for (int u = 0; u < 16; ++u) most_t = fmaxf(most_t, magnitude(t[u]));
+        }
+        t_most_s[half][row] = most_t;
+        __syncthreads();
+        const int et = top_exponent(fmaxf(most_t, t_most_s[half ^ 1][row]));
+        const float up_t = lift(et);
+        if (half == 0)
+            pixel_exponents(c)[(size_t)blockIdx.x * kTile + row].y = et + ex_s[row] + __float_as_int(*info_of(a.packed, s, id)) - 3 * 141 + far;
+        for (int rb = 0; rb < s.RB; ++rb) {
+            char *to = ws_of(c) + c.at.ranks_at + ((size_t)blockIdx.x * s.RB + rb) * kRankBytes;
+            float t[16];
+            ranks(rb, t);
+#pragma unroll
+            for (int u = 0; u < 16; u += 4) store4<32>(to, row, half * 16 + u, make_float4(t[u], t[u + 1], t[u + 2], t[u + 3]), up_t);
         }
     }
     if (warp == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -380,7 +382,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
             const char *u = reinterpret_cast<const char *>(a.packed + s.up_halves_at + id * s.up_halves) + (size_t)kt * s.RB * kFilterTile * 32 * 128;
             for (int k = 0; k < c.s.chunks + ranks; ++k) {
                 if (issued >= kStages && !(ok = mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit))) break;
-                const int rb = k - c.s.chunks;
+                const int rb = k < ranks ? k : -1, ch = k - ranks;
                 if (elect_one()) {
                     const uint32_t to = smem_u32(stages + slot * kStageBytes), bar = full + slot * 16;
                     auto load = [&](uint32_t at, const char *from, uint32_t bytes, uint32_t b) {
@@ -392,7 +394,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                         load(kPixelBytes, u + (size_t)rb * rows * 128, rows * 128, bar);
                         if (kX3) mbar_arrive(bar + 8);
                     } else {                             // high parts lie in front; the terms begin with low pixels and high filters
-                        const char *fx = x + (size_t)k * kPixelBytes, *fw = w + (size_t)k * rows * 256;
+                        const char *fx = x + (size_t)ch * kPixelBytes, *fw = w + (size_t)ch * rows * 256;
                         const uint32_t half = kPixelBytes / 2;
                         mbar_expect_tx(bar, half + rows * 128);
                         load(kX3 ? half : 0, kX3 ? fx + half : fx, half, bar);
@@ -423,27 +425,27 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                 if (!(ok = mbar_wait_uniform(full + slot * 16, phase, stop, c.status, c.limit))) break;
                 tc_fence_after();
                 if (kX3) {                               // small terms first: low pixels and high filters while the rest is on its way
-                    if (k < c.s.chunks && elect_one())
+                    if (k >= ranks && elect_one())
 #pragma unroll
                         for (int e = 0; e < 4; ++e) mma_f16(d, x + e * 2 + kPixelBytes / 32, w + e * 2, desc, in_run > 0 || e > 0);
                     __syncwarp();
                     if (!(ok = mbar_wait_uniform(full + slot * 16 + 8, phase, stop, c.status, c.limit))) break;
                     tc_fence_after();
                 }
-                // the ranks' steps belong to the last run of channels
-                const bool last = k == c.s.chunks + ranks - 1 || (in_run == kRun<kX3> - 1 && k < c.s.chunks - 1);
+                // the ranks' steps are a run of their own, the first one: their product has another scale
+                const bool last = k == ranks - 1 || k == c.s.chunks + ranks - 1 || (in_run == kRun<kX3> - 1 && k >= ranks);
                 if (elect_one()) {
-                    if (k < c.s.chunks) {
+                    if (k >= ranks) {
 #pragma unroll
                         for (int term = kX3 ? 1 : 2; term < 3; ++term)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
                                 mma_f16(d, x + e * 2, w + e * 2 + (term == 1 ? rows * 8 : 0), desc, kX3 || in_run > 0 || e > 0);
                     } else {
-                        const int steps = (min(s.R - (k - c.s.chunks) * 32, 32) + 15) / 16;
+                        const int steps = (min(s.R - k * 32, 32) + 15) / 16;
 #pragma unroll
                         for (int term = kX3 ? 0 : 2; term < 3; ++term)
-                            for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, 1);
+                            for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, in_run > 0 || e > 0 || term > (kX3 ? 0 : 2));
                     }
                     mma_commit(empty + slot * 8);
                     if (last) mma_commit(done + buffer * 8);
@@ -465,18 +467,43 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         }
     } else {
         const int lane = threadIdx.x & 31, half = warp >> 2;
-        const int w_exponent = exponents(c)[0];
         float4 *rows = reinterpret_cast<float4 *>(stages + kStages * kStageBytes) + warp * 256;
         int buffer = 0, phase = 0;
         for (int i = blockIdx.x; i < work; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
-            // undoes both operands' scaling: the pixel's and the filters' parts may each pass FP32's range where the result does not
-            const TwoFactors back(exponents(c)[4 + (size_t)np * kTile + (warp & 3) * 32 + lane] + w_exponent - 2 * 141);
             const int blocks = tile_rows(c, kt) / 32;
-            float sum[kFilterTile / 2][32] = {};         // of this warp's blocks of filters
+            // What undoes a filter's scaling, of W and of Up, and its bias, where the results pass through later: [block]{32 of each}
+            const bool some = ranks_of(np) > 0;
+            const float *w_factors = filter_factors(c) + kt * kFilterTile * 32, *u_factors = info_of(a.packed, s, some ? a.adapter[n] : 0) + 4 + kt * kFilterTile * 32;
+#pragma unroll
+            for (int e = 0; e < kFilterTile / 2; ++e) {
+                const int k = (half + e * 2) * 32 + lane;
+                if (half + e * 2 >= blocks) continue;
+                float *to = reinterpret_cast<float *>(rows) + e * 96 + lane;
+                to[0] = w_factors[k];
+                to[32] = some ? u_factors[k] : 0.0f;
+                to[64] = a.bias && kt * kFilterTile * 32 + k < s.K ? a.bias[kt * kFilterTile * 32 + k] : 0.0f;
+            }
+            // and a pixel's: sums are kept smaller by 2^(64 - exponent) where that would let them pass FP32's range in front of the filter's factor
+            const int2 ex = pixel_exponents(c)[(size_t)np * kTile + (warp & 3) * 32 + lane];
+            const int kept_back = min(max((some ? max(ex.x - 141, ex.y) : ex.x - 141) - 64, 0), 127);
+            const float x_back = power(ex.x - 141 - kept_back), t_back = some ? power(ex.y - kept_back) : 0.0f;
+            __syncwarp();
+            uint64_t sum[kFilterTile / 2][16];           // of this warp's blocks of filters, by twos
+#pragma unroll
+            for (int e = 0; e < kFilterTile / 2; ++e)
+#pragma unroll
+                for (int u = 0; u < 32; u += 4) {
+                    const float4 add = rows[e * 24 + 16 + u / 4];
+                    const float down = power(-kept_back);
+                    sum[e][u / 2] = mul2(pair(add.x, add.y), pair(down, down));
+                    sum[e][u / 2 + 1] = mul2(pair(add.z, add.w), pair(down, down));
+                }
             bool given_up = false;
 #pragma unroll 1
-            for (int k = 0; k < c.s.chunks; k += kRun<kX3>) {
+            for (int k = some ? -1 : 0; k < c.s.chunks; k = k < 0 ? 0 : k + kRun<kX3>) {             // -1: the adapter's part
+                const float back = k < 0 ? t_back : x_back;
+                const float4 *factors = rows + (k < 0 ? 8 : 0);
                 if ((given_up = !mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit))) break;
                 tc_fence_after();
 #pragma unroll
@@ -487,7 +514,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                         float v[16];
                         tmem_ld16(tmem + buffer * 256 + (half + e * 2) * 32 + g + ((uint32_t)(warp & 3) << 21), v);
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) sum[e][g + u] += v[u];
+                        for (int u = 0; u < 16; u += 4) {
+                            const float4 f = factors[e * 24 + (g + u) / 4];
+                            uint64_t *y = &sum[e][(g + u) / 2];
+                            y[0] = fma2(mul2(pair(v[u], v[u + 1]), pair(back, back)), pair(f.x, f.y), y[0]);
+                            y[1] = fma2(mul2(pair(v[u + 2], v[u + 3]), pair(back, back)), pair(f.z, f.w), y[1]);
+                        }
                     }
                 }
                 tc_fence_before();
@@ -495,38 +527,47 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                 if (++buffer == 2) { buffer = 0; phase ^= 1; }
             }
             if (given_up) break;
+            __syncwarp();                                // (all have read the factors)
+            const float up = power(kept_back);
+            const int left = a.HW - p0;                  // pixels
 #pragma unroll
             for (int e = 0; e < kFilterTile / 2; ++e) {
                 const int b = half + e * 2;
                 if (b >= blocks) continue;
-                const float (&v)[32] = sum[e];
                 // through shared memory, so that a store is whole lines: eight lanes a pixel
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    rows[lane * 8 + (u ^ (lane & 7))] = make_float4(v[u * 4] * back.a * back.b, v[u * 4 + 1] * back.a * back.b, v[u * 4 + 2] * back.a * back.b,
-                                                                    v[u * 4 + 3] * back.a * back.b);
-                __syncwarp();
-                const int k0 = (kt * kFilterTile + b) * 32 + (lane & 7) * 4;
-                float4 add = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (a.bias) {
-                    if (k0 + 4 <= s.K) add = *reinterpret_cast<const float4 *>(a.bias + k0);
-                    else add = make_float4(k0 < s.K ? a.bias[k0] : 0.0f, k0 + 1 < s.K ? a.bias[k0 + 1] : 0.0f, k0 + 2 < s.K ? a.bias[k0 + 2] : 0.0f, 0.0f);
-                }
-                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8 + lane;
-#pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const int r = u * 4 + (lane >> 3);
-                    float4 y = rows[r * 8 + ((lane & 7) ^ (r & 7))];
-                    y.x += add.x; y.y += add.y; y.z += add.z; y.w += add.w;
-                    if (p0 + r >= a.HW) continue;
-                    if (a.accumulate) {
-                        const float4 before = out[u * 32];
-                        y.x += before.x; y.y += before.y; y.z += before.z; y.w += before.w;
-                    }
-                    if (a.relu) y = make_float4(fmaxf(y.x, 0.0f), fmaxf(y.y, 0.0f), fmaxf(y.z, 0.0f), fmaxf(y.w, 0.0f));
-                    if (k0 + 4 > s.K) y = make_float4(k0 < s.K ? y.x : 0.0f, k0 + 1 < s.K ? y.y : 0.0f, k0 + 2 < s.K ? y.z : 0.0f, 0.0f);       // +0 in pad lanes
-                    __stcs(out + u * 32, y);             // operands are read again, results here not: they leave L2 first (131 -> 128 us)
+                    float4 y;
+                    unpair(mul2(sum[e][u * 2], pair(up, up)), y.x, y.y);
+                    unpair(mul2(sum[e][u * 2 + 1], pair(up, up)), y.z, y.w);
+                    rows[lane * 8 + (u ^ (lane & 7))] = y;
                 }
+                __syncwarp();
+                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8 + lane;
+                float4 y[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) y[u] = rows[(u * 4 + (lane >> 3)) * 8 + ((lane & 7) ^ ((u * 4 + (lane >> 3)) & 7))];
+                if (a.accumulate) {
+                    float4 before[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) before[u] = u * 4 + (lane >> 3) < left ? out[u * 32] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) { y[u].x += before[u].x; y[u].y += before[u].y; y[u].z += before[u].z; y[u].w += before[u].w; }
+                }
+                if (a.relu)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) y[u] = make_float4(fmaxf(y[u].x, 0.0f), fmaxf(y[u].y, 0.0f), fmaxf(y[u].z, 0.0f), fmaxf(y[u].w, 0.0f));
+                if ((kt * kFilterTile + b + 1) * 32 > s.K)           // +0 in pad lanes
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) y[u] = clear_from(y[u], s.K - (kt * kFilterTile + b) * 32 - (lane & 7) * 4);
+                // operands are read again, results here not: they leave L2 first (131 -> 128 us)
+                if (left >= 32)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) __stcs(out + u * 32, y[u]);
+                else
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        if (u * 4 + (lane >> 3) < left) __stcs(out + u * 32, y[u]);
                 __syncwarp();
             }
         }
@@ -540,48 +581,66 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
-// Up and Down as halves, a block an adapter each.
+// Up and Down as halves, a block an adapter each.  Each row of Down (a rank) is brought to the same size; what that takes from some ranks beside the
+// largest one, Up's columns get, in front of each of its rows being brought to one size, too.
 __global__ void __launch_bounds__(kThreads) pack_halves_kernel(const float *__restrict__ down, const float *__restrict__ up, float *__restrict__ packed, const AdapterShape s) {
-    __shared__ float most_s[kThreads / 32], sum_s[kThreads / 32];
+    __shared__ int rank_s[128];
     grid_dep_sync();
     grid_dep_trigger();
-    const int a = blockIdx.x, cols = blockIdx.y ? s.C : s.R;             // of a row: Up is [K][R], Down [R][C]
-    const float *w = blockIdx.y ? down + (size_t)a * s.R * s.C : up + (size_t)a * s.K * s.R;
-    float most = 0.0f, sums = 0.0f;
-    for (size_t i = threadIdx.x; i < (size_t)(blockIdx.y ? s.C : s.K) * s.R; i += kThreads) most = fmaxf(most, magnitude(w[i]));
-    const int ex = top_exponent(block_max(most, most_s));
-    const float by = lift(ex);
-    if (blockIdx.y) {
-        for (int r = threadIdx.x >> 5; r < s.R; r += kThreads / 32) {    // a warp a row
-            float sum = 0.0f;
-            for (int ch = threadIdx.x & 31; ch < s.C; ch += 32) sum += magnitude(w[(size_t)r * s.C + ch]);
+    const int a = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float *d = down + (size_t)a * s.R * s.C, *u = up + (size_t)a * s.K * s.R;
+    for (int r = warp; r < s.R; r += kThreads / 32) {
+        float most = 0.0f;
+        for (int ch = lane; ch < s.C; ch += 32) most = fmaxf(most, magnitude(d[(size_t)r * s.C + ch]));
 #pragma unroll
-            for (int o = 16; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
-            sums = fmaxf(sums, sum);
+        for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+        if (lane == 0) rank_s[r] = top_exponent(most);
+    }
+    __syncthreads();
+    int ed = 0;
+    for (int r = 0; r < s.R; ++r) ed = max(ed, rank_s[r]);
+    float *info = info_of(packed, s, a);
+    if (blockIdx.y) {                                    // Down: rows of 128 bytes hold 64 channels' high (or low) halves
+        if (threadIdx.x == 0) info[0] = __int_as_float(ed);
+        char *out = reinterpret_cast<char *>(packed + s.down_halves_at + a * s.down_halves);
+        for (size_t i = threadIdx.x; i < (size_t)s.RQ * s.chunks * 16; i += kThreads) {
+            const int e = (int)(i % 16) * 4, run = (int)(i / 16 % s.chunks), r = (int)(i / 16 / s.chunks), ch = run * 64 + e;
+            const float by = r < s.R ? lift(rank_s[r]) : 0.0f;
+            float v[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] = r < s.R && ch + x < s.C ? d[(size_t)r * s.C + ch + x] * by : 0.0f;
+            uint2 hi, lo;
+            split_finite(v[0], v[1], hi.x, lo.x);
+            split_finite(v[2], v[3], hi.y, lo.y);
+            char *to = out + (size_t)run * s.RQ * 256;
+            *reinterpret_cast<uint2 *>(to + chunk_at(r, e, s.RQ) + (e & 4) * 2) = hi;
+            *reinterpret_cast<uint2 *>(to + chunk_at(r, 64 + e, s.RQ) + (e & 4) * 2) = lo;
         }
-        sums = block_max(sums, sum_s);
+        return;
     }
-    if (threadIdx.x == 0) {
-        float *info = packed + s.info_at + 4 * (size_t)a;
-        info[blockIdx.y] = __int_as_float(ex);
-        if (blockIdx.y) info[2] = sums;
-    }
-    char *out = reinterpret_cast<char *>(blockIdx.y ? packed + s.down_halves_at + a * s.down_halves : packed + s.up_halves_at + a * s.up_halves);
-    // four columns at a time; a row of 128 bytes holds 64 channels' high (or low) halves, or both of 32 ranks
-    const int wide = blockIdx.y ? 64 : 32, runs = blockIdx.y ? s.chunks : s.RB, all = blockIdx.y ? s.RQ : s.KB * 32;
-    for (size_t i = threadIdx.x; i < (size_t)all * runs * (wide / 4); i += kThreads) {
-        const int e = (int)(i % (wide / 4)) * 4, run = (int)(i / (wide / 4) % runs), r = (int)(i / (wide / 4) / runs);
-        float v[4];
+    // Up: rows of 128 bytes hold both halves of 32 ranks; a warp a row, a lane a rank of each 32
+    char *out = reinterpret_cast<char *>(packed + s.up_halves_at + a * s.up_halves);
+    for (int k = warp; k < s.KB * 32; k += kThreads / 32) {
+        int ex = 15;                                     // of the row's largest value
+        for (int r = lane; k < s.K && r < s.R; r += 32) {
+            const float m = magnitude(u[(size_t)k * s.R + r]);
+            if (m > 0.0f) ex = max(ex, (int)(__float_as_uint(m) >> 23) + rank_s[r] - ed);
+        }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = r < (blockIdx.y ? s.R : s.K) && run * wide + e + u < cols ? w[(size_t)r * cols + run * wide + e + u] * by : 0.0f;
-        uint2 hi, lo;
-        split_finite(v[0], v[1], hi.x, lo.x);
-        split_finite(v[2], v[3], hi.y, lo.y);
-        const int kt = blockIdx.y ? 0 : r / (kFilterTile * 32), row = blockIdx.y ? r : r % (kFilterTile * 32);
-        const int rows = blockIdx.y ? s.RQ : min(kFilterTile, s.KB - kt * kFilterTile) * 32;
-        char *to = blockIdx.y ? out + (size_t)run * rows * 256 : out + ((size_t)kt * s.RB * kFilterTile * 32 + (size_t)run * rows) * 128;
-        *reinterpret_cast<uint2 *>(to + chunk_at(row, e, rows) + (e & 4) * 2) = hi;
-        *reinterpret_cast<uint2 *>(to + chunk_at(row, wide + e, rows) + (e & 4) * 2) = lo;
+        for (int o = 16; o; o /= 2) ex = max(ex, __shfl_xor_sync(~0u, ex, o));
+        if (lane == 0) info[4 + k] = drop(ex);
+        const int kt = k / (kFilterTile * 32), row = k % (kFilterTile * 32), rows = min(kFilterTile, s.KB - kt * kFilterTile) * 32;
+        for (int rb = 0; rb < s.RB; ++rb) {
+            const int r = rb * 32 + lane;
+            const float v = k < s.K && r < s.R ? ldexpf(u[(size_t)k * s.R + r], 141 - ex + rank_s[r] - ed) : 0.0f, w = __shfl_down_sync(~0u, v, 1);
+            uint32_t hi, lo;
+            split_finite(v, w, hi, lo);
+            char *to = out + ((size_t)kt * s.RB * kFilterTile * 32 + (size_t)rb * rows) * 128;
+            if ((lane & 1) == 0) {
+                *reinterpret_cast<uint32_t *>(to + chunk_at(row, lane, rows) + (lane & 7) * 2) = hi;
+                *reinterpret_cast<uint32_t *>(to + chunk_at(row, 32 + lane, rows) + (lane & 7) * 2) = lo;
+            }
+        }
     }
 }
 
@@ -611,7 +670,7 @@ int launch_pack_halves(small_ctx *ctx, const float *down, const float *up, float
 
 int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s, bool x3, cudaStream_t st) {
     const TcArgs c{a, s, Layout(a.N, s.C, s.K, a.HW, s.R), ctx->dev_status, ctx->wait_iters};
-    launch_clusters(ctx, adapter_filters_kernel, dim3(kCluster), dim3(kThreads * kTeams), kCluster, 0, st, c);
+    launch_kernel(ctx, adapter_filters_kernel, dim3((unsigned)s.KB), dim3(kThreads * kTeams), 0, st, c);
     if (int e = check_launch(ctx)) return e;
     static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
     const size_t passing = 1024 + (size_t)kPixelBytes + (size_t)s.RQ * (256 + (s.chunks > kDownRun ? kTile * sizeof(float) : 0)), stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;

@@ -21,15 +21,11 @@ __device__ __forceinline__ int top_exponent(float most) { return min(max((int)(_
 __device__ __forceinline__ float lift(int e) { return __uint_as_float((uint32_t)(268 - e) << 23); }
 __device__ __forceinline__ float drop(int e) { return __uint_as_float((uint32_t)(e - 14) << 23); }
 
-// 2^e for e from -252 to 254 as two factors: x * a * b leaves FP32's range only where x * 2^e does.
-struct TwoFactors {
-    float a, b;
-    __device__ explicit TwoFactors(int e) {
-        const int first = min(max(e, -126), 127);
-        a = __uint_as_float((uint32_t)(first + 127) << 23);
-        b = __uint_as_float((uint32_t)(e - first + 127) << 23);
-    }
-};
+// 2^e: 0 where it is less than any float, and no more than 2^127.
+__device__ __forceinline__ float power(int e) {
+    e = min(e, 127);
+    return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : e >= -149 ? 1u << (e + 149) : 0u);
+}
 
 // |x|; what is not finite does not count: it stays what it is at any scale, and must not take its tile's other values with it.
 __device__ __forceinline__ float magnitude(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.0f; }
@@ -82,6 +78,29 @@ __device__ __forceinline__ void mma_f16_tmem(uint32_t d, uint32_t a, uint32_t b_
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
         ::"r"(d), "r"(a), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate) : "memory");
 }
+// Two floats as one operand of the packed FP32 instructions.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"

@@ -85,3 +85,45 @@ def test_long_reductions(C, K, R, mode):
     layer.w, layer.b[:] = np.zeros_like(layer.w), 0                 # the adapters' products by themselves
     some = ids >= 0
     assert rel_err(layer.run(x, ids, mode)[some], layer.ref(x, ids)[some]) <= TOL[mode]
+
+
+SIZES = np.array([0, -24, -28, -32, -40, -60, 20, -90], np.float64)
+
+
+@pytest.mark.parametrize("mode", A.MODES)
+@pytest.mark.parametrize("R", [12, 40])
+def test_filters_and_rows_of_up_of_very_different_size(R, mode):
+    """Every output channel has a size of its own, and in half of them the adapter's row another one than the filter: each keeps its own accuracy."""
+    rng = np.random.default_rng(73 + R)
+    layer, x = A.Layer(rng, 96, 160, R, 3, bias=False), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    on_tensor_cores(layer, 80, 9, 10)
+    k = np.arange(160)
+    layer.w = (layer.w * 2.0 ** SIZES[k % 8][:, None]).astype(np.float32)
+    layer.up = (layer.up * 2.0 ** SIZES[np.where(k % 3 < 2, k, k // 8) % 8][:, None]).astype(np.float32)
+    for ids in (np.full(80, -1, np.int32), (np.arange(80) % 3).astype(np.int32)):
+        assert by_channel(layer.run(x, ids, mode), layer.ref(x, ids)) <= TOL[mode]
+
+
+@pytest.mark.parametrize("mode", A.MODES)
+def test_ranks_of_very_different_size(mode):
+    """Rows of Down far below and above one another, and columns of Up that make up for it: every rank has the same part in the result."""
+    rng = np.random.default_rng(74)
+    layer, x = A.Layer(rng, 96, 160, 16, 3, bias=False), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    on_tensor_cores(layer, 80, 9, 10)
+    size = 2.0 ** SIZES[np.arange(16) % 8]
+    layer.down, layer.up = (layer.down * size[:, None]).astype(np.float32), (layer.up / size).astype(np.float32)
+    layer.w *= 0.1
+    ids = (np.arange(80) % 3).astype(np.int32)
+    assert rel_err(layer.run(x, ids, mode), layer.ref(x, ids)) <= TOL[mode]
+
+
+@pytest.mark.parametrize("mode", ["fp32", "3xtf32"])
+def test_scales_of_adapters_far_from_one(mode):
+    rng = np.random.default_rng(75)
+    layer, x = A.Layer(rng, 96, 160, 16, 5, bias=False), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    on_tensor_cores(layer, 80, 9, 10)
+    layer.scale = np.array([0.0, -1e-30, 1e30, -3.0, 1e-38], np.float32)
+    layer.up[1] *= 1e30
+    layer.up[2] *= 1e-30
+    ids = (np.arange(80) % 6 - 1).astype(np.int32)
+    assert rel_err(layer.run(x, ids, mode), layer.ref(x, ids)) <= TOL[mode]
