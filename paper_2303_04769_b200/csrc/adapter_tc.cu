@@ -10,9 +10,10 @@
 //   next.  t times Up is a run of its own, because rows of Up are brought to one size whatever the filters' is.
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
 //
-// Batch 64, 256 -> 768, 28 x 28, rank 16: 164 us.  Pixels 37 (the filters, 5, beside them): the largest values, while memory still takes the result
-// before, then four chunks that wait for their loads.  Product 105: the epilogue, two thirds of it in its stores and waits for scales.  Floor 33 for
-// the bytes, 37 for three products.
+// Batch 64, 256 -> 768, 28 x 28, rank 16: 134 us.  Pixels 36 (the filters, 5, beside them): the largest values, while memory still takes the result
+// before, then four chunks that wait for their loads.  Product 83: MMAs some 45 % of the time; what a stage takes to load, and the epilogue's sums, scales
+// and stores, fill the rest.  With an accumulator for all of a tile's steps 72, see kRun; of 168 registers a thread for all roles 94, as the epilogue's sums spill.
+// Floor 33 for the bytes, 37 for three products.
 #include "adapter.cuh"
 #include "halves.cuh"
 
@@ -129,6 +130,13 @@ __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const
 
 __device__ __forceinline__ void bulk_store(void *to, uint32_t from, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+}
+// The same, for what is not read again soon: it leaves L2 first.
+__device__ __forceinline__ void bulk_store_first(void *to, uint32_t from, uint32_t bytes) {
+    asm volatile(
+        "{\n\t.reg .b64 policy;\n\tcreatepolicy.fractional.L2::evict_first.b64 policy, 1.0;\n\t"
+        "cp.async.bulk.global.shared::cta.bulk_group.L2::cache_hint [%0], [%1], %2, policy;\n\t}\n\tcp.async.bulk.commit_group;"
+        ::"l"(to), "r"(from), "r"(bytes) : "memory");
 }
 template <int kLeft>
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
@@ -333,10 +341,18 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
 
 // The tensor core cuts its accumulator off at 24 bits at each step, on the average by 0.36 * 2^-23 of what stands there: what a result loses that way
 // grows with the steps of a sum and is lost on one side.  So an accumulator takes a run of chunks, and the epilogue adds the runs' products in FP32
-// registers, where sums are rounded; sums that lose nothing stay exact.
+// registers, where sums are rounded; sums that lose nothing stay exact.  (Four chunks in 3xTF32: 131 us for 134, errors of 256 channels 1.1e-6 for 5e-7.)
 template <bool kX3> constexpr int kRun = kX3 ? 2 : 8;        // chunks
 
-constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, kProductThreads = 320;
+constexpr int kPassing = 4096;           // bytes of shared memory that a warp's results pass through: 32 pixels x 32 filters, which lie together in memory, too
+constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, kEpilogueWarps = 8, kProductThreads = kEpilogueWarps * 32 + 128;
+constexpr int kRolesRegs = 40, kEpilogueRegs = 232;     // a thread, of the 168 that each is launched with
+static_assert(kRolesRegs * 128 + kEpilogueRegs * kEpilogueWarps * 32 <= 168 * kProductThreads, "more than the launch brings is waited for without an end");
+
+// mbar_wait_uniform without a call: a kernel that deals out its registers by role must not have any.
+__device__ __forceinline__ bool wait_here(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status, uint32_t limit) {
+    return __all_sync(0xffffffffu, mbar_wait<64>(bar, parity, abort_flag, status, limit));
+}
 
 template <bool kX3>
 __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(const TcArgs c) {
@@ -350,11 +366,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
     const int warp = warp_index();
     char *stages = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t full = smem_u32(full_s), empty = smem_u32(empty_s), done = smem_u32(done_s), free = smem_u32(free_s);
-    if (warp == 9) tmem_alloc(smem_u32(&tmem_s), 512);
+    constexpr int kLoader = kEpilogueWarps, kIssuer = kLoader + 1;
+    if (warp == kIssuer) tmem_alloc(smem_u32(&tmem_s), 512);
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int i = 0; i < kStages; ++i) { mbar_init(full + i * 16, 1); mbar_init(full + i * 16 + 8, 1); mbar_init(empty + i * 8, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(done + i * 8, 1); mbar_init(free + i * 8, 256); }
+        for (int i = 0; i < 2; ++i) { mbar_init(done + i * 8, 1); mbar_init(free + i * 8, kEpilogueWarps * 32); }
         mbar_init(smem_u32(&drained), 1);
         mbar_fence_init();
     }
@@ -370,215 +387,267 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         const int id = a.adapter[np / c.at.tiles];
         return id >= 0 && id < a.adapters ? s.RB : 0;
     };
-    int issued = 0;                                      // stages, by warp 8
-    if (warp == 8) {
-        int slot = 0, phase = 1;
-        bool ok = true;
-        for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
-            const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, rows = tile_rows(c, kt), ranks = ranks_of(np);
-            const int id = ranks ? a.adapter[np / c.at.tiles] : 0;
-            const char *x = ws_of(c) + (size_t)np * c.s.chunks * kPixelBytes, *t = ws_of(c) + c.at.ranks_at + (size_t)np * s.RB * kRankBytes;
-            const char *w = ws_of(c) + c.at.filters_at + (size_t)kt * c.s.chunks * kFilterTile * 32 * 256;
-            const char *u = reinterpret_cast<const char *>(a.packed + s.up_halves_at + id * s.up_halves) + (size_t)kt * s.RB * kFilterTile * 32 * 128;
-            for (int k = 0; k < c.s.chunks + ranks; ++k) {
-                if (issued >= kStages && !(ok = mbar_wait_uniform(empty + slot * 8, phase, stop, c.status, c.limit))) break;
-                const int rb = k < ranks ? k : -1, ch = k - ranks;
-                if (elect_one()) {
-                    const uint32_t to = smem_u32(stages + slot * kStageBytes), bar = full + slot * 16;
-                    auto load = [&](uint32_t at, const char *from, uint32_t bytes, uint32_t b) {
-                        for (uint32_t e = 0; e < bytes; e += 8192) bulk_load(to + at + e, from + e, min(8192u, bytes - e), b);
-                    };
-                    if (rb >= 0) {                       // 32 ranks have both parts in a row
-                        mbar_expect_tx(bar, kRankBytes + rows * 128);
-                        load(0, t + (size_t)rb * kRankBytes, kRankBytes, bar);
-                        load(kPixelBytes, u + (size_t)rb * rows * 128, rows * 128, bar);
-                        if (kX3) mbar_arrive(bar + 8);
-                    } else {                             // high parts lie in front; the terms begin with low pixels and high filters
-                        const char *fx = x + (size_t)ch * kPixelBytes, *fw = w + (size_t)ch * rows * 256;
-                        const uint32_t half = kPixelBytes / 2;
-                        mbar_expect_tx(bar, half + rows * 128);
-                        load(kX3 ? half : 0, kX3 ? fx + half : fx, half, bar);
-                        load(kPixelBytes, fw, rows * 128, bar);
-                        if (kX3) {
-                            mbar_expect_tx(bar + 8, half + rows * 128);
-                            load(0, fx, half, bar + 8);
-                            load(kPixelBytes + rows * 128, fw + rows * 128, rows * 128, bar + 8);
+    int issued = 0;                                      // stages, by the loading warp
+    if (warp >= kLoader) {                               // two roles, two idle warps
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRolesRegs));
+        if (warp == kLoader) {
+            int slot = 0, phase = 1;
+            bool ok = true;
+            for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
+                const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, rows = tile_rows(c, kt), ranks = ranks_of(np);
+                const int id = ranks ? a.adapter[np / c.at.tiles] : 0;
+                const char *x = ws_of(c) + (size_t)np * c.s.chunks * kPixelBytes, *t = ws_of(c) + c.at.ranks_at + (size_t)np * s.RB * kRankBytes;
+                const char *w = ws_of(c) + c.at.filters_at + (size_t)kt * c.s.chunks * kFilterTile * 32 * 256;
+                const char *u = reinterpret_cast<const char *>(a.packed + s.up_halves_at + id * s.up_halves) + (size_t)kt * s.RB * kFilterTile * 32 * 128;
+                for (int k = 0; k < c.s.chunks + ranks; ++k) {
+                    if (issued >= kStages && !(ok = wait_here(empty + slot * 8, phase, stop, c.status, c.limit))) break;
+                    const int rb = k - c.s.chunks;
+                    if (elect_one()) {
+                        const uint32_t to = smem_u32(stages + slot * kStageBytes), bar = full + slot * 16;
+                        auto load = [&](uint32_t at, const char *from, uint32_t bytes, uint32_t b) {
+                            for (uint32_t e = 0; e < bytes; e += 8192) bulk_load(to + at + e, from + e, min(8192u, bytes - e), b);
+                        };
+                        if (rb >= 0) {                       // 32 ranks have both parts in a row
+                            mbar_expect_tx(bar, kRankBytes + rows * 128);
+                            load(0, t + (size_t)rb * kRankBytes, kRankBytes, bar);
+                            load(kPixelBytes, u + (size_t)rb * rows * 128, rows * 128, bar);
+                            if (kX3) mbar_arrive(bar + 8);
+                        } else {                             // high parts lie in front; the terms begin with low pixels and high filters
+                            const char *fx = x + (size_t)k * kPixelBytes, *fw = w + (size_t)k * rows * 256;
+                            const uint32_t half = kPixelBytes / 2;
+                            mbar_expect_tx(bar, half + rows * 128);
+                            load(kX3 ? half : 0, kX3 ? fx + half : fx, half, bar);
+                            load(kPixelBytes, fw, rows * 128, bar);
+                            if (kX3) {
+                                mbar_expect_tx(bar + 8, half + rows * 128);
+                                load(0, fx, half, bar + 8);
+                                load(kPixelBytes + rows * 128, fw + rows * 128, rows * 128, bar + 8);
+                            }
                         }
                     }
-                }
-                __syncwarp();
-                ++issued;
-                if (++slot == kStages) { slot = 0; phase ^= 1; }
-            }
-        }
-    } else if (warp == 9) {
-        const uint32_t first = smem_desc_lo(smem_u32(stages));
-        int slot = 0, phase = 0, buffer = 0, buffer_phase = 1, turn = 0;
-        bool ok = true;
-        for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
-            const int np = i / c.at.filter_tiles, rows = tile_rows(c, i % c.at.filter_tiles), ranks = ranks_of(np);
-            const uint32_t desc = f16_desc(rows);
-            for (int k = 0, in_run = 0; k < c.s.chunks + ranks; ++k) {
-                if (in_run == 0 && turn >= 2 && !(ok = mbar_wait_uniform(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
-                const uint32_t d = tmem + buffer * 256;
-                const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
-                if (!(ok = mbar_wait_uniform(full + slot * 16, phase, stop, c.status, c.limit))) break;
-                tc_fence_after();
-                if (kX3) {                               // small terms first: low pixels and high filters while the rest is on its way
-                    if (k >= ranks && elect_one())
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mma_f16(d, x + e * 2 + kPixelBytes / 32, w + e * 2, desc, in_run > 0 || e > 0);
                     __syncwarp();
-                    if (!(ok = mbar_wait_uniform(full + slot * 16 + 8, phase, stop, c.status, c.limit))) break;
-                    tc_fence_after();
-                }
-                // the ranks' steps are a run of their own, the first one: their product has another scale
-                const bool last = k == ranks - 1 || k == c.s.chunks + ranks - 1 || (in_run == kRun<kX3> - 1 && k >= ranks);
-                if (elect_one()) {
-                    if (k >= ranks) {
-#pragma unroll
-                        for (int term = kX3 ? 1 : 2; term < 3; ++term)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                mma_f16(d, x + e * 2, w + e * 2 + (term == 1 ? rows * 8 : 0), desc, kX3 || in_run > 0 || e > 0);
-                    } else {
-                        const int steps = (min(s.R - k * 32, 32) + 15) / 16;
-#pragma unroll
-                        for (int term = kX3 ? 0 : 2; term < 3; ++term)
-                            for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, in_run > 0 || e > 0 || term > (kX3 ? 0 : 2));
-                    }
-                    mma_commit(empty + slot * 8);
-                    if (last) mma_commit(done + buffer * 8);
-                }
-                __syncwarp();
-                if (++slot == kStages) { slot = 0; phase ^= 1; }
-                ++in_run;
-                if (last) {
-                    in_run = 0;
-                    ++turn;
-                    if (++buffer == 2) { buffer = 0; buffer_phase ^= 1; }
+                    ++issued;
+                    if (++slot == kStages) { slot = 0; phase ^= 1; }
                 }
             }
-        }
-        if (!ok) {
-            if (elect_one()) mma_commit(smem_u32(&drained));
-            __syncwarp();
-            mbar_wait(smem_u32(&drained), 0, kDefaultWaitIters);
+        } else if (warp == kIssuer) {
+            const uint32_t first = smem_desc_lo(smem_u32(stages));
+            int slot = 0, phase = 0, buffer = 0, buffer_phase = 1, turn = 0;
+            bool ok = true;
+            for (int i = blockIdx.x; i < work && ok; i += gridDim.x) {
+                const int np = i / c.at.filter_tiles, rows = tile_rows(c, i % c.at.filter_tiles), ranks = ranks_of(np);
+                const uint32_t desc = f16_desc(rows);
+                for (int k = 0, in_run = 0; k < c.s.chunks + ranks; ++k) {
+                    if (in_run == 0 && turn >= 2 && !(ok = wait_here(free + buffer * 8, buffer_phase, stop, c.status, c.limit))) break;
+                    const uint32_t d = tmem + buffer * 256;
+                    const uint32_t x = first + slot * (kStageBytes >> 4), w = x + (kPixelBytes >> 4);
+                    if (!(ok = wait_here(full + slot * 16, phase, stop, c.status, c.limit))) break;
+                    tc_fence_after();
+                    if (kX3) {                               // small terms first: low pixels and high filters while the rest is on its way
+                        if (k < c.s.chunks && elect_one())
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) mma_f16(d, x + e * 2 + kPixelBytes / 32, w + e * 2, desc, in_run > 0 || e > 0);
+                        __syncwarp();
+                        if (!(ok = wait_here(full + slot * 16 + 8, phase, stop, c.status, c.limit))) break;
+                        tc_fence_after();
+                    }
+                    // the ranks' steps are a run of their own: their product has another scale
+                    const bool last = k == c.s.chunks - 1 || k == c.s.chunks + ranks - 1 || (in_run == kRun<kX3> - 1 && k < c.s.chunks);
+                    if (elect_one()) {
+                        if (k < c.s.chunks) {
+#pragma unroll
+                            for (int term = kX3 ? 1 : 2; term < 3; ++term)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    mma_f16(d, x + e * 2, w + e * 2 + (term == 1 ? rows * 8 : 0), desc, kX3 || in_run > 0 || e > 0);
+                        } else {
+                            const int steps = (min(s.R - (k - c.s.chunks) * 32, 32) + 15) / 16;
+#pragma unroll
+                            for (int term = kX3 ? 0 : 2; term < 3; ++term)
+                                for (int e = 0; e < steps; ++e) mma_f16(d, x + e * 2 + (term == 0 ? 4 : 0), w + e * 2 + (term == 1 ? 4 : 0), desc, in_run > 0 || e > 0 || term > (kX3 ? 0 : 2));
+                        }
+                        mma_commit(empty + slot * 8);
+                        if (last) mma_commit(done + buffer * 8);
+                    }
+                    __syncwarp();
+                    if (++slot == kStages) { slot = 0; phase ^= 1; }
+                    ++in_run;
+                    if (last) {
+                        in_run = 0;
+                        ++turn;
+                        if (++buffer == 2) { buffer = 0; buffer_phase ^= 1; }
+                    }
+                }
+            }
+            if (!ok) {
+                if (elect_one()) mma_commit(smem_u32(&drained));
+                __syncwarp();
+                mbar_wait(smem_u32(&drained), 0, kDefaultWaitIters);
+            }
         }
     } else {
-        const int lane = threadIdx.x & 31, half = warp >> 2;
-        float4 *rows = reinterpret_cast<float4 *>(stages + kStages * kStageBytes) + warp * 256;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
+        // a warp takes 32 pixels of every other block of filters, a thread a pixel
+        constexpr int kShares = kEpilogueWarps / 4, kBlocks = kFilterTile / kShares;
+        const int lane = threadIdx.x & 31, part = warp >> 2;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        float4 *rows = reinterpret_cast<float4 *>(stages + kStages * kStageBytes) + warp * kPassing / 16;
+        // What undoes a filter's scaling, of W and of Up, and its bias; what undoes a pixel's.  Asked for while the tile before is stored.
+        float w_factor[kBlocks], u_factor[kBlocks], bias[kBlocks];
+        int2 ex;
+        int id;
+        bool some;
+        auto fetch_id = [&](int i) { id = a.adapter[i / c.at.filter_tiles / c.at.tiles]; };
+        auto fetch = [&](int i) {
+            const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles;
+            some = id >= 0 && id < a.adapters;
+            ex = pixel_exponents(c)[(size_t)np * kTile + (warp & 3) * 32 + lane];
+#pragma unroll
+            for (int e = 0; e < kBlocks; ++e) {
+                const int k = (kt * kFilterTile + part + e * kShares) * 32 + lane;
+                w_factor[e] = k < s.KB * 32 ? filter_factors(c)[k] : 0.0f;
+                bias[e] = a.bias && k < s.K ? a.bias[k] : 0.0f;
+                u_factor[e] = some && k < s.KB * 32 ? info_of(a.packed, s, id)[4 + k] : 0.0f;
+            }
+        };
         int buffer = 0, phase = 0;
+        fetch_id(blockIdx.x);                            // (no block without work is launched)
+        fetch(blockIdx.x);
         for (int i = blockIdx.x; i < work; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
             const int blocks = tile_rows(c, kt) / 32;
-            // What undoes a filter's scaling, of W and of Up, and its bias, where the results pass through later: [block]{32 of each}
-            const bool some = ranks_of(np) > 0;
-            const float *w_factors = filter_factors(c) + kt * kFilterTile * 32, *u_factors = info_of(a.packed, s, some ? a.adapter[n] : 0) + 4 + kt * kFilterTile * 32;
-#pragma unroll
-            for (int e = 0; e < kFilterTile / 2; ++e) {
-                const int k = (half + e * 2) * 32 + lane;
-                if (half + e * 2 >= blocks) continue;
-                float *to = reinterpret_cast<float *>(rows) + e * 96 + lane;
-                to[0] = w_factors[k];
-                to[32] = some ? u_factors[k] : 0.0f;
-                to[64] = a.bias && kt * kFilterTile * 32 + k < s.K ? a.bias[kt * kFilterTile * 32 + k] : 0.0f;
-            }
-            // and a pixel's: sums are kept smaller by 2^(64 - exponent) where that would let them pass FP32's range in front of the filter's factor
-            const int2 ex = pixel_exponents(c)[(size_t)np * kTile + (warp & 3) * 32 + lane];
-            const int kept_back = min(max((some ? max(ex.x - 141, ex.y) : ex.x - 141) - 64, 0), 127);
-            const float x_back = power(ex.x - 141 - kept_back), t_back = some ? power(ex.y - kept_back) : 0.0f;
+            // a filter's three go to all lanes, where the results pass through later: [block]{32 of each}
+            if (elect_one()) bulk_store_wait<0>();
             __syncwarp();
-            uint64_t sum[kFilterTile / 2][16];           // of this warp's blocks of filters, by twos
 #pragma unroll
-            for (int e = 0; e < kFilterTile / 2; ++e)
-#pragma unroll
-                for (int u = 0; u < 32; u += 4) {
-                    const float4 add = rows[e * 24 + 16 + u / 4];
-                    const float down = power(-kept_back);
-                    sum[e][u / 2] = mul2(pair(add.x, add.y), pair(down, down));
-                    sum[e][u / 2 + 1] = mul2(pair(add.z, add.w), pair(down, down));
-                }
-            bool given_up = false;
-#pragma unroll 1
-            for (int k = some ? -1 : 0; k < c.s.chunks; k = k < 0 ? 0 : k + kRun<kX3>) {             // -1: the adapter's part
-                const float back = k < 0 ? t_back : x_back;
-                const float4 *factors = rows + (k < 0 ? 8 : 0);
-                if ((given_up = !mbar_wait_uniform(done + buffer * 8, phase, stop, c.status, c.limit))) break;
+            for (int e = 0; e < kBlocks; ++e) {
+                float *to = reinterpret_cast<float *>(rows) + e * 96 + lane;
+                to[0] = w_factor[e];
+                to[32] = u_factor[e];
+                to[64] = bias[e];
+            }
+            // sums are kept smaller by 2^(64 - exponent) where a pixel's scale would let them pass FP32's range in front of the filter's
+            const int kept_back = min(max((some ? max(ex.x - 141, ex.y) : ex.x - 141) - 64, 0), 127);
+            float *pixel = reinterpret_cast<float *>(rows) + kBlocks * 96 + lane;         // a pixel's wait there, too: registers are short
+            pixel[0] = power(ex.x - 141 - kept_back);
+            pixel[32] = some ? power(ex.y - kept_back) : 0.0f;
+            pixel[64] = power(-kept_back);
+            pixel[96] = power(kept_back);
+            __syncwarp();
+            uint64_t sum[kBlocks][16] = {};              // of this warp's blocks of filters, by twos
+            // the next accumulator's columns, a block at a time
+            auto take = [&](auto before, auto use) -> bool {
+                if (!wait_here(done + buffer * 8, phase, stop, c.status, c.limit)) return false;
                 tc_fence_after();
 #pragma unroll
-                for (int e = 0; e < kFilterTile / 2; ++e) {
-                    if (half + e * 2 >= blocks) continue;
-#pragma unroll
-                    for (int g = 0; g < 32; g += 16) {
-                        float v[16];
-                        tmem_ld16(tmem + buffer * 256 + (half + e * 2) * 32 + g + ((uint32_t)(warp & 3) << 21), v);
-#pragma unroll
-                        for (int u = 0; u < 16; u += 4) {
-                            const float4 f = factors[e * 24 + (g + u) / 4];
-                            uint64_t *y = &sum[e][(g + u) / 2];
-                            y[0] = fma2(mul2(pair(v[u], v[u + 1]), pair(back, back)), pair(f.x, f.y), y[0]);
-                            y[1] = fma2(mul2(pair(v[u + 2], v[u + 3]), pair(back, back)), pair(f.z, f.w), y[1]);
-                        }
-                    }
+                for (int e = 0; e < kBlocks; ++e) {
+                    if (part + e * kShares >= blocks) continue;
+                    before(e);
+                    float v[32];
+                    tmem_ld32(tmem + buffer * 256 + (part + e * kShares) * 32 + lanes, v);
+                    use(e, v);
                 }
                 tc_fence_before();
                 mbar_arrive(free + buffer * 8);
                 if (++buffer == 2) { buffer = 0; phase ^= 1; }
-            }
-            if (given_up) break;
-            __syncwarp();                                // (all have read the factors)
-            const float up = power(kept_back);
-            const int left = a.HW - p0;                  // pixels
+                return true;
+            };
+            bool ok = true;
+#pragma unroll 1
+            for (int k = 0; k < c.s.chunks && ok; k += kRun<kX3>)
+                ok = take([](int) {}, [&](int e, const float (&v)[32]) {
 #pragma unroll
-            for (int e = 0; e < kFilterTile / 2; ++e) {
-                const int b = half + e * 2;
-                if (b >= blocks) continue;
-                // through shared memory, so that a store is whole lines: eight lanes a pixel
+                    for (int u = 0; u < 32; u += 2) sum[e][u / 2] = add2(sum[e][u / 2], pair(v[u], v[u + 1]));
+                });
+            if (!ok) break;
+            // scales and bias, while the adapter's part is on its way
+            const float x_back = pixel[0], down = pixel[64];
+            float4 f[8], add[8];
+#pragma unroll
+            for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) { f[u] = rows[e * 24 + u]; add[u] = rows[e * 24 + 16 + u]; }
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    float4 y;
-                    unpair(mul2(sum[e][u * 2], pair(up, up)), y.x, y.y);
-                    unpair(mul2(sum[e][u * 2 + 1], pair(up, up)), y.z, y.w);
-                    rows[lane * 8 + (u ^ (lane & 7))] = y;
+                    uint64_t *y = &sum[e][u * 2];
+                    y[0] = fma2(mul2(y[0], pair(x_back, x_back)), pair(f[u].x, f[u].y), mul2(pair(add[u].x, add[u].y), pair(down, down)));
+                    y[1] = fma2(mul2(y[1], pair(x_back, x_back)), pair(f[u].z, f[u].w), mul2(pair(add[u].z, add[u].w), pair(down, down)));
                 }
-                __syncwarp();
-                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8 + lane;
+            }
+            const float t_back = pixel[32];
+            if (some && !take([&](int e) {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) f[u] = rows[e * 24 + 8 + u];
+                }, [&](int e, const float (&v)[32]) {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        uint64_t *y = &sum[e][u * 2];
+                        y[0] = fma2(mul2(pair(v[u * 4], v[u * 4 + 1]), pair(t_back, t_back)), pair(f[u].x, f[u].y), y[0]);
+                        y[1] = fma2(mul2(pair(v[u * 4 + 2], v[u * 4 + 3]), pair(t_back, t_back)), pair(f[u].z, f[u].w), y[1]);
+                    }
+                })) break;
+            const float up = pixel[96];
+            const int left = a.HW - p0;                  // pixels
+#pragma unroll
+            for (int e = 0; e < kBlocks; ++e) {
+                if (e == 0) fetch_id(min(i + (int)gridDim.x, work - 1));          // (asked for at the end, too: values kept instead would take registers all along)
+                if (e == kBlocks - 1) fetch(min(i + (int)gridDim.x, work - 1));
+                const int b = part + e * kShares;
+                if (b >= blocks) continue;
                 float4 y[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) y[u] = rows[(u * 4 + (lane >> 3)) * 8 + ((lane & 7) ^ ((u * 4 + (lane >> 3)) & 7))];
-                if (a.accumulate) {
-                    float4 before[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) before[u] = u * 4 + (lane >> 3) < left ? out[u * 32] : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) { y[u].x += before[u].x; y[u].y += before[u].y; y[u].z += before[u].z; y[u].w += before[u].w; }
+                for (int u = 0; u < 8; ++u) {
+                    unpair(mul2(sum[e][u * 2], pair(up, up)), y[u].x, y[u].y);
+                    unpair(mul2(sum[e][u * 2 + 1], pair(up, up)), y[u].z, y[u].w);
                 }
+                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8;
+                if (a.accumulate && lane < left)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float4 before = out[lane * 8 + u];
+                        y[u].x += before.x; y[u].y += before.y; y[u].z += before.z; y[u].w += before.w;
+                    }
                 if (a.relu)
 #pragma unroll
                     for (int u = 0; u < 8; ++u) y[u] = make_float4(fmaxf(y[u].x, 0.0f), fmaxf(y[u].y, 0.0f), fmaxf(y[u].z, 0.0f), fmaxf(y[u].w, 0.0f));
-                if ((kt * kFilterTile + b + 1) * 32 > s.K)           // +0 in pad lanes
+                const int filters = s.K - (kt * kFilterTile + b) * 32;
+                if (filters < 32)                        // +0 in pad lanes
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) y[u] = clear_from(y[u], s.K - (kt * kFilterTile + b) * 32 - (lane & 7) * 4);
-                // operands are read again, results here not: they leave L2 first (131 -> 128 us)
-                if (left >= 32)
+                    for (int u = 0; u < 8; ++u) y[u] = clear_from(y[u], filters - u * 4);
+                // A pixel's 128 bytes begin with another 16 in four lanes each, so that no more than two of eight lanes write to one bank (all eight apart: the
+                // same time for half as many selections again).
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) __stcs(out + u * 32, y[u]);
-                else
+                for (int bit = 1; bit < 4; bit *= 2) {
+                    const bool turn = lane & bit;
+                    float4 z[8];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u)
-                        if (u * 4 + (lane >> 3) < left) __stcs(out + u * 32, y[u]);
+                    for (int u = 0; u < 8; ++u) {
+                        const float4 &next = y[(u + bit) & 7];
+                        z[u] = make_float4(turn ? next.x : y[u].x, turn ? next.y : y[u].y, turn ? next.z : y[u].z, turn ? next.w : y[u].w);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) y[u] = z[u];
+                }
+                if (elect_one()) bulk_store_wait<0>();   // the block before has been read
+                __syncwarp();
+#pragma unroll
+                for (int u = 0; u < 8; ++u) rows[lane * 8 + ((u + (lane & 3)) & 7)] = y[u];
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (left > 0 && elect_one()) bulk_store_first(out, smem_u32(rows), min(left, 32) * 128);
                 __syncwarp();
             }
         }
+        if (elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        __syncwarp();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (gave_up && warp == 8)                            // what is still on its way must land before the block ends
+    if (gave_up && warp == kLoader)                            // what is still on its way must land before the block ends
         for (int x = max(0, issued - kStages); x < issued; ++x)
             for (int y = 0; y < (kX3 ? 2 : 1); ++y) mbar_wait(full + x % kStages * 16 + y * 8, (x / kStages) & 1, kDefaultWaitIters);
-    if (warp == 9) tmem_dealloc(tmem, 512);
+    if (warp == kIssuer) tmem_dealloc(tmem, 512);
 }
 
 // Up and Down as halves, a block an adapter each.  Each row of Down (a rank) is brought to the same size; what that takes from some ranks beside the
@@ -673,7 +742,19 @@ int launch_adapted_tc(small_ctx *ctx, const AdaptArgs &a, const AdapterShape &s,
     launch_kernel(ctx, adapter_filters_kernel, dim3((unsigned)s.KB), dim3(kThreads * kTeams), 0, st, c);
     if (int e = check_launch(ctx)) return e;
     static std::atomic<unsigned long long> pixels{0}, exact{0}, fast{0};
-    const size_t passing = 1024 + (size_t)kPixelBytes + (size_t)s.RQ * (256 + (s.chunks > kDownRun ? kTile * sizeof(float) : 0)), stages = 1024 + (size_t)kStages * kStageBytes + 8 * 4096;
+    // a role's share of the registers is waited for without an end if the launch brings fewer than all shares together
+    static std::atomic<unsigned long long> counted{0};
+    const unsigned long long bit = 1ull << (ctx->device & 63);
+    if (!(counted.load(std::memory_order_relaxed) & bit)) {
+        for (const void *kern : {reinterpret_cast<const void *>(adapter_product_kernel<true>), reinterpret_cast<const void *>(adapter_product_kernel<false>)}) {
+            cudaFuncAttributes f;
+            const cudaError_t e = cudaFuncGetAttributes(&f, kern);
+            if (e != cudaSuccess) { ctx->last_cuda = (int)e; return SMALL_ERR_CUDA; }
+            if (f.numRegs * kProductThreads < kRolesRegs * 128 + kEpilogueRegs * kEpilogueWarps * 32) return SMALL_ERR_UNSUPPORTED;
+        }
+        counted.fetch_or(bit, std::memory_order_relaxed);
+    }
+    const size_t passing = 1024 + (size_t)kPixelBytes + (size_t)s.RQ * (256 + (s.chunks > kDownRun ? kTile * sizeof(float) : 0)), stages = 1024 + (size_t)kStages * kStageBytes + kEpilogueWarps * kPassing;
     if (int e = allow_shared_memory(ctx, adapter_pixels_kernel, pixels, 1024 + kPixelBytes + 128 * (256 + kTile * sizeof(float)))) return e;
     launch_kernel(ctx, adapter_pixels_kernel, dim3((unsigned)(a.N * c.at.tiles)), dim3(kThreads), passing, st, c);
     if (int e = check_launch(ctx)) return e;
