@@ -716,11 +716,13 @@ __global__ void __launch_bounds__(kThreads) pack_halves_kernel(const float *__re
 }  // namespace
 
 // The other form writes the result twice and takes the adapter's products in FP32, which costs the more the larger the rank; this one lays the
-// pixels out first.  us, here / there, rank 8 and 32, batch 64 unless said: 256 -> 768 on 28 x 28 110 / 209 and 114 / 338; 256 -> 256 74 / 92 and 74 /
-// 173; 128 -> 128 37 / 38 and 38 / 78; 64 -> 64 27 / 24 and 27 / 47; 256 -> 256 on 14 x 14 30 / 33 and 30 / 61; 512 -> 128 on 28 x 28 119 / 104 and 119 /
-// 236; batch 128, 512 -> 512 on 14 x 14 94 / 136 and 95 / 224, on 8 x 8 56 / 46 and 57 / 82; batch 4, 320 -> 960 on 32 x 32 40 / 35 and 40 / 61.  Few
-// channels, ranks 16 and 32: batch 95, 11 -> 52 on 11 x 19 20.2 / 14.4 and 20.4 / 20.5, batch 41, 41 -> 17 on 32 x 8 15.3 / 10.2 and 15.4 / 14.1.  Few
-// tiles, many operations: batch 31, 390 -> 135, rank 31 on 11 x 20 35.4 / 58.6.
+// pixels out first.  us, here / there, back to back on three sets of tensors in turn, rank 8 and 32, batch 64 unless said: 256 -> 768 on 28 x 28 126 / 220
+// and 126 / 369; 256 -> 256 77 / 100 and 78 / 192; 128 -> 128 45 / 44 and 45 / 88; 64 -> 64 34 / 26 and 34 / 51; 256 -> 256 on 14 x 14 31 / 34 and 31 /
+// 68; 512 -> 128 on 28 x 28 122 / 115 and 120 / 263; batch 128, 512 -> 512 on 14 x 14 102 / 143 and 103 / 236, on 8 x 8 55 / 51 and 55 / 88; batch 4, 320 ->
+// 960 on 32 x 32 31 / 36 and 32 / 63.  Few channels, ranks 16 and 32: batch 95, 11 -> 52 on 11 x 19 20.1 / 14.7 and 20.4 / 20.8, batch 41, 41 -> 17 on
+// 32 x 8 14.2 / 10.7 and 14.1 / 15.4.  Few tiles, many operations: batch 31, 390 -> 135, rank 31 on 11 x 20 37.5 / 59.0; batch 20, 256 -> 512, rank 24 on
+// 14 x 14 26.6 / 38.4.  Near the line: batch 64, 64 -> 64, rank 16 on 28 x 28 34 / 34, batch 80, 96 -> 160, rank 16 on 9 x 10 18.3 / 17.6, 64 -> 96, rank 9
+// on 8 x 8 14.6 / 11.3.
 bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms) {
     const long long tiles = (long long)N * ceil_div(HW, kTile) * ceil_div(blocks_of(K), kFilterTile);
     if (HW < 64 || tiles >= (1 << 28)) return false;

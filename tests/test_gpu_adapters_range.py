@@ -3,6 +3,7 @@ filters and adapters' rows of very different size, long reductions, sums that lo
 math modes' own (gpu_util.TOL) where nothing else is said, taken for each output channel by itself where channels differ in size."""
 import numpy as np
 import pytest
+import torch
 
 import test_gpu_adapters as A
 from gpu_util import B, TOL, ctx, dev, from_blk, new_blk, rel_err, to_blk
@@ -127,3 +128,69 @@ def test_scales_of_adapters_far_from_one(mode):
     layer.up[2] *= 1e-30
     ids = (np.arange(80) % 6 - 1).astype(np.int32)
     assert rel_err(layer.run(x, ids, mode), layer.ref(x, ids)) <= TOL[mode]
+
+
+@pytest.mark.parametrize("mode", ["3xtf32", "tf32"])
+def test_repeatable_on_streams_and_in_a_graph(mode):
+    """The tensor-core form: two calls at once with workspaces of their own, then a captured one whose adapters and inputs change between replays."""
+    rng = np.random.default_rng(77)
+    N, H, W = 80, 12, 11
+    layer, x = A.Layer(rng, 200, 300, 20, 5), rng.standard_normal((N, 200, H, W)).astype(np.float32)
+    on_tensor_cores(layer, N, H, W)
+    ids = rng.integers(-1, 5, N).astype(np.int32)
+    first = layer.run(x, ids, mode)
+    assert np.array_equal(layer.run(x, ids, mode), first)
+    blk, idt = to_blk(x), dev(ids)
+    outs, wss = [new_blk(N, 300, H, W) for _ in range(2)], [layer.workspace(N, H, W) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, o, ws in zip(streams, outs, wss):
+            with torch.cuda.stream(s):
+                layer.call(blk, idt, o, ws, N, H, W, B.MATH[mode])
+    torch.cuda.synchronize()
+    for o in outs:
+        assert np.array_equal(from_blk(o, N, 300, H, W), first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.call(blk, idt, outs[0], wss[0], N, H, W, B.MATH[mode])
+    for i in range(3):
+        y, other = (x * (i + 1)).astype(np.float32), rng.integers(-1, 5, N).astype(np.int32)
+        blk.copy_(to_blk(y))
+        idt.copy_(dev(other))
+        graph.replay()
+        assert rel_err(from_blk(outs[0], N, 300, H, W), layer.ref(y, other)) <= TOL[mode]
+    assert B.small_device_status(ctx()) == B.OK
+
+
+@pytest.mark.parametrize("mode", ["3xtf32", "tf32"])
+@pytest.mark.parametrize("N,C,K,H,W,R", [(80, 33, 290, 8, 8, 9), (9, 70, 1111, 21, 19, 128), (80, 130, 257, 8, 9, 33), (300, 64, 32, 8, 8, 100), (3, 500, 800, 56, 55, 17)])
+def test_every_edge_of_a_tile(N, C, K, H, W, R, mode):
+    """Pixels that end inside a warp's 32, filters that end inside a block and inside a tile, the previous output added, with and without ReLU."""
+    rng = np.random.default_rng(78)
+    layer, x = A.Layer(rng, C, K, R, 3), rng.standard_normal((N, C, H, W)).astype(np.float32)
+    on_tensor_cores(layer, N, H, W)
+    ids = (np.arange(N) % 4 - 1).astype(np.int32)
+    before = rng.standard_normal((N, K, H, W)).astype(np.float32)
+    plain = layer.ref(x, ids)
+    assert by_channel(layer.run(x, ids, mode), plain) <= TOL[mode]
+    assert rel_err(layer.run(x, ids, mode, before=before), plain + before) <= TOL[mode]
+    assert rel_err(layer.run(x, ids, mode, relu=True, before=before), np.maximum(plain + before, 0)) <= TOL[mode]
+
+
+@pytest.mark.parametrize("mode", ["3xtf32", "tf32"])
+def test_values_that_are_not_finite_stay_with_their_pixel(mode):
+    rng = np.random.default_rng(79)
+    layer, x = A.Layer(rng, 96, 160, 16, 4), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    on_tensor_cores(layer, 80, 9, 10)
+    ids = (np.arange(80) % 5 - 1).astype(np.int32)
+    ref = layer.ref(x, ids)
+    x[7, 50, 3, 4], x[11, 0, 8, 9], x[20, 95, 0, 0] = np.nan, np.inf, -np.inf
+    layer.up[3, 10, 5] = np.nan                                 # filter 10 of the images that use adapter 3
+    got = layer.run(x, ids, mode)
+    for n, p in ((7, (3, 4)), (11, (8, 9)), (20, (0, 0))):
+        assert not np.isfinite(got[(n, slice(None)) + p]).any()
+        got[(n, slice(None)) + p] = ref[(n, slice(None)) + p]
+    assert np.isnan(got[ids == 3, 10]).all()
+    got[ids == 3, 10] = ref[ids == 3, 10]
+    assert rel_err(got, ref) <= TOL[mode]
