@@ -420,15 +420,16 @@ __global__ void __launch_bounds__(kBlock<DP, kGeneral>, 1) attention_tc_kernel(c
             tc_fence_after();
             const uint32_t st = s_at(buffer) + lanes + half * kKeys;
             const float f = q_drop * drops.x, scale2 = f * kLog2e;
-            const float to_cap = fminf(f * over_cap, FLT_MAX);           // (an infinite one would make NaN of a score of 0)
             // The scores, in chunks of 32 keys: the last two stay in registers between the maximum and the exponentials.
             constexpr int kChunks = kKeys / 32;
             float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, one[32], two[32];
             auto take = [&](float (&v)[32], int g) {     // scores as the softmax takes them; the largest of each in `top`
                 if (kGeneral) {
-                    if (a.cap > 0.0f)
+                    if (a.cap > 0.0f) {
+                        const float to_cap = fminf(f * over_cap, FLT_MAX);           // (an infinite one would make NaN of a score of 0)
 #pragma unroll
                         for (int u = 0; u < 32; u += 2) capped(v[u], v[u + 1], cap2, to_cap);
+                    }
                     if (bias) {
                         const float f1 = a.cap > 0.0f ? 1.0f : scale2;
                         const int *place = sh.places[t % kPlaces] + half * kKeys + g;
