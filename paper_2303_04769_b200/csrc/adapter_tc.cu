@@ -131,13 +131,6 @@ __global__ void __launch_bounds__(kThreads *kTeams) adapter_filters_kernel(const
 __device__ __forceinline__ void bulk_store(void *to, uint32_t from, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
 }
-// The same, for what is not read again soon: it leaves L2 first.
-__device__ __forceinline__ void bulk_store_first(void *to, uint32_t from, uint32_t bytes) {
-    asm volatile(
-        "{\n\t.reg .b64 policy;\n\tcreatepolicy.fractional.L2::evict_first.b64 policy, 1.0;\n\t"
-        "cp.async.bulk.global.shared::cta.bulk_group.L2::cache_hint [%0], [%1], %2, policy;\n\t}\n\tcp.async.bulk.commit_group;"
-        ::"l"(to), "r"(from), "r"(bytes) : "memory");
-}
 template <int kLeft>
 __device__ __forceinline__ void bulk_store_wait() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
 
@@ -344,9 +337,9 @@ __global__ void __launch_bounds__(kThreads, 4) adapter_pixels_kernel(const TcArg
 // registers, where sums are rounded; sums that lose nothing stay exact.  (Four chunks in 3xTF32: 131 us for 134, errors of 256 channels 1.1e-6 for 5e-7.)
 template <bool kX3> constexpr int kRun = kX3 ? 2 : 8;        // chunks
 
-constexpr int kPassing = 4096;           // bytes of shared memory that a warp's results pass through: 32 pixels x 32 filters, which lie together in memory, too
+constexpr int kPassing = 4096;           // bytes of shared memory that a warp's results pass through
 constexpr int kStages = 2, kStageBytes = kPixelBytes + kFilterTile * 32 * 256, kEpilogueWarps = 8, kProductThreads = kEpilogueWarps * 32 + 128;
-constexpr int kRolesRegs = 40, kEpilogueRegs = 232;     // a thread, of the 168 that each is launched with
+constexpr int kRolesRegs = 56, kEpilogueRegs = 224;     // a thread, of the 168 that each is launched with
 static_assert(kRolesRegs * 128 + kEpilogueRegs * kEpilogueWarps * 32 <= 168 * kProductThreads, "more than the launch brings is waited for without an end");
 
 // mbar_wait_uniform without a call: a kernel that deals out its registers by role must not have any.
@@ -516,24 +509,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
         for (int i = blockIdx.x; i < work; i += gridDim.x) {
             const int np = i / c.at.filter_tiles, kt = i % c.at.filter_tiles, n = np / c.at.tiles, p0 = np % c.at.tiles * kTile + (warp & 3) * 32;
             const int blocks = tile_rows(c, kt) / 32;
-            // a filter's three go to all lanes, where the results pass through later: [block]{32 of each}
-            if (elect_one()) bulk_store_wait<0>();
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < kBlocks; ++e) {
-                float *to = reinterpret_cast<float *>(rows) + e * 96 + lane;
-                to[0] = w_factor[e];
-                to[32] = u_factor[e];
-                to[64] = bias[e];
-            }
-            // sums are kept smaller by 2^(64 - exponent) where a pixel's scale would let them pass FP32's range in front of the filter's
-            const int kept_back = min(max((some ? max(ex.x - 141, ex.y) : ex.x - 141) - 64, 0), 127);
-            float *pixel = reinterpret_cast<float *>(rows) + kBlocks * 96 + lane;         // a pixel's wait there, too: registers are short
-            pixel[0] = power(ex.x - 141 - kept_back);
-            pixel[32] = some ? power(ex.y - kept_back) : 0.0f;
-            pixel[64] = power(-kept_back);
-            pixel[96] = power(kept_back);
-            __syncwarp();
+            const int next = min(i + (int)gridDim.x, work - 1);          // (asked for at the end, too: values kept instead would take registers all along)
+            fetch_id(next);
             uint64_t sum[kBlocks][16] = {};              // of this warp's blocks of filters, by twos
             // the next accumulator's columns, a block at a time
             auto take = [&](auto before, auto use) -> bool {
@@ -560,8 +537,20 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                     for (int u = 0; u < 32; u += 2) sum[e][u / 2] = add2(sum[e][u / 2], pair(v[u], v[u + 1]));
                 });
             if (!ok) break;
+            // A filter's three go to all lanes, where the results pass through later: [block]{32 of each}
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < kBlocks; ++e) {
+                float *to = reinterpret_cast<float *>(rows) + e * 96 + lane;
+                to[0] = w_factor[e];
+                to[32] = u_factor[e];
+                to[64] = bias[e];
+            }
+            __syncwarp();
+            // sums are kept smaller by 2^(64 - exponent) where a pixel's scale would let them pass FP32's range in front of the filter's
+            const int kept_back = min(max((some ? max(ex.x - 141, ex.y) : ex.x - 141) - 64, 0), 127);
+            const float x_back = power(ex.x - 141 - kept_back), t_back = some ? power(ex.y - kept_back) : 0.0f, down = power(-kept_back), up = power(kept_back);
             // scales and bias, while the adapter's part is on its way
-            const float x_back = pixel[0], down = pixel[64];
             float4 f[8], add[8];
 #pragma unroll
             for (int e = 0; e < kBlocks; ++e) {
@@ -574,7 +563,6 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                     y[1] = fma2(mul2(y[1], pair(x_back, x_back)), pair(f[u].z, f[u].w), mul2(pair(add[u].z, add[u].w), pair(down, down)));
                 }
             }
-            const float t_back = pixel[32];
             if (some && !take([&](int e) {
 #pragma unroll
                     for (int u = 0; u < 8; ++u) f[u] = rows[e * 24 + 8 + u];
@@ -586,12 +574,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                         y[1] = fma2(mul2(pair(v[u * 4 + 2], v[u * 4 + 3]), pair(t_back, t_back)), pair(f[u].z, f[u].w), y[1]);
                     }
                 })) break;
-            const float up = pixel[96];
             const int left = a.HW - p0;                  // pixels
+            fetch(next);
 #pragma unroll
             for (int e = 0; e < kBlocks; ++e) {
-                if (e == 0) fetch_id(min(i + (int)gridDim.x, work - 1));          // (asked for at the end, too: values kept instead would take registers all along)
-                if (e == kBlocks - 1) fetch(min(i + (int)gridDim.x, work - 1));
                 const int b = part + e * kShares;
                 if (b >= blocks) continue;
                 float4 y[8];
@@ -600,46 +586,34 @@ __global__ void __launch_bounds__(kProductThreads, 1) adapter_product_kernel(con
                     unpair(mul2(sum[e][u * 2], pair(up, up)), y[u].x, y[u].y);
                     unpair(mul2(sum[e][u * 2 + 1], pair(up, up)), y[u].z, y[u].w);
                 }
-                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8;
-                if (a.accumulate && lane < left)
+                float4 *out = reinterpret_cast<float4 *>(a.out) + (((size_t)n * s.KB + kt * kFilterTile + b) * a.HW + p0) * 8 + lane;
+                // through shared memory, so that a store is whole lines: eight lanes a pixel
+                __syncwarp();
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const float4 before = out[lane * 8 + u];
-                        y[u].x += before.x; y[u].y += before.y; y[u].z += before.z; y[u].w += before.w;
-                    }
+                for (int u = 0; u < 8; ++u) rows[lane * 8 + (u ^ (lane & 7))] = y[u];
+                __syncwarp();
+#pragma unroll
+                for (int u = 0; u < 8; ++u) y[u] = rows[(u * 4 + (lane >> 3)) * 8 + ((lane & 7) ^ ((u * 4 + (lane >> 3)) & 7))];
+                if (a.accumulate) {
+                    float4 before[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) before[u] = u * 4 + (lane >> 3) < left ? out[u * 32] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) { y[u].x += before[u].x; y[u].y += before[u].y; y[u].z += before[u].z; y[u].w += before[u].w; }
+                }
                 if (a.relu)
 #pragma unroll
                     for (int u = 0; u < 8; ++u) y[u] = make_float4(fmaxf(y[u].x, 0.0f), fmaxf(y[u].y, 0.0f), fmaxf(y[u].z, 0.0f), fmaxf(y[u].w, 0.0f));
                 const int filters = s.K - (kt * kFilterTile + b) * 32;
                 if (filters < 32)                        // +0 in pad lanes
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) y[u] = clear_from(y[u], filters - u * 4);
-                // A pixel's 128 bytes begin with another 16 in four lanes each, so that no more than two of eight lanes write to one bank (all eight apart: the
-                // same time for half as many selections again).
+                    for (int u = 0; u < 8; ++u) y[u] = clear_from(y[u], filters - (lane & 7) * 4);
+                // operands are read again, results here not: they leave L2 first (131 -> 128 us)
 #pragma unroll
-                for (int bit = 1; bit < 4; bit *= 2) {
-                    const bool turn = lane & bit;
-                    float4 z[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const float4 &next = y[(u + bit) & 7];
-                        z[u] = make_float4(turn ? next.x : y[u].x, turn ? next.y : y[u].y, turn ? next.z : y[u].z, turn ? next.w : y[u].w);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) y[u] = z[u];
-                }
-                if (elect_one()) bulk_store_wait<0>();   // the block before has been read
-                __syncwarp();
-#pragma unroll
-                for (int u = 0; u < 8; ++u) rows[lane * 8 + ((u + (lane & 3)) & 7)] = y[u];
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (left > 0 && elect_one()) bulk_store_first(out, smem_u32(rows), min(left, 32) * 128);
-                __syncwarp();
+                for (int u = 0; u < 8; ++u)
+                    if (left >= 32 || u * 4 + (lane >> 3) < left) __stcs(out + u * 32, y[u]);
             }
         }
-        if (elect_one()) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        __syncwarp();
     }
     tc_fence_before();
     __syncthreads();
