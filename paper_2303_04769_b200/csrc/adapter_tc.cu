@@ -11,7 +11,7 @@
 //   256 filters a tile: 96 KB of operands for 1536 cycles of MMAs (62 bytes a cycle and SM from L2).
 //
 // Batch 64, 256 -> 768, 28 x 28, rank 16: 134 us.  Pixels 36 (the filters, 5, beside them): the largest values, while memory still takes the result
-// before, then four chunks that wait for their loads.  Product 83: MMAs some 45 % of the time; what a stage takes to load, and the epilogue's sums, scales
+// before, then four chunks that wait for their loads.  Product 83: MMAs half of the time; what a stage takes to load, and the epilogue's sums, scales
 // and stores, fill the rest.  With an accumulator for all of a tile's steps 72, see kRun; of 168 registers a thread for all roles 94, as the epilogue's sums spill.
 // Floor 33 for the bytes, 37 for three products.
 #include "adapter.cuh"
@@ -690,13 +690,13 @@ __global__ void __launch_bounds__(kThreads) pack_halves_kernel(const float *__re
 }  // namespace
 
 // The other form writes the result twice and takes the adapter's products in FP32, which costs the more the larger the rank; this one lays the
-// pixels out first.  us, here / there, back to back on three sets of tensors in turn, rank 8 and 32, batch 64 unless said: 256 -> 768 on 28 x 28 126 / 220
-// and 126 / 369; 256 -> 256 77 / 100 and 78 / 192; 128 -> 128 45 / 44 and 45 / 88; 64 -> 64 34 / 26 and 34 / 51; 256 -> 256 on 14 x 14 31 / 34 and 31 /
-// 68; 512 -> 128 on 28 x 28 122 / 115 and 120 / 263; batch 128, 512 -> 512 on 14 x 14 102 / 143 and 103 / 236, on 8 x 8 55 / 51 and 55 / 88; batch 4, 320 ->
-// 960 on 32 x 32 31 / 36 and 32 / 63.  Few channels, ranks 16 and 32: batch 95, 11 -> 52 on 11 x 19 20.1 / 14.7 and 20.4 / 20.8, batch 41, 41 -> 17 on
-// 32 x 8 14.2 / 10.7 and 14.1 / 15.4.  Few tiles, many operations: batch 31, 390 -> 135, rank 31 on 11 x 20 37.5 / 59.0; batch 20, 256 -> 512, rank 24 on
-// 14 x 14 26.6 / 38.4.  Near the line: batch 64, 64 -> 64, rank 16 on 28 x 28 34 / 34, batch 80, 96 -> 160, rank 16 on 9 x 10 18.3 / 17.6, 64 -> 96, rank 9
-// on 8 x 8 14.6 / 11.3.
+// pixels out first.  us, here / there, back to back on three sets of tensors in turn, rank 8 and 32, batch 64 unless said: 256 -> 768 on 28 x 28 124 / 220
+// and 125 / 369; 256 -> 256 77 / 100 and 78 / 192; 128 -> 128 44 / 44 and 44 / 88; 64 -> 64 33 / 26 and 33 / 51; 256 -> 256 on 14 x 14 30 / 34 and 30 /
+// 68; 512 -> 128 on 28 x 28 121 / 115 and 119 / 263; batch 128, 512 -> 512 on 14 x 14 100 / 143 and 101 / 236, on 8 x 8 54 / 51 and 54 / 88; batch 4, 320 ->
+// 960 on 32 x 32 32 / 36 and 33 / 63.  Few channels, ranks 16 and 32: batch 95, 11 -> 52 on 11 x 19 20.0 / 14.7 and 20.0 / 20.8, batch 41, 41 -> 17 on
+// 32 x 8 14.2 / 10.7 and 14.1 / 15.4.  Few tiles, many operations: batch 31, 390 -> 135, rank 31 on 11 x 20 37.0 / 59.0; batch 20, 256 -> 512, rank 24 on
+// 14 x 14 26.1 / 38.4.  Near the line: batch 64, 64 -> 64, rank 16 on 28 x 28 33 / 34, batch 80, 96 -> 160, rank 16 on 9 x 10 17.8 / 17.6, 64 -> 96, rank 9
+// on 8 x 8 14.3 / 11.3.
 bool adapted_tc_preferred(int N, int C, int K, int HW, int R, int sms) {
     const long long tiles = (long long)N * ceil_div(HW, kTile) * ceil_div(blocks_of(K), kFilterTile);
     if (HW < 64 || tiles >= (1 << 28)) return false;

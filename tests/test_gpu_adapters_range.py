@@ -194,3 +194,20 @@ def test_values_that_are_not_finite_stay_with_their_pixel(mode):
     assert np.isnan(got[ids == 3, 10]).all()
     got[ids == 3, 10] = ref[ids == 3, 10]
     assert rel_err(got, ref) <= TOL[mode]
+
+
+@pytest.mark.parametrize("mode", A.MODES)
+@pytest.mark.parametrize("w_size", [1.0, 2.0 ** 70, 2.0 ** -70])
+def test_pixels_at_the_ends_of_the_range(w_size, mode):
+    """Pixels from 1e-33 to 1e35, beside filters that bring the results back in, or not so far out: each pixel keeps its own accuracy."""
+    rng = np.random.default_rng(80)
+    layer, x = A.Layer(rng, 96, 160, 12, 3, bias=False), rng.standard_normal((80, 96, 9, 10)).astype(np.float32)
+    on_tensor_cores(layer, 80, 9, 10)
+    sizes = np.array([1e-33, 1e-20, 1.0, 1e12] + [1e16 if w_size > 1 else 1e35])
+    size = sizes[np.arange(90) % 5].reshape(9, 10)
+    x = (x * size).astype(np.float32)
+    layer.w, layer.up = (layer.w * w_size).astype(np.float32), (layer.up * w_size).astype(np.float32)
+    ids = (np.arange(80) % 4 - 1).astype(np.int32)
+    seen = size * w_size > 1e-30                                # below it, TF32 pairs and FP32's own products lose bits to the smallest numbers
+    got, ref = layer.run(x, ids, mode)[:, :, seen] / (size * w_size)[seen], layer.ref(x, ids)[:, :, seen] / (size * w_size)[seen]
+    assert rel_err(got, ref) <= TOL[mode]
